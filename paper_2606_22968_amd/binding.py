@@ -24,7 +24,7 @@ MOCAP_ERR_HIP = 4
 # MOCAP_NOALLOC_SCRATCH_BYTES: the static device scratch of mocap_chunk_attn_noalloc.
 NOALLOC_SCRATCH_BYTES = 128 << 20
 
-# Every entry point the header declares.
+# Every entry point mocap_attn.h declares.
 EXPORTED = (
     "mocap_kv_append",
     "mocap_chunk_attn_workspace_size",
@@ -42,6 +42,20 @@ EXPORTED = (
     "mocap_lbcp_refine_e2e",
     "mocap_status_string",
     "mocap_check_block_table",
+)
+
+# Every entry point mocap_serve.h declares.
+SERVE_EXPORTED = (
+    "mocap_decode_append",
+    "mocap_decode_attn_workspace_size",
+    "mocap_decode_attn",
+    "mocap_window_attn_workspace_size",
+    "mocap_window_attn",
+    "mocap_key_weights_workspace_size",
+    "mocap_key_weights",
+    "mocap_decode_key_weights",
+    "mocap_kv_evict_workspace_size",
+    "mocap_kv_evict",
 )
 
 
@@ -171,6 +185,27 @@ def load_library():
     lib.mocap_chunk_prefixes.restype = st
     lib.mocap_chunk_prefixes.argtypes = [
         ctypes.POINTER(ctypes.c_int32), ctypes.c_int32, ctypes.POINTER(ctypes.c_int64)]
+    i32, i64, ptr, size = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t
+    store, size_out = ctypes.POINTER(mocap_kv_store), ctypes.POINTER(ctypes.c_size_t)
+    serve = dict(
+        mocap_decode_append=[store, ptr, i32, ptr, i32, ptr, ptr, ptr],
+        mocap_decode_attn_workspace_size=[i32, i64, i32, i32, i32, i64, i64, size_out],
+        mocap_decode_attn=[store, ptr, i32, ptr, i32, i64, ptr, i32, i32, i32, ctypes.c_float, i64, i64, ptr, ptr, ptr,
+                           size, ptr],
+        mocap_window_attn_workspace_size=[i64, i32, i32, i32, i32, i64, i64, i32, ctypes.POINTER(i32), size_out],
+        mocap_window_attn=[store, ptr, i32, ptr, i64, i32, i32, i32, i32, ctypes.c_float, i64, i64, ptr, ptr, ptr, size,
+                           i32, ptr],
+        mocap_key_weights_workspace_size=[i64, i32, i32, i32, i32, size_out],
+        mocap_key_weights=[store, ptr, i32, ptr, i64, i32, i32, i32, i32, ctypes.c_float, ptr, ptr, ptr, i64, ptr, size,
+                           ptr],
+        mocap_decode_key_weights=[store, ptr, i32, ptr, i32, i64, ptr, i32, i32, i32, ctypes.c_float, ptr, ptr, ptr, i64,
+                                  ptr],
+        mocap_kv_evict_workspace_size=[i64, i32, i32, size_out],
+        mocap_kv_evict=[store, ptr, i32, store, ptr, i32, i64, i32, i32, i32, ptr, i64, ptr, ptr, ptr, size, ptr],
+    )
+    for name, argtypes in serve.items():
+        f = getattr(lib, name)
+        f.restype, f.argtypes = st, argtypes
     _lib = lib
     return lib
 
@@ -502,3 +537,222 @@ def mocap_lbcp_refine_e2e(seq_len: int, num_chunks: int, num_stages: int, align:
         float(temp_min), float(alpha), int(rounds), int(seed) & 0xFFFFFFFFFFFFFFFF, io, ctypes.byref(b),
         ctypes.byref(pre), ctypes.byref(t)), "mocap_lbcp_refine_e2e")
     return list(io), b.value, pre.value, t.value
+
+
+# ---- After the prefill (mocap_serve.h) ----
+
+def _workspace(workspace: Optional[torch.Tensor]):
+    if workspace is None:
+        return None, 0
+    _require(workspace, workspace.dtype if isinstance(workspace, torch.Tensor) else None, "workspace")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _one_device(*tensors) -> None:
+    """Every tensor on the current device, where the call enqueues its work."""
+    device = _raw_device()
+    for t in tensors:
+        if t is not None and t.device.index != device:
+            raise ValueError(f"a tensor on {t.device}, but the current device is cuda:{device}")
+
+
+def _batch(store: KvStore, block_tables: torch.Tensor, seq_lens: torch.Tensor, max_len: Optional[int], window: int = 0,
+           sinks: int = 0) -> int:
+    """Checks a batch's tables and lengths; returns max_len."""
+    _require(block_tables, torch.int32, "block_tables", 2)
+    _require(seq_lens, torch.int32, "seq_lens", 1)
+    if block_tables.shape[0] != seq_lens.shape[0]:
+        raise ValueError("block_tables must be [batch][table_stride] and seq_lens [batch]")
+    _one_device(store.k_pool, store.v_pool, block_tables, seq_lens)
+    capacity = block_tables.shape[1] * store.block_size
+    max_len = min(capacity, (1 << 31) - 128) if max_len is None else int(max_len)
+    if _check_tables:
+        for table, n in zip(block_tables.cpu(), seq_lens.tolist()):
+            n = min(n, max_len)
+            low = max(0, n - window) if window > 0 else 0
+            mocap_check_block_table(table, 0, max(0, min(sinks, low)), store.block_size, store.num_blocks)
+            mocap_check_block_table(table, low, max(low, n), store.block_size, store.num_blocks)
+    return max_len
+
+
+def mocap_decode_append(store: KvStore, block_tables: torch.Tensor, seq_lens: torch.Tensor, k: torch.Tensor,
+                        v: torch.Tensor, stream=None) -> None:
+    """Stores row b of k and v (bf16 [batch][h_kv][head_dim]) at position seq_lens[b] - 1 of sequence b."""
+    _batch(store, block_tables, seq_lens, None)
+    batch = seq_lens.shape[0]
+    for name, t in (("k", k), ("v", v)):
+        _require(t, torch.bfloat16, name, 3)
+        if tuple(t.shape) != (batch, store.h_kv, store.head_dim):
+            raise ValueError("k/v must be [batch][h_kv][head_dim] of the store")
+    _one_device(k, v)
+    desc = store.descriptor()
+    _check(load_library().mocap_decode_append(
+        ctypes.byref(desc), block_tables.data_ptr(), block_tables.shape[1], seq_lens.data_ptr(), batch, k.data_ptr(),
+        v.data_ptr(), _stream_handle(stream)), "mocap_decode_append")
+
+
+def mocap_decode_attn_workspace_size(batch: int, h_q: int, h_kv: int, head_dim: int, max_len: int, window: int = 0,
+                                     sinks: int = 0) -> int:
+    nbytes = ctypes.c_size_t(0)
+    _check(load_library().mocap_decode_attn_workspace_size(
+        int(batch), int(max_len), int(h_q), int(h_kv), int(head_dim), int(window), int(sinks), ctypes.byref(nbytes)),
+        "mocap_decode_attn_workspace_size")
+    return nbytes.value
+
+
+def mocap_decode_attn(store: KvStore, block_tables: torch.Tensor, seq_lens: torch.Tensor, q: torch.Tensor,
+                      max_len: Optional[int], scale: float, o: torch.Tensor, lse: torch.Tensor,
+                      workspace: Optional[torch.Tensor] = None, window: int = 0, sinks: int = 0, stream=None) -> None:
+    """q, o: bf16 [batch][h_q][head_dim]; lse: fp32 [batch][h_q]; max_len None: what the tables hold."""
+    max_len = _batch(store, block_tables, seq_lens, max_len, int(window), int(sinks))
+    _require(q, torch.bfloat16, "q", 3)
+    _require(o, torch.bfloat16, "o", 3)
+    _require(lse, torch.float32, "lse", 2)
+    batch, h_q, head_dim = q.shape
+    if batch != seq_lens.shape[0] or o.shape != q.shape or tuple(lse.shape) != (batch, h_q):
+        raise ValueError("q and o must be [batch][h_q][head_dim] and lse [batch][h_q]")
+    _one_device(q, o, lse, workspace)
+    ws_ptr, ws_bytes = _workspace(workspace)
+    desc = store.descriptor()
+    _check(load_library().mocap_decode_attn(
+        ctypes.byref(desc), block_tables.data_ptr(), block_tables.shape[1], seq_lens.data_ptr(), batch, max_len,
+        q.data_ptr(), h_q, store.h_kv, head_dim, float(scale), int(window), int(sinks), o.data_ptr(), lse.data_ptr(),
+        ws_ptr, ws_bytes, _stream_handle(stream)), "mocap_decode_attn")
+
+
+def mocap_window_attn_workspace_size(prefix_len: int, chunk_len: int, h_q: int, h_kv: int, head_dim: int, window: int,
+                                     sinks: int = 0, num_splits: int = 0) -> Tuple[int, int]:
+    """Returns (number of KV ranges, workspace bytes)."""
+    splits = ctypes.c_int32(0)
+    nbytes = ctypes.c_size_t(0)
+    _check(load_library().mocap_window_attn_workspace_size(
+        int(prefix_len), int(chunk_len), int(h_q), int(h_kv), int(head_dim), int(window), int(sinks), int(num_splits),
+        ctypes.byref(splits), ctypes.byref(nbytes)), "mocap_window_attn_workspace_size")
+    return splits.value, nbytes.value
+
+
+def mocap_window_attn(store: KvStore, block_table: torch.Tensor, q: torch.Tensor, prefix_len: int, scale: float,
+                      window: int, sinks: int, o: torch.Tensor, lse: torch.Tensor,
+                      workspace: Optional[torch.Tensor] = None, num_splits: int = 0, stream=None) -> None:
+    """As mocap_chunk_attn, each row seeing its last `window` positions and the first `sinks`."""
+    _require(block_table, torch.int32, "block_table", 1)
+    _require(q, torch.bfloat16, "q", 3)
+    _require(o, torch.bfloat16, "o", 3)
+    _require(lse, torch.float32, "lse", 2)
+    chunk_len, h_q, head_dim = q.shape
+    if o.shape != q.shape or tuple(lse.shape) != (h_q, chunk_len):
+        raise ValueError("o must match q and lse must be [h_q][chunk_len]")
+    _one_device(store.k_pool, store.v_pool, block_table, q, o, lse, workspace)
+    ws_ptr, ws_bytes = _workspace(workspace)
+    end = int(prefix_len) + chunk_len
+    _maybe_check(store, block_table, 0, min(int(sinks), end))
+    _maybe_check(store, block_table, max(0, int(prefix_len) - int(window) + 1), end)
+    desc = store.descriptor()
+    _check(load_library().mocap_window_attn(
+        ctypes.byref(desc), block_table.data_ptr(), block_table.numel(), q.data_ptr(), int(prefix_len), chunk_len, h_q,
+        store.h_kv, head_dim, float(scale), int(window), int(sinks), o.data_ptr(), lse.data_ptr(), ws_ptr, ws_bytes,
+        int(num_splits), _stream_handle(stream)), "mocap_window_attn")
+
+
+def mocap_key_weights_workspace_size(prefix_len: int, chunk_len: int, h_q: int, h_kv: int, head_dim: int) -> int:
+    nbytes = ctypes.c_size_t(0)
+    _check(load_library().mocap_key_weights_workspace_size(
+        int(prefix_len), int(chunk_len), int(h_q), int(h_kv), int(head_dim), ctypes.byref(nbytes)),
+        "mocap_key_weights_workspace_size")
+    return nbytes.value
+
+
+def _same_or_apart(prev: Optional[torch.Tensor], weights: torch.Tensor, ndim: int) -> Optional[int]:
+    """prev's address; prev must be weights' memory exactly, or none of it."""
+    _require(weights, torch.float32, "weights", ndim)
+    if prev is None:
+        return None
+    _require(prev, torch.float32, "prev", ndim)
+    if prev.shape != weights.shape:
+        raise ValueError("prev must have the shape of weights")
+    a, b, n = prev.data_ptr(), weights.data_ptr(), 4 * weights.numel()
+    if a != b and a < b + n and b < a + n:
+        raise ValueError("prev must be weights itself or not overlap it")
+    return a
+
+
+def mocap_key_weights(store: KvStore, block_table: torch.Tensor, q: torch.Tensor, prefix_len: int, scale: float,
+                      lse: torch.Tensor, prev: Optional[torch.Tensor], weights: torch.Tensor,
+                      workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """q: bf16 [chunk_len][h_q][head_dim]; lse: fp32 [h_q][chunk_len]; prev, weights: fp32 [h_kv][stride], stride at
+    least prefix_len + chunk_len."""
+    _require(block_table, torch.int32, "block_table", 1)
+    _require(q, torch.bfloat16, "q", 3)
+    _require(lse, torch.float32, "lse", 2)
+    chunk_len, h_q, head_dim = q.shape
+    if tuple(lse.shape) != (h_q, chunk_len):
+        raise ValueError("lse must be [h_q][chunk_len]")
+    prev_ptr = _same_or_apart(prev, weights, 2)
+    if weights.shape[0] != store.h_kv:
+        raise ValueError("weights must be [h_kv][stride]")
+    _one_device(store.k_pool, store.v_pool, block_table, q, lse, prev, weights, workspace)
+    ws_ptr, ws_bytes = _workspace(workspace)
+    _maybe_check(store, block_table, 0, int(prefix_len) + chunk_len)
+    desc = store.descriptor()
+    _check(load_library().mocap_key_weights(
+        ctypes.byref(desc), block_table.data_ptr(), block_table.numel(), q.data_ptr(), int(prefix_len), chunk_len, h_q,
+        store.h_kv, head_dim, float(scale), lse.data_ptr(), prev_ptr, weights.data_ptr(), weights.shape[1], ws_ptr,
+        ws_bytes, _stream_handle(stream)), "mocap_key_weights")
+
+
+def mocap_decode_key_weights(store: KvStore, block_tables: torch.Tensor, seq_lens: torch.Tensor, q: torch.Tensor,
+                             max_len: Optional[int], scale: float, lse: torch.Tensor, prev: Optional[torch.Tensor],
+                             weights: torch.Tensor, stream=None) -> None:
+    """q: bf16 [batch][h_q][head_dim]; lse: fp32 [batch][h_q]; prev, weights: fp32 [batch][h_kv][stride], stride at
+    least max_len (None: what the tables hold)."""
+    max_len = _batch(store, block_tables, seq_lens, max_len)
+    _require(q, torch.bfloat16, "q", 3)
+    _require(lse, torch.float32, "lse", 2)
+    batch, h_q, head_dim = q.shape
+    if batch != seq_lens.shape[0] or tuple(lse.shape) != (batch, h_q):
+        raise ValueError("q must be [batch][h_q][head_dim] and lse [batch][h_q]")
+    prev_ptr = _same_or_apart(prev, weights, 3)
+    if tuple(weights.shape[:2]) != (batch, store.h_kv):
+        raise ValueError("weights must be [batch][h_kv][stride]")
+    _one_device(q, lse, prev, weights)
+    desc = store.descriptor()
+    _check(load_library().mocap_decode_key_weights(
+        ctypes.byref(desc), block_tables.data_ptr(), block_tables.shape[1], seq_lens.data_ptr(), batch, max_len,
+        q.data_ptr(), h_q, store.h_kv, head_dim, float(scale), lse.data_ptr(), prev_ptr, weights.data_ptr(),
+        weights.shape[2], _stream_handle(stream)), "mocap_decode_key_weights")
+
+
+def mocap_kv_evict_workspace_size(n: int, h_kv: int, keep: int) -> int:
+    nbytes = ctypes.c_size_t(0)
+    _check(load_library().mocap_kv_evict_workspace_size(int(n), int(h_kv), int(keep), ctypes.byref(nbytes)),
+           "mocap_kv_evict_workspace_size")
+    return nbytes.value
+
+
+def mocap_kv_evict(src: KvStore, src_table: torch.Tensor, dst: KvStore, dst_table: torch.Tensor, n: int, keep: int,
+                   sinks: int, recent: int, weights: torch.Tensor, kept: torch.Tensor,
+                   kept_weights: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                   stream=None) -> None:
+    """weights: fp32 [h_kv][stride], stride at least n; kept: int32 [h_kv][keep]; kept_weights: fp32 [h_kv][keep] or
+    None."""
+    _require(src_table, torch.int32, "src_table", 1)
+    _require(dst_table, torch.int32, "dst_table", 1)
+    _require(weights, torch.float32, "weights", 2)
+    _require(kept, torch.int32, "kept", 2)
+    if weights.shape[0] != src.h_kv or tuple(kept.shape) != (src.h_kv, keep):
+        raise ValueError("weights must be [h_kv][stride] and kept [h_kv][keep]")
+    if kept_weights is not None:
+        _require(kept_weights, torch.float32, "kept_weights", 2)
+        if kept_weights.shape != kept.shape:
+            raise ValueError("kept_weights must be [h_kv][keep]")
+    _one_device(src.k_pool, src.v_pool, dst.k_pool, dst.v_pool, src_table, dst_table, weights, kept, kept_weights,
+                workspace)
+    ws_ptr, ws_bytes = _workspace(workspace)
+    _maybe_check(src, src_table, 0, int(n))
+    _maybe_check(dst, dst_table, 0, int(keep))
+    from_desc, to_desc = src.descriptor(), dst.descriptor()
+    _check(load_library().mocap_kv_evict(
+        ctypes.byref(from_desc), src_table.data_ptr(), src_table.numel(), ctypes.byref(to_desc), dst_table.data_ptr(),
+        dst_table.numel(), int(n), int(keep), int(sinks), int(recent), weights.data_ptr(), weights.shape[1],
+        kept.data_ptr(), kept_weights.data_ptr() if kept_weights is not None else None, ws_ptr, ws_bytes,
+        _stream_handle(stream)), "mocap_kv_evict")

@@ -1,0 +1,518 @@
+// Host side of the calls that follow the prefill (mocap_serve.h): argument
+// validation, how the work is cut, and kernel dispatch.  Every check runs before
+// anything is enqueued.
+#include "mocap_serve.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <memory>
+#include <new>
+
+#include "host_common.h"
+#include "serve.h"
+
+namespace {
+
+using mocap::aligned16;
+using mocap::block_divider;
+using mocap::check_positions;
+using mocap::check_store;
+using mocap::device_cu_count;
+using mocap::kMaxPositions;
+using mocap::kTileKeys;
+using mocap::round_up;
+using mocap::supported_head_dim;
+
+// A grid dimension holds fewer than 2^32 threads; no workgroup has more than 512.
+constexpr int64_t kMaxGroups = ((int64_t)1 << 23) - 1;
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Integer and fp32 arrays are read and written value by value.
+bool aligned4(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 3u) == 0; }
+
+bool valid_scale(float scale) { return scale > 0.f && std::isfinite(scale); }
+
+mocap_status check_heads(int32_t h_q, int32_t h_kv, int32_t head_dim) {
+  if (h_q <= 0 || h_kv <= 0 || h_q % h_kv != 0) return MOCAP_ERR_INVALID_ARG;
+  return supported_head_dim(head_dim) ? MOCAP_OK : MOCAP_ERR_UNSUPPORTED;
+}
+
+// ---- Batches of sequences ----
+
+// How many workgroups a launch that reads a batch aims at per compute unit, and
+// the fewest tiles of a part.
+constexpr int kDecodeGroupsPerCu = 4;
+constexpr int kDecodeMinTiles = 8;
+constexpr int kDecodeHeads = 32;  // query heads of a workgroup, at most
+
+// Fills in how a batch's tiles are cut: per_item workgroups work on an item.
+mocap_status plan_batch(int32_t batch, int64_t max_len, int64_t window, int64_t sinks, int64_t per_item,
+                        int32_t min_tiles, mocap::SeqBatch* s, bool* may_split) {
+  int cus = 0;
+  const mocap_status st = device_cu_count(&cus);
+  if (st != MOCAP_OK) return st;
+  if (window >= max_len) window = 0;
+  int64_t most = ceil_div(max_len, kTileKeys);
+  if (window > 0) most = std::min(most, ceil_div(window, kTileKeys) + 1 + ceil_div(std::min(sinks, max_len), kTileKeys));
+  s->batch = batch;
+  s->max_len = (int32_t)max_len;
+  s->window = (int32_t)window;
+  s->sinks = (int32_t)(window > 0 ? std::min(sinks, max_len) : 0);
+  s->target = (int32_t)ceil_div((int64_t)cus * kDecodeGroupsPerCu, per_item);
+  s->min_tiles = min_tiles;
+  const int64_t items = std::min<int64_t>((int64_t)s->target + batch, batch * std::max<int64_t>(1, ceil_div(most, min_tiles)));
+  if (items * per_item > kMaxGroups) return MOCAP_ERR_UNSUPPORTED;
+  s->items = (int32_t)items;
+  *may_split = most > min_tiles;
+  return MOCAP_OK;
+}
+
+// Checks of a batch's tables and lengths.
+mocap_status check_batch(const mocap_kv_store* kv, const int32_t* block_tables, int32_t table_stride,
+                         const int32_t* seq_lens, int32_t batch, int64_t max_len) {
+  const mocap_status st = check_store(kv);
+  if (st != MOCAP_OK) return st;
+  if (batch < 0 || table_stride < 0 || max_len < 0 || max_len > kMaxPositions) return MOCAP_ERR_INVALID_ARG;
+  if (max_len > (int64_t)table_stride * kv->block_size) return MOCAP_ERR_INVALID_ARG;
+  if (batch == 0) return MOCAP_OK;
+  if (!kv->k_pool || !kv->v_pool || !block_tables || !seq_lens) return MOCAP_ERR_INVALID_ARG;
+  if (!aligned16(kv->k_pool) || !aligned16(kv->v_pool) || !aligned4(block_tables) || !aligned4(seq_lens))
+    return MOCAP_ERR_INVALID_ARG;
+  return MOCAP_OK;
+}
+
+void set_tables(const mocap_kv_store* kv, const int32_t* block_tables, int32_t table_stride, const int32_t* seq_lens,
+                mocap::SeqBatch* s) {
+  s->tables = block_tables;
+  s->seq_lens = seq_lens;
+  s->table_stride = table_stride;
+  s->block_size = kv->block_size;
+  block_divider((uint32_t)kv->block_size, &s->block_magic, &s->block_shift);
+}
+
+#ifdef MOCAP_DEBUG_TABLES
+// Every entry that the visible positions of a sequence use names a block.
+// Sequences may share blocks.
+mocap_status debug_check_batch(const mocap_kv_store* kv, const int32_t* block_tables, int32_t table_stride,
+                               const int32_t* seq_lens, int32_t batch, int64_t max_len, int64_t window, int64_t sinks) {
+  const int64_t entries = (int64_t)batch * table_stride;
+  std::unique_ptr<int32_t[]> host(new (std::nothrow) int32_t[entries + batch]);
+  if (!host) return MOCAP_ERR_UNSUPPORTED;
+  if (hipMemcpy(host.get(), block_tables, entries * sizeof(int32_t), hipMemcpyDeviceToHost) != hipSuccess ||
+      hipMemcpy(host.get() + entries, seq_lens, batch * sizeof(int32_t), hipMemcpyDeviceToHost) != hipSuccess)
+    return MOCAP_ERR_HIP;
+  for (int32_t b = 0; b < batch; ++b) {
+    const int64_t n = std::min<int64_t>(host[entries + b], max_len);
+    const int64_t low = window > 0 ? std::max<int64_t>(0, n - window) : 0;
+    for (int64_t lb = 0; lb * kv->block_size < n; ++lb) {
+      if ((lb + 1) * kv->block_size <= low && lb * kv->block_size >= sinks) continue;
+      const int32_t block = host[b * (int64_t)table_stride + lb];
+      if (block < 0 || block >= kv->num_blocks) return MOCAP_ERR_INVALID_ARG;
+    }
+  }
+  return MOCAP_OK;
+}
+#define MOCAP_DEBUG_CHECK_BATCH(...)                             \
+  do {                                                           \
+    const mocap_status debug_st_ = debug_check_batch(__VA_ARGS__); \
+    if (debug_st_ != MOCAP_OK) return debug_st_;                 \
+  } while (0)
+#else
+#define MOCAP_DEBUG_CHECK_BATCH(...) \
+  do {                               \
+  } while (0)
+#endif
+
+mocap_status plan_decode(int32_t batch, int64_t max_len, int32_t h_q, int32_t h_kv, int64_t window, int64_t sinks,
+                         mocap::DecodeAttnLaunch* p) {
+  p->h_q = h_q;
+  p->h_kv = h_kv;
+  p->group = h_q / h_kv;
+  p->row_blocks = (int32_t)ceil_div(p->group, p->group <= 16 ? 16 : kDecodeHeads);
+  if ((int64_t)batch * h_q > 2 * kMaxGroups) return MOCAP_ERR_UNSUPPORTED;
+  return plan_batch(batch, max_len, window, sinks, (int64_t)h_kv * p->row_blocks, kDecodeMinTiles, &p->seqs, &p->may_split);
+}
+
+size_t decode_workspace(const mocap::DecodeAttnLaunch& p, int32_t head_dim) {
+  if (!p.may_split) return 0;
+  const size_t rows = (size_t)p.seqs.items * p.h_q;
+  return round_up(rows * head_dim * sizeof(float), 256) + round_up(rows * sizeof(float), 256);
+}
+
+// ---- A chunk in a window ----
+
+// Time model for the number of ranges: a workgroup of 256 rows costs a tile time
+// per 64-key tile, two wavefronts on each SIMD, plus fixed work, one workgroup
+// per compute unit at a time; a split adds the merge's launch and traffic.
+constexpr double kWindowTileUs128 = 1.4, kWindowTileUs64 = 0.9;
+constexpr double kWindowGroupUs = 4.0, kWindowMergeUs = 5.0, kWindowMergeBytesPerUs = 4.0e6;
+constexpr int64_t kWindowMaxRanges = 64;
+
+mocap_status plan_window(int64_t prefix_len, int32_t chunk_len, int32_t h_q, int32_t h_kv, int32_t head_dim,
+                         int64_t window, int64_t sinks, int32_t num_splits, mocap::WindowLaunch* p) {
+  const int64_t group = h_q / h_kv, rows = chunk_len * group;
+  if (rows > ((int64_t)1 << 31) - 2 * mocap::kWindowRows) return MOCAP_ERR_UNSUPPORTED;
+  p->prefix_len = (int32_t)prefix_len;
+  p->chunk_len = chunk_len;
+  p->h_q = h_q;
+  p->h_kv = h_kv;
+  p->group = (int32_t)group;
+  block_divider((uint32_t)group, &p->group_magic, &p->group_shift);
+  p->row_blocks = (int32_t)ceil_div(rows, mocap::kWindowRows);
+  p->window = (int32_t)std::min<int64_t>(window, kMaxPositions);
+  p->sinks = (int32_t)std::min<int64_t>(sinks, kMaxPositions);
+  const int64_t wgs = (int64_t)p->row_blocks * h_kv;
+  // Tiles of the workgroup with the most.
+  const int64_t span = std::min<int64_t>(chunk_len, ceil_div(mocap::kWindowRows, group) + 1) + p->window;
+  const int64_t tiles = std::min(ceil_div(prefix_len + chunk_len, kTileKeys),
+                                 ceil_div(span, kTileKeys) + 1 + ceil_div(p->sinks, kTileKeys));
+  int64_t best = 1;
+  if (num_splits > 1) {
+    best = std::min<int64_t>(num_splits, tiles);
+  } else if (num_splits == 0) {
+    int cus = 0;
+    const mocap_status st = device_cu_count(&cus);
+    if (st != MOCAP_OK) return st;
+    const double tile_us = head_dim == 128 ? kWindowTileUs128 : kWindowTileUs64;
+    double best_us = INFINITY;
+    for (int64_t n = 1; n <= std::min(kWindowMaxRanges, tiles); ++n) {
+      double us = (double)ceil_div(wgs * n, cus) * (ceil_div(tiles, n) * tile_us + kWindowGroupUs);
+      if (n > 1) us += kWindowMergeUs + 2.0 * n * chunk_len * h_q * (head_dim + 1) * 4.0 / kWindowMergeBytesPerUs;
+      if (us < best_us * 0.98) {
+        best_us = us;
+        best = n;
+      }
+    }
+  }
+  if (wgs * best > kMaxGroups) return MOCAP_ERR_UNSUPPORTED;
+  p->n_ranges = (int32_t)best;
+  p->total_wgs = (int32_t)(wgs * best);
+  return MOCAP_OK;
+}
+
+size_t window_workspace(const mocap::WindowLaunch& p, int32_t head_dim) {
+  if (p.n_ranges <= 1) return 0;
+  const size_t rows = (size_t)p.n_ranges * p.h_q * p.chunk_len;
+  return round_up(rows * head_dim * sizeof(float), 256) + round_up(rows * sizeof(float), 256);
+}
+
+// ---- Key weights ----
+
+mocap_status plan_weights(int64_t prefix_len, int32_t chunk_len, int32_t h_q, int32_t h_kv, mocap::KeyWeightsLaunch* p) {
+  const int64_t group = h_q / h_kv, rows = chunk_len * group, n = prefix_len + chunk_len;
+  if (rows > ((int64_t)1 << 31) - 1024) return MOCAP_ERR_UNSUPPORTED;
+  int cus = 0;
+  const mocap_status st = device_cu_count(&cus);
+  if (st != MOCAP_OK) return st;
+  p->prefix_len = (int32_t)prefix_len;
+  p->chunk_len = chunk_len;
+  p->h_q = h_q;
+  p->h_kv = h_kv;
+  p->group = (int32_t)group;
+  block_divider((uint32_t)group, &p->group_magic, &p->group_shift);
+  // As many wavefronts along the keys as leave a workgroup for every compute unit.
+  p->key_waves = 8;
+  while (p->key_waves > 1 && ceil_div(n, p->key_waves * mocap::kWeightKeys) * h_kv < cus) p->key_waves /= 2;
+  p->key_blocks = (int32_t)ceil_div(n, p->key_waves * mocap::kWeightKeys);
+  p->row_parts = 1;
+  if ((int64_t)p->key_blocks * h_kv > kMaxGroups) return MOCAP_ERR_UNSUPPORTED;
+  return MOCAP_OK;
+}
+
+size_t weights_workspace(const mocap::KeyWeightsLaunch& p) {
+  if (p.row_parts <= 1) return 0;
+  return (size_t)p.row_parts * p.h_kv * ((size_t)p.prefix_len + p.chunk_len) * sizeof(float);
+}
+
+mocap_status check_chunk(int64_t prefix_len, int32_t chunk_len) {
+  if (prefix_len < 0 || chunk_len < 0 || prefix_len + (int64_t)chunk_len > kMaxPositions) return MOCAP_ERR_INVALID_ARG;
+  return MOCAP_OK;
+}
+
+// Checks shared by the calls on one chunk of one sequence.
+mocap_status check_chunk_args(const mocap_kv_store* kv, const int32_t* block_table, int32_t n_table, const void* q,
+                              int64_t prefix_len, int32_t chunk_len, int32_t h_q, int32_t h_kv, int32_t head_dim,
+                              float scale) {
+  mocap_status st = check_store(kv);
+  if (st != MOCAP_OK) return st;
+  if (h_q <= 0 || h_kv <= 0 || h_q % h_kv != 0 || h_kv != kv->h_kv || head_dim != kv->head_dim || !valid_scale(scale))
+    return MOCAP_ERR_INVALID_ARG;
+  st = check_positions(kv, n_table, prefix_len, chunk_len);
+  if (st != MOCAP_OK) return st;
+  if (chunk_len == 0) return MOCAP_OK;
+  if (!kv->k_pool || !kv->v_pool || !block_table || !q) return MOCAP_ERR_INVALID_ARG;
+  if (!aligned16(kv->k_pool) || !aligned16(kv->v_pool) || !aligned4(block_table) || !aligned16(q))
+    return MOCAP_ERR_INVALID_ARG;
+  return MOCAP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+mocap_status mocap_decode_append(const mocap_kv_store* kv, const int32_t* block_tables, int32_t table_stride,
+                                 const int32_t* seq_lens, int32_t batch, const void* k, const void* v, void* stream) {
+  const mocap_status st = check_batch(kv, block_tables, table_stride, seq_lens, batch, 0);
+  if (st != MOCAP_OK || batch == 0) return st;
+  if (!k || !v || !aligned16(k) || !aligned16(v)) return MOCAP_ERR_INVALID_ARG;
+  if (batch > kMaxGroups) return MOCAP_ERR_UNSUPPORTED;
+  MOCAP_DEBUG_CHECK_BATCH(kv, block_tables, table_stride, seq_lens, batch, (int64_t)table_stride * kv->block_size, 1, 0);
+  mocap::DecodeAppendLaunch p;
+  p.k = static_cast<const uint16_t*>(k);
+  p.v = static_cast<const uint16_t*>(v);
+  p.k_pool = static_cast<uint16_t*>(kv->k_pool);
+  p.v_pool = static_cast<uint16_t*>(kv->v_pool);
+  p.tables = block_tables;
+  p.seq_lens = seq_lens;
+  p.table_stride = table_stride;
+  p.batch = batch;
+  p.h_kv = kv->h_kv;
+  p.block_size = kv->block_size;
+  return mocap::launch_decode_append(p, kv->head_dim, static_cast<hipStream_t>(stream)) == hipSuccess ? MOCAP_OK
+                                                                                                      : MOCAP_ERR_HIP;
+}
+
+mocap_status mocap_decode_attn_workspace_size(int32_t batch, int64_t max_len, int32_t h_q, int32_t h_kv,
+                                              int32_t head_dim, int64_t window, int64_t sinks, size_t* bytes_out) {
+  if (bytes_out == nullptr || batch < 0 || max_len < 0 || max_len > kMaxPositions || window < 0 || sinks < 0)
+    return MOCAP_ERR_INVALID_ARG;
+  mocap_status st = check_heads(h_q, h_kv, head_dim);
+  if (st != MOCAP_OK) return st;
+  *bytes_out = 0;
+  if (batch == 0) return MOCAP_OK;
+  mocap::DecodeAttnLaunch p;
+  st = plan_decode(batch, max_len, h_q, h_kv, window, sinks, &p);
+  if (st == MOCAP_OK) *bytes_out = decode_workspace(p, head_dim);
+  return st;
+}
+
+mocap_status mocap_decode_attn(const mocap_kv_store* kv, const int32_t* block_tables, int32_t table_stride,
+                               const int32_t* seq_lens, int32_t batch, int64_t max_len, const void* q, int32_t h_q,
+                               int32_t h_kv, int32_t head_dim, float scale, int64_t window, int64_t sinks, void* o,
+                               float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  mocap_status st = check_batch(kv, block_tables, table_stride, seq_lens, batch, max_len);
+  if (st != MOCAP_OK) return st;
+  if (h_q <= 0 || h_kv <= 0 || h_q % h_kv != 0 || h_kv != kv->h_kv || head_dim != kv->head_dim || !valid_scale(scale) ||
+      window < 0 || sinks < 0)
+    return MOCAP_ERR_INVALID_ARG;
+  if (batch == 0) return MOCAP_OK;
+  if (!q || !o || !lse || !aligned16(q) || !aligned16(o) || !aligned4(lse)) return MOCAP_ERR_INVALID_ARG;
+  mocap::DecodeAttnLaunch p;
+  st = plan_decode(batch, max_len, h_q, h_kv, window, sinks, &p);
+  if (st != MOCAP_OK) return st;
+  if (p.may_split && (!workspace || !aligned16(workspace) || workspace_bytes < decode_workspace(p, head_dim)))
+    return MOCAP_ERR_WORKSPACE;
+  MOCAP_DEBUG_CHECK_BATCH(kv, block_tables, table_stride, seq_lens, batch, max_len, window, sinks);
+  set_tables(kv, block_tables, table_stride, seq_lens, &p.seqs);
+  p.q = static_cast<const uint16_t*>(q);
+  p.k_pool = static_cast<const uint16_t*>(kv->k_pool);
+  p.v_pool = static_cast<const uint16_t*>(kv->v_pool);
+  p.o = static_cast<uint16_t*>(o);
+  p.lse = lse;
+  p.ws_o = nullptr;
+  p.ws_lse = nullptr;
+  if (p.may_split) {
+    p.ws_o = static_cast<float*>(workspace);
+    p.ws_lse = reinterpret_cast<float*>(static_cast<char*>(workspace) +
+                                        round_up((size_t)p.seqs.items * h_q * head_dim * sizeof(float), 256));
+  }
+  p.scale_log2 = (float)((double)scale * 1.4426950408889634);
+  return mocap::launch_decode_attn(p, head_dim, static_cast<hipStream_t>(stream)) == hipSuccess ? MOCAP_OK
+                                                                                                : MOCAP_ERR_HIP;
+}
+
+mocap_status mocap_window_attn_workspace_size(int64_t prefix_len, int32_t chunk_len, int32_t h_q, int32_t h_kv,
+                                              int32_t head_dim, int64_t window, int64_t sinks, int32_t num_splits,
+                                              int32_t* splits_out, size_t* bytes_out) {
+  if (bytes_out == nullptr || window < 1 || sinks < 0 || num_splits < 0) return MOCAP_ERR_INVALID_ARG;
+  mocap_status st = check_chunk(prefix_len, chunk_len);
+  if (st == MOCAP_OK) st = check_heads(h_q, h_kv, head_dim);
+  if (st != MOCAP_OK) return st;
+  mocap::WindowLaunch p;
+  p.n_ranges = 1;
+  if (chunk_len > 0) st = plan_window(prefix_len, chunk_len, h_q, h_kv, head_dim, window, sinks, num_splits, &p);
+  if (st != MOCAP_OK) return st;
+  if (splits_out) *splits_out = p.n_ranges;
+  *bytes_out = chunk_len > 0 ? window_workspace(p, head_dim) : 0;
+  return MOCAP_OK;
+}
+
+mocap_status mocap_window_attn(const mocap_kv_store* kv, const int32_t* block_table, int32_t n_table, const void* q,
+                               int64_t prefix_len, int32_t chunk_len, int32_t h_q, int32_t h_kv, int32_t head_dim,
+                               float scale, int64_t window, int64_t sinks, void* o, float* lse, void* workspace,
+                               size_t workspace_bytes, int32_t num_splits, void* stream) {
+  mocap_status st = check_chunk_args(kv, block_table, n_table, q, prefix_len, chunk_len, h_q, h_kv, head_dim, scale);
+  if (st != MOCAP_OK) return st;
+  if (window < 1 || sinks < 0 || num_splits < 0) return MOCAP_ERR_INVALID_ARG;
+  if (chunk_len == 0) return MOCAP_OK;
+  if (!o || !lse || !aligned16(o) || !aligned4(lse)) return MOCAP_ERR_INVALID_ARG;
+  mocap::WindowLaunch p;
+  st = plan_window(prefix_len, chunk_len, h_q, h_kv, head_dim, window, sinks, num_splits, &p);
+  if (st != MOCAP_OK) return st;
+  if (p.n_ranges > 1 && (!workspace || !aligned16(workspace) || workspace_bytes < window_workspace(p, head_dim)))
+    return MOCAP_ERR_WORKSPACE;
+  MOCAP_DEBUG_CHECK(block_table, 0, std::min<int64_t>(sinks, prefix_len + chunk_len), kv);
+  MOCAP_DEBUG_CHECK(block_table, std::max<int64_t>(0, prefix_len - window + 1), prefix_len + chunk_len, kv);
+  p.q = static_cast<const uint16_t*>(q);
+  p.k_pool = static_cast<const uint16_t*>(kv->k_pool);
+  p.v_pool = static_cast<const uint16_t*>(kv->v_pool);
+  p.table = block_table;
+  p.o = static_cast<uint16_t*>(o);
+  p.lse = lse;
+  p.block_size = kv->block_size;
+  block_divider((uint32_t)kv->block_size, &p.block_magic, &p.block_shift);
+  p.scale_log2 = (float)((double)scale * 1.4426950408889634);
+  p.ws_o = nullptr;
+  p.ws_lse = nullptr;
+  if (p.n_ranges > 1) {
+    p.ws_o = static_cast<float*>(workspace);
+    p.ws_lse = reinterpret_cast<float*>(
+        static_cast<char*>(workspace) + round_up((size_t)p.n_ranges * h_q * chunk_len * head_dim * sizeof(float), 256));
+  }
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (mocap::launch_window_attn(p, head_dim, s) != hipSuccess) return MOCAP_ERR_HIP;
+  if (p.n_ranges > 1) {
+    const mocap::MergeLaunch m{p.ws_o, p.ws_lse, p.o, lse, chunk_len, h_q, p.n_ranges};
+    if (mocap::launch_lse_merge(m, head_dim, s) != hipSuccess) return MOCAP_ERR_HIP;
+  }
+  return MOCAP_OK;
+}
+
+mocap_status mocap_key_weights_workspace_size(int64_t prefix_len, int32_t chunk_len, int32_t h_q, int32_t h_kv,
+                                              int32_t head_dim, size_t* bytes_out) {
+  if (bytes_out == nullptr) return MOCAP_ERR_INVALID_ARG;
+  mocap_status st = check_chunk(prefix_len, chunk_len);
+  if (st == MOCAP_OK) st = check_heads(h_q, h_kv, head_dim);
+  if (st != MOCAP_OK) return st;
+  *bytes_out = 0;
+  if (chunk_len == 0) return MOCAP_OK;
+  mocap::KeyWeightsLaunch p;
+  st = plan_weights(prefix_len, chunk_len, h_q, h_kv, &p);
+  if (st == MOCAP_OK) *bytes_out = weights_workspace(p);
+  return st;
+}
+
+mocap_status mocap_key_weights(const mocap_kv_store* kv, const int32_t* block_table, int32_t n_table, const void* q,
+                               int64_t prefix_len, int32_t chunk_len, int32_t h_q, int32_t h_kv, int32_t head_dim,
+                               float scale, const float* lse, const float* prev, float* weights, int64_t weight_stride,
+                               void* workspace, size_t workspace_bytes, void* stream) {
+  mocap_status st = check_chunk_args(kv, block_table, n_table, q, prefix_len, chunk_len, h_q, h_kv, head_dim, scale);
+  if (st != MOCAP_OK) return st;
+  if (weight_stride < prefix_len + chunk_len) return MOCAP_ERR_INVALID_ARG;
+  if (chunk_len == 0) return MOCAP_OK;
+  if (!lse || !weights || !aligned4(lse) || !aligned4(weights) || !aligned4(prev)) return MOCAP_ERR_INVALID_ARG;
+  mocap::KeyWeightsLaunch p;
+  st = plan_weights(prefix_len, chunk_len, h_q, h_kv, &p);
+  if (st != MOCAP_OK) return st;
+  if (p.row_parts > 1 && (!workspace || !aligned16(workspace) || workspace_bytes < weights_workspace(p)))
+    return MOCAP_ERR_WORKSPACE;
+  MOCAP_DEBUG_CHECK(block_table, 0, prefix_len + chunk_len, kv);
+  p.q = static_cast<const uint16_t*>(q);
+  p.k_pool = static_cast<const uint16_t*>(kv->k_pool);
+  p.table = block_table;
+  p.lse = lse;
+  p.prev = prev;
+  p.weights = weights;
+  p.ws = static_cast<float*>(workspace);
+  p.weight_stride = weight_stride;
+  p.block_size = kv->block_size;
+  block_divider((uint32_t)kv->block_size, &p.block_magic, &p.block_shift);
+  p.scale_log2 = (float)((double)scale * 1.4426950408889634);
+  return mocap::launch_key_weights(p, head_dim, static_cast<hipStream_t>(stream)) == hipSuccess ? MOCAP_OK
+                                                                                                : MOCAP_ERR_HIP;
+}
+
+mocap_status mocap_decode_key_weights(const mocap_kv_store* kv, const int32_t* block_tables, int32_t table_stride,
+                                      const int32_t* seq_lens, int32_t batch, int64_t max_len, const void* q,
+                                      int32_t h_q, int32_t h_kv, int32_t head_dim, float scale, const float* lse,
+                                      const float* prev, float* weights, int64_t weight_stride, void* stream) {
+  mocap_status st = check_batch(kv, block_tables, table_stride, seq_lens, batch, max_len);
+  if (st != MOCAP_OK) return st;
+  if (h_q <= 0 || h_kv <= 0 || h_q % h_kv != 0 || h_kv != kv->h_kv || head_dim != kv->head_dim || !valid_scale(scale) ||
+      weight_stride < max_len)
+    return MOCAP_ERR_INVALID_ARG;
+  if (batch == 0) return MOCAP_OK;
+  if (!q || !lse || !weights || !aligned16(q) || !aligned4(lse) || !aligned4(weights) || !aligned4(prev))
+    return MOCAP_ERR_INVALID_ARG;
+  mocap::DecodeKeyWeightsLaunch p;
+  bool may_split;
+  st = plan_batch(batch, max_len, 0, 0, h_kv, kDecodeMinTiles, &p.seqs, &may_split);
+  if (st != MOCAP_OK) return st;
+  MOCAP_DEBUG_CHECK_BATCH(kv, block_tables, table_stride, seq_lens, batch, max_len, 0, 0);
+  set_tables(kv, block_tables, table_stride, seq_lens, &p.seqs);
+  p.q = static_cast<const uint16_t*>(q);
+  p.k_pool = static_cast<const uint16_t*>(kv->k_pool);
+  p.lse = lse;
+  p.prev = prev;
+  p.weights = weights;
+  p.weight_stride = weight_stride;
+  p.h_q = h_q;
+  p.h_kv = h_kv;
+  p.group = h_q / h_kv;
+  p.scale_log2 = (float)((double)scale * 1.4426950408889634);
+  return mocap::launch_decode_key_weights(p, head_dim, static_cast<hipStream_t>(stream)) == hipSuccess ? MOCAP_OK
+                                                                                                       : MOCAP_ERR_HIP;
+}
+
+mocap_status mocap_kv_evict_workspace_size(int64_t n, int32_t h_kv, int32_t keep, size_t* bytes_out) {
+  if (bytes_out == nullptr || n < 0 || n > kMaxPositions || h_kv <= 0 || keep < 0 || keep > n || (n > 0 && keep == 0))
+    return MOCAP_ERR_INVALID_ARG;
+  if (h_kv > 65535) return MOCAP_ERR_UNSUPPORTED;
+  *bytes_out = 0;
+  return MOCAP_OK;
+}
+
+mocap_status mocap_kv_evict(const mocap_kv_store* src, const int32_t* src_table, int32_t n_src_table,
+                            const mocap_kv_store* dst, const int32_t* dst_table, int32_t n_dst_table, int64_t n,
+                            int32_t keep, int32_t sinks, int32_t recent, const float* weights, int64_t weight_stride,
+                            int32_t* kept, float* kept_weights, void* workspace, size_t workspace_bytes, void* stream) {
+  mocap_status st = check_store(src);
+  if (st == MOCAP_OK) st = check_store(dst);
+  if (st != MOCAP_OK) return st;
+  if (src->h_kv != dst->h_kv || src->head_dim != dst->head_dim || n < 0 || n > kMaxPositions || keep < 0 || keep > n ||
+      (n > 0 && keep == 0) || sinks < 0 || recent < 0 || (int64_t)sinks + recent > keep || weight_stride < n)
+    return MOCAP_ERR_INVALID_ARG;
+  st = check_positions(src, n_src_table, n, 0);
+  if (st == MOCAP_OK) st = check_positions(dst, n_dst_table, 0, keep);
+  if (st != MOCAP_OK) return st;
+  if (n == 0) return MOCAP_OK;
+  if (!src->k_pool || !src->v_pool || !dst->k_pool || !dst->v_pool || !src_table || !dst_table || !weights || !kept)
+    return MOCAP_ERR_INVALID_ARG;
+  if (!aligned16(src->k_pool) || !aligned16(src->v_pool) || !aligned16(dst->k_pool) || !aligned16(dst->v_pool) ||
+      !aligned4(src_table) || !aligned4(dst_table) || !aligned4(weights) || !aligned4(kept) ||
+      !aligned4(kept_weights))
+    return MOCAP_ERR_INVALID_ARG;
+  if ((src->k_pool == dst->k_pool || src->v_pool == dst->v_pool) && src_table == dst_table) return MOCAP_ERR_INVALID_ARG;
+  size_t need = 0;
+  st = mocap_kv_evict_workspace_size(n, src->h_kv, keep, &need);
+  if (st != MOCAP_OK) return st;
+  if (need > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return MOCAP_ERR_WORKSPACE;
+  MOCAP_DEBUG_CHECK(src_table, 0, n, src);
+  MOCAP_DEBUG_CHECK(dst_table, 0, keep, dst);
+  mocap::EvictLaunch p;
+  p.k_src = static_cast<const uint16_t*>(src->k_pool);
+  p.v_src = static_cast<const uint16_t*>(src->v_pool);
+  p.k_dst = static_cast<uint16_t*>(dst->k_pool);
+  p.v_dst = static_cast<uint16_t*>(dst->v_pool);
+  p.src_table = src_table;
+  p.dst_table = dst_table;
+  p.weights = weights;
+  p.kept = kept;
+  p.kept_weights = kept_weights;
+  p.weight_stride = weight_stride;
+  p.n = (int32_t)n;
+  p.keep = keep;
+  p.sinks = sinks;
+  p.recent = recent;
+  p.h_kv = src->h_kv;
+  p.src_block_size = src->block_size;
+  p.dst_block_size = dst->block_size;
+  return mocap::launch_kv_evict(p, src->head_dim, static_cast<hipStream_t>(stream)) == hipSuccess ? MOCAP_OK
+                                                                                                  : MOCAP_ERR_HIP;
+}
+
+}  // extern "C"
