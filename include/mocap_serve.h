@@ -184,7 +184,7 @@ mocap_status mocap_decode_key_weights(const mocap_kv_store* kv, const int32_t* b
 /*
  * mocap_kv_evict_workspace_size -- workspace bytes of mocap_kv_evict.
  * Errors: INVALID_ARG for a null bytes_out or malformed sizes; UNSUPPORTED for
- * more than 65535 heads.
+ * more than 65535 heads or 2^30 positions.
  */
 mocap_status mocap_kv_evict_workspace_size(int64_t n, int32_t h_kv, int32_t keep, size_t* bytes_out);
 
@@ -216,8 +216,8 @@ mocap_status mocap_kv_evict_workspace_size(int64_t n, int32_t h_kv, int32_t keep
  * Slots of dst at position keep and beyond are left as they were.
  * Errors: INVALID_ARG for null/misaligned pointers, malformed sizes, stores that
  * differ in h_kv or head_dim, tables that are too short, or dst = src (see
- * above); UNSUPPORTED for a head_dim or block size the store does not have;
- * WORKSPACE when the workspace is missing or too small; HIP if a launch fails.
+ * above); UNSUPPORTED as mocap_kv_evict_workspace_size, or for a head_dim or
+ * block size the store does not have; WORKSPACE when the workspace is missing or too small; HIP if a launch fails.
  */
 mocap_status mocap_kv_evict(const mocap_kv_store* src, const int32_t* src_table, int32_t n_src_table,
                             const mocap_kv_store* dst, const int32_t* dst_table, int32_t n_dst_table, int64_t n,

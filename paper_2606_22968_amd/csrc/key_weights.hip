@@ -2,18 +2,24 @@
 //   w[h][j] = sum over rows i that see key j and heads g of group h of
 //             exp(scale <q_ig, k_jh> - lse_gi)
 // Many rows are bound by the matrix unit (2 D FLOP a pair) and the exponentials
-// beside it (one a pair, as many issue cycles as the products at head_dim 128),
-// few rows by HBM (the keys, once).
+// beside it (one a pair, with an FMA and an add as many issue cycles as the
+// products at head_dim 128), few rows by HBM (the keys, once).
 //
-//   * The keys stay, the rows stream: a wavefront holds 64 keys as B operands in
-//     registers and walks the rows, S = Q K^T with v_mfma_f32_32x32x16_bf16.  Lane
-//     l then holds key l % 32 of each product and 16 of its 32 rows, so the sum
-//     over the rows stays within the lane: one exponential, one FMA and one add a
-//     score, and no exchange between lanes before the end.
+// Many rows: the keys stay, the rows stream.
+//   * A wavefront holds 64 keys as B operands in registers and walks the rows,
+//     S = Q K^T with v_mfma_f32_32x32x16_bf16.  Lane l then holds key l % 32 of
+//     each product and 16 of its 32 rows, so the sum over the rows stays within
+//     the lane, with no exchange between lanes before the end.
 //   * Rows ((token, query head) pairs of the group, token-major) come in tiles of
-//     32 through LDS, Q copied straight to it, a row's LSE in base 2 beside it.
-//     key_waves wavefronts along the keys share a tile; 8 / key_waves row tiles
-//     are worked on at a time, whose sums meet in LDS at the end.
+//     32, four tiles a stage, through a 3-stage LDS ring that a workgroup's eight
+//     wavefronts (512 keys) share, two stages ahead; a row's LSE in base 2 lies
+//     beside it.
+//   * A tile's products have the exponentials and sums of the tile before woven
+//     in between, two scores per MFMA at head_dim 128, through all of a stage and
+//     on into the next.  A wavefront's first tiles, whose rows do not all see its
+//     keys, and those of an incomplete last stage are done one by one.
+//   * Where keys are few, the rows are cut into parts whose sums a second launch
+//     adds in order.
 //   * Sums are fp32: 16 rows first, then tile by tile.
 #include "serve_device.h"
 
@@ -21,6 +27,8 @@ namespace mocap {
 namespace {
 
 constexpr int kRowTile = 32;
+constexpr int kStageTiles = 4;
+constexpr int kStageRows = kRowTile * kStageTiles;
 constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ void lds_barrier() {
@@ -37,47 +45,46 @@ __device__ __forceinline__ int q_swizzle(int r) {
   return D == 128 ? (r & 15) : ((r >> 1) & 7);
 }
 
-// KW: wavefronts along the keys.
-template <int D, int KW>
+template <int D>
 __global__ __launch_bounds__(64 * kWeightWaves, 2) void key_weights_kernel(const KeyWeightsLaunch p) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int KS = D / 16;
-  constexpr int RW = kWeightWaves / KW;           // row tiles at a time
   constexpr int ROW_CHUNKS = D / 8;
-  constexpr int TILE_ELEMS = kRowTile * D;
-  constexpr int STAGE_ROWS = RW * kRowTile;
-  constexpr int COPIES = RW * TILE_ELEMS / 8 / (64 * kWeightWaves);  // 16-byte copies of a thread per stage (0: half of them)
-  constexpr int COPY_THREADS = COPIES > 0 ? 64 * kWeightWaves : RW * TILE_ELEMS / 8;
-  constexpr int COPIES_EACH = COPIES > 0 ? COPIES : 1;
-  constexpr int STAGES = 2;
-  __shared__ __attribute__((aligned(1024))) uint16_t ring[STAGES][RW * TILE_ELEMS];
-  __shared__ __attribute__((aligned(16))) float lse2[STAGES][STAGE_ROWS];
-  __shared__ float sums[RW > 1 ? RW : 1][KW * kWeightKeys];
+  constexpr int STAGE_ELEMS = kStageRows * D;
+  constexpr int COPIES = STAGE_ELEMS / 8 / (64 * kWeightWaves);  // 16-byte copies of a thread per stage
+  constexpr int STAGES = 3;
+  // One array for the ring and the LSE beside it: with two, the compiler tells
+  // them apart, takes every read of the ring to depend on the copies in flight,
+  // and waits for those (588 -> 566 us for 2048 tokens of 32/8/128
+  // heads behind 30720).
+  __shared__ __attribute__((aligned(1024))) uint16_t lds[STAGES * (STAGE_ELEMS + 2 * kStageRows)];
+  float* const lse2 = reinterpret_cast<float*>(lds + STAGES * STAGE_ELEMS);
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5, l32 = lane & 31;
-  const int kw = wave % KW, rw = wave / KW;
   const int P = p.prefix_len, n = P + p.chunk_len;
 
   // Logical order: KV head, row part, key block.
-  const int total = p.key_blocks * p.row_parts * p.h_kv;
-  const int logical = xcd_contiguous(blockIdx.x, total);
+  const int logical = xcd_contiguous(blockIdx.x, p.key_blocks * p.row_parts * p.h_kv);
   const int kv_head = logical / (p.key_blocks * p.row_parts);
   const int in_kv = logical - kv_head * p.key_blocks * p.row_parts;
   const int part = in_kv / p.key_blocks;
-  const int block0 = (in_kv - part * p.key_blocks) * (KW * kWeightKeys);
-  const int key0 = block0 + kw * kWeightKeys;  // this wavefront's keys
+  const int block0 = (in_kv - part * p.key_blocks) * (kWeightWaves * kWeightKeys);
+  const int key0 = block0 + wave * kWeightKeys;  // this wavefront's keys
 
-  // Rows [begin, end) of this part, in tiles; rows before begin see no key of
-  // the workgroup (row r sees key j if r >= (j - P) G).
+  // Row r sees key j if r >= (j - P) G.  The row tiles [t0, t1) of this part, of
+  // those that see some key of the workgroup; this wavefront starts at tile `from`
+  // and masks those before `full`.
   const int rows = p.chunk_len * p.group;
-  const int row_tiles = (rows + kRowTile - 1) / kRowTile;
-  const int first_tile = max(0, block0 - P) * p.group / kRowTile;
-  const int span = row_tiles - first_tile;
+  auto first_row = [&](int key) { return (int)min((int64_t)max(key - P, 0) * p.group, (int64_t)rows); };
+  const int first_tile = first_row(block0) / kRowTile;
+  const int span = (rows + kRowTile - 1) / kRowTile - first_tile;
   const int t0 = first_tile + (int)((int64_t)span * part / p.row_parts);
   const int t1 = first_tile + (int)((int64_t)span * (part + 1) / p.row_parts);
+  const int from = first_row(key0) / kRowTile;
+  const int full = (first_row(key0 + kWeightKeys - 1) + kRowTile - 1) / kRowTile;
 
   // K as the B operand: lane l holds key l % 32 of a 32-key half, dims 16 ks + 8 (l / 32) .. + 7.
   // Keys past the last take it; nothing of theirs is stored.
@@ -92,121 +99,222 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void key_weights_kernel(const
     for (int ks = 0; ks < KS; ++ks) kf[b][ks] = *reinterpret_cast<const bf16x8*>(k + ks * 16);
   }
 
-  // Stage s of the ring holds row tiles t0 + s RW ..; copy j of a thread moves
-  // 16-byte chunk j * 512 + tid, from a column XORed with the row.  Rows past the
-  // last take it, with an LSE of +infinity (a weight of 0).
+  // Stage s of the ring holds row tiles t0 + 4 s .. + 3; copy j of a thread moves
+  // 16-byte chunk j * 512 + tid, from a column XORed with the row.
+  // Rows past the last take it, with an LSE of +infinity (a weight of 0).
+  // Offsets of this thread's chunks of rows that start at base_row, from the first
+  // one's token: all of Q may not fit in 32 bits.
+  auto offsets = [&](int base_row, int base_token, int* at) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < COPIES; ++j) {
+      const int chunk = j * 64 * kWeightWaves + tid;
+      const int lr = chunk / ROW_CHUNKS, c = (chunk % ROW_CHUNKS) ^ q_swizzle<D>(lr);
+      const int r = min(base_row + lr, rows - 1);
+      const int token = (int)div_by((uint32_t)r, p.group_magic, p.group_shift);
+      at[j] = (((token - base_token) * p.h_q + (r - token * p.group)) * D + c * 8) * 2;
+    }
+  };
+  // A group that divides a stage's rows: every whole stage has the same ones.
+  const bool same = kStageRows % p.group == 0 && rows >= kStageRows;
+  int usual[COPIES];
+  if (same) offsets(0, 0, usual);
   auto issue = [&](int s) __attribute__((always_inline)) {
-    // Offsets from the stage's first token: a stage spans few tokens, all of Q
-    // may not fit in 32 bits.
-    const int base_row = (t0 + s * RW) * kRowTile;
+    const int base_row = (t0 + s * kStageTiles) * kRowTile;
     const int base_token = (int)div_by((uint32_t)min(base_row, rows - 1), p.group_magic, p.group_shift);
     const uint16_t* base = p.q + ((int64_t)base_token * p.h_q + kv_head * p.group) * D;
     const __amdgpu_buffer_rsrc_t q = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, -1, kBufferWord3);
-    if (tid < COPY_THREADS) {
+    int at[COPIES];
+    if (same && base_row + kStageRows <= rows && base_token * p.group == base_row) {
 #pragma unroll
-      for (int j = 0; j < COPIES_EACH; ++j) {
-        const int chunk = j * COPY_THREADS + tid;
-        const int lr = chunk / ROW_CHUNKS, c = (chunk % ROW_CHUNKS) ^ q_swizzle<D>(lr);
-        const int r = min(base_row + lr, rows - 1);
-        const int token = (int)div_by((uint32_t)r, p.group_magic, p.group_shift);
-        const int at = ((token - base_token) * p.h_q + (r - token * p.group)) * D + c * 8;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(q, (lds_ptr_t)(&ring[s % STAGES][(j * COPY_THREADS + wave * 64) * 8]),
-                                                 16, at * 2, 0, 0, 0);
-      }
+      for (int j = 0; j < COPIES; ++j) at[j] = usual[j];
+    } else {
+      offsets(base_row, base_token, at);
     }
+#pragma unroll
+    for (int j = 0; j < COPIES; ++j)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          q, (lds_ptr_t)(lds + s % STAGES * STAGE_ELEMS + (j * 64 * kWeightWaves + wave * 64) * 8), 16, at[j], 0, 0, 0);
   };
+  // The first two wavefronts bring the stage's LSE: requested with its copies, used
+  // (waited for) one stage later.
+  static_assert(kStageRows == 128, "a row for every lane of two wavefronts");
   auto load_lse = [&](int s) __attribute__((always_inline)) -> float {
-    if (tid >= STAGE_ROWS) return 0.f;
-    const int r = (t0 + s * RW) * kRowTile + tid;
-    const int q = min(r, rows - 1);
-    const int token = (int)div_by((uint32_t)q, p.group_magic, p.group_shift);
-    const float x = p.lse[(int64_t)(kv_head * p.group + (q - token * p.group)) * p.chunk_len + token];
-    return r < rows && x != -INFINITY ? x * kLog2e : INFINITY;
+    const int r = min((t0 + s * kStageTiles) * kRowTile + tid, rows - 1);
+    const int token = (int)div_by((uint32_t)r, p.group_magic, p.group_shift);
+    return p.lse[(int64_t)(kv_head * p.group + (r - token * p.group)) * p.chunk_len + token];
   };
   auto put_lse = [&](int s, float x) __attribute__((always_inline)) {
-    if (tid < STAGE_ROWS) lse2[s % STAGES][tid] = x;
+    const bool live = (t0 + s * kStageTiles) * kRowTile + tid < rows;
+    lse2[s % STAGES * kStageRows + tid] = live && x != -INFINITY ? x * kLog2e : INFINITY;
   };
 
   const float sl2 = p.scale_log2;
   float w[2] = {0.f, 0.f};
-  const int stages = (t1 - t0 + RW - 1) / RW;
+  f32x16 acc[2][2];  // scores of even and odd tiles, per 32-key half
+  // Fragment i of a stage: k-step i % KS of its tile i / KS.
+  auto qfrag = [&](int s, int i) __attribute__((always_inline)) {
+    return *reinterpret_cast<const bf16x8*>(lds + s % STAGES * STAGE_ELEMS + (i / KS * kRowTile + l32) * D +
+                                            (((i % KS * 2 + half) ^ q_swizzle<D>(l32)) << 3));
+  };
+  // Score j of a lane belongs to row 8 (j / 4) + 4 half + j % 4 of its tile.
+  auto lse_quad = [&](int s, int u, int quad) __attribute__((always_inline)) {
+    return *reinterpret_cast<const f32x4*>(lse2 + s % STAGES * kStageRows + u * kRowTile + quad * 8 + half * 4);
+  };
+  constexpr int NM = 2 * KS;      // MFMAs of a tile
+  constexpr int EACH = 32 / NM;   // scores woven in behind one
+  // All tiles of stage s, each with the weights of the tile before woven in; the
+  // first one's are those of the stage before, if `cont`.  The last tile's scores
+  // stay in acc[1].
+  //
+  // Behind an MFMA come the FMAs of the scores after next, the exponentials of
+  // the next ones and the sums of the last, so nothing there waits for the
+  // instruction before it.  Scores are taken in the order (quad, half, row): a
+  // quad's LSE serves eight, and the half whose products were issued last is not
+  // touched in the first turns.
+  auto stage = [&](int s, auto continued) __attribute__((always_inline)) {
+    constexpr bool cont = decltype(continued)::value;
+    constexpr int AHEAD = 3;
+    bf16x8 f[AHEAD + 1];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) f[i] = qfrag(s, i);
+    f32x4 l2[2];
+    if constexpr (cont) l2[0] = lse_quad(s - 1, kStageTiles - 1, 0);
+#pragma unroll
+    for (int u = 0; u < kStageTiles; ++u) {
+      f32x16* const a = acc[u % 2];
+      const f32x16* const before = acc[1 - u % 2];
+      float sum[2] = {0.f, 0.f}, x[2][EACH], v[2][EACH];  // arguments and exponentials of even and odd turns
+      auto fmas = [&](int k) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+          const int j = k * EACH + i, quad = j / 8, h = j / 4 % 2, e = j % 4;
+          x[k % 2][i] = fmaf(before[h][quad * 4 + e], sl2, -l2[quad % 2][e]);
+        }
+      };
+      auto exps = [&](int k) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) v[k % 2][i] = __builtin_amdgcn_exp2f(x[k % 2][i]);
+      };
+      auto sums = [&](int k) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < EACH; i += 2) sum[(k * EACH + i) / 4 % 2] += v[k % 2][i] + v[k % 2][i + 1];
+      };
+#pragma unroll
+      for (int k = 0; k < NM; ++k) {
+        const int i = u * KS + k / 2, b = k % 2;
+        if (b == 0 && i + AHEAD < kStageTiles * KS) f[(i + AHEAD) % (AHEAD + 1)] = qfrag(s, i + AHEAD);
+        a[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % (AHEAD + 1)], kf[b][k / 2], k < 2 ? f32x16{} : a[b], 0, 0, 0);
+        if (cont || u > 0) {
+          if (k * EACH % 8 == 0 && k * EACH < 24)
+            l2[(k * EACH / 8 + 1) % 2] = lse_quad(u ? s : s - 1, u ? u - 1 : kStageTiles - 1, k * EACH / 8 + 1);
+          if (k >= 2) sums(k - 2);
+          if (k >= 1) exps(k - 1);
+          fmas(k);
+        }
+        if (k == NM - 1 && u + 1 < kStageTiles) l2[0] = lse_quad(s, u, 0);
+        // Kept in this order by groups (an MFMA, an LDS read, the vector work of a
+        // turn) rather than a barrier per turn: 575 -> 556 us.
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x402, 3 * EACH, 0);
+      }
+      if (cont || u > 0) {
+        sums(NM - 2);
+        exps(NM - 1);
+        sums(NM - 1);
+        w[0] += sum[0];
+        w[1] += sum[1];
+      }
+    }
+  };
+  // The weights of tile u of stage s, from a, alone; t: its number, masked if some
+  // key is not seen by all of its rows.
+  auto finish = [&](int s, int u, int t, bool masked, const f32x16* a) __attribute__((always_inline)) {
+    float sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int quad = 0; quad < 4; ++quad) {
+      const f32x4 l2 = lse_quad(s, u, quad);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int seen_from = masked ? first_row(key0 + h * 32 + l32) : 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float v = __builtin_amdgcn_exp2f(fmaf(a[h][quad * 4 + e], sl2, -l2[e]));
+          sum[h] += t * kRowTile + quad * 8 + half * 4 + e >= seen_from ? v : 0.f;
+        }
+      }
+    }
+    w[0] += sum[0];
+    w[1] += sum[1];
+  };
+  auto alone = [&](int s, int u, int t) __attribute__((always_inline)) {
+    f32x16* const a = acc[0];
+    a[0] = a[1] = f32x16{};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const bf16x8 f = qfrag(s, u * KS + ks);
+      a[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, kf[0][ks], a[0], 0, 0, 0);
+      a[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, kf[1][ks], a[1], 0, 0, 0);
+    }
+    finish(s, u, t, t < full, a);
+  };
+
+  const int stages = (t1 - t0 + kStageTiles - 1) / kStageTiles;
+  // Whole stages of tiles that need no mask.
+  const int whole0 = max(0, (full - t0 + kStageTiles - 1) / kStageTiles), whole1 = (t1 - t0) / kStageTiles;
   if (stages > 0) {
     issue(0);
-    put_lse(0, load_lse(0));
+    float coming = 0.f;  // the LSE of the next stage
+    if (wave < 2) put_lse(0, load_lse(0));
+    // Also the keys: without this the loop waits for them in every turn.
+    wait_vmem<0>();
+    if (stages > 1) {
+      issue(1);
+      if (wave < 2) coming = load_lse(1);
+    }
     for (int s = 0; s < stages; ++s) {
-      float next_lse = 0.f;
-      wait_vmem<0>();
+      // In flight, oldest first: this stage's copies, the next one's (and in the
+      // first wavefronts the next one's LSE).
+      if (s + 1 == stages) {
+        wait_vmem<0>();
+      } else {
+        wait_vmem<COPIES>();
+      }
       lds_barrier();
-      if (s + 1 < stages) {
-        issue(s + 1);
-        next_lse = load_lse(s + 1);
+      float later = 0.f;
+      if (s + 2 < stages) {
+        issue(s + 2);
+        if (wave < 2) later = load_lse(s + 2);
       }
-      const int t = t0 + s * RW + rw;
-      // Rows of tile t: the first sees keys up to P + r / G, the last ...
-      const int r0 = t * kRowTile, r1 = min(r0 + kRowTile, rows) - 1;
-      const bool any = t < t1 && key0 <= P + (int)div_by((uint32_t)max(r1, 0), p.group_magic, p.group_shift);
-      if (any) {
-        const bool masked = r0 + kRowTile > rows ||
-                            key0 + kWeightKeys - 1 > P + (int)div_by((uint32_t)r0, p.group_magic, p.group_shift);
-        const uint16_t* ql = &ring[s % STAGES][rw * TILE_ELEMS];
-        f32x16 sc[2] = {f32x16{}, f32x16{}};
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          const bf16x8 a = *reinterpret_cast<const bf16x8*>(ql + l32 * D + (((ks * 2 + half) ^ q_swizzle<D>(l32)) << 3));
-          sc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, kf[0][ks], sc[0], 0, 0, 0);
-          sc[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, kf[1][ks], sc[1], 0, 0, 0);
+      if (s >= whole0 && s < whole1) {
+        if (s > whole0) {
+          stage(s, std::integral_constant<bool, true>());
+        } else {
+          stage(s, std::integral_constant<bool, false>());
         }
-        // Score j of this lane belongs to row r0 + 8 (j / 4) + 4 half + j % 4.
-        float l2[16];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const f32x4 x = *reinterpret_cast<const f32x4*>(&lse2[s % STAGES][rw * kRowTile + j * 8 + half * 4]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) l2[j * 4 + e] = x[e];
-        }
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          float e[16];
-#pragma unroll
-          for (int j = 0; j < 16; ++j) e[j] = __builtin_amdgcn_exp2f(fmaf(sc[b][j], sl2, -l2[j]));
-          if (masked) {
-            // The first row that sees this lane's key.
-            const int64_t from = max((int64_t)(key0 + b * 32 + l32 - P) * p.group, (int64_t)0);
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              const int r = r0 + (j >> 2) * 8 + half * 4 + (j & 3);
-              e[j] = r >= from && r < rows ? e[j] : 0.f;
-            }
-          }
-#pragma unroll
-          for (int off = 8; off > 0; off >>= 1)
-#pragma unroll
-            for (int j = 0; j < off; ++j) e[j] += e[j + off];
-          w[b] += e[0];
+        if (s + 1 == whole1) finish(s, kStageTiles - 1, 0, false, acc[1]);
+      } else {
+#pragma unroll 1
+        for (int u = 0; u < kStageTiles; ++u) {
+          const int t = t0 + s * kStageTiles + u;
+          if (t >= from && t < t1) alone(s, u, t);
         }
       }
-      if (s + 1 < stages) put_lse(s + 1, next_lse);
+      if (wave < 2 && s + 1 < stages) put_lse(s + 1, coming);
+      coming = later;
     }
   }
 
   w[0] = lane_pair_sum(w[0]);
   w[1] = lane_pair_sum(w[1]);
-  float total_w = half ? w[1] : w[0];  // of key key0 + lane
-  if constexpr (RW > 1) {
-    sums[rw][kw * kWeightKeys + lane] = total_w;
-    __syncthreads();
-    if (rw != 0) return;
-    total_w = 0.f;
-#pragma unroll
-    for (int r = 0; r < RW; ++r) total_w += sums[r][kw * kWeightKeys + lane];
-  }
+  const float total = half ? w[1] : w[0];  // of key key0 + lane
   const int key = key0 + lane;
   if (key >= n) return;
   if (p.row_parts == 1) {
     const int64_t at = kv_head * p.weight_stride + key;
-    p.weights[at] = (p.prev != nullptr && key < P ? p.prev[at] : 0.f) + total_w;
+    p.weights[at] = (p.prev != nullptr && key < P ? p.prev[at] : 0.f) + total;
   } else {
-    p.ws[((int64_t)part * p.h_kv + kv_head) * n + key] = total_w;
+    p.ws[((int64_t)part * p.h_kv + kv_head) * n + key] = total;
   }
 #endif  // __HIP_DEVICE_COMPILE__
 }
@@ -298,12 +406,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_key_weights_kernel(c
 template <int D>
 void launch(const KeyWeightsLaunch& p, hipStream_t stream) {
   const dim3 grid((unsigned)((int64_t)p.key_blocks * p.row_parts * p.h_kv)), block(64 * kWeightWaves);
-  switch (p.key_waves) {
-    case 1: hipLaunchKernelGGL((key_weights_kernel<D, 1>), grid, block, 0, stream, p); break;
-    case 2: hipLaunchKernelGGL((key_weights_kernel<D, 2>), grid, block, 0, stream, p); break;
-    case 4: hipLaunchKernelGGL((key_weights_kernel<D, 4>), grid, block, 0, stream, p); break;
-    default: hipLaunchKernelGGL((key_weights_kernel<D, 8>), grid, block, 0, stream, p); break;
-  }
+  hipLaunchKernelGGL((key_weights_kernel<D>), grid, block, 0, stream, p);
   if (p.row_parts > 1) {
     const int n = p.prefix_len + p.chunk_len;
     hipLaunchKernelGGL(key_weights_join_kernel, dim3((n + 255) / 256, p.h_kv), dim3(256), 0, stream, p);

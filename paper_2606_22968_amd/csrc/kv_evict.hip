@@ -3,19 +3,27 @@
 //
 // Selection: the positions between the sinks and the recent ones are candidates,
 // c of them stay.  A weight becomes a 32-bit key whose unsigned order is the
-// order of the weights (NaN the largest, -0 as 0); the c-th largest key is found
-// digit by digit from histograms of the candidates that share the digits found
-// so far; keys above it stay, and of those equal to it the first ones.  Counts
-// are integers, so the result does not depend on the order of the atomics.
+// order of the weights (NaN the largest, -0 as 0); the c-th largest key (the
+// border) is found digit by digit, 10, 12 and 10 bits, from histograms of the
+// candidates that have the digits found so far; keys above it stay, and of those
+// equal to it the first ones.  Counts are integers, so the result does not depend
+// on the order of the atomics.
+//
+// Up to kEvictOneGroup candidates are held by one workgroup per head, which needs one
+// launch; more are cut into chunks, in four launches.
 #include "attn_device.h"
 #include "serve.h"
+
+#include <type_traits>
 
 namespace mocap {
 namespace {
 
 constexpr int kSelectThreads = 1024;
 constexpr int kSelectWaves = kSelectThreads / 64;
-constexpr int kBins = 256;
+constexpr int kDigitBits[3] = {10, 12, 10}, kDigitShift[3] = {22, 10, 0};
+constexpr int kMostBins = 4096;
+constexpr int bins(int d) { return 1 << kDigitBits[d]; }
 
 __device__ __forceinline__ uint32_t weight_key(float w) {
   if (w != w) return 0xFFFFFFFFu;
@@ -23,142 +31,412 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
   return x >> 31 ? ~x : x | 0x80000000u;
 }
 
-__global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const EvictLaunch p) {
-  __shared__ uint32_t hist[kBins];
-  __shared__ uint32_t digit_s, left_s;
-  __shared__ uint32_t counts[2][kSelectWaves];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int h = blockIdx.x;
-  const float* w = p.weights + h * p.weight_stride;
-  const int first = p.sinks, end = p.n - p.recent;  // candidates [first, end)
-  uint32_t left = (uint32_t)(p.keep - p.sinks - p.recent);  // still to be found among those with this prefix
-  uint32_t prefix = 0;
-  // Digit by digit, the highest first.  With nothing or everything to keep the
-  // border is found all the same, and `left` of the keys equal to it stay.
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = tid; i < kBins; i += kSelectThreads) hist[i] = 0;
-    __syncthreads();
-    for (int i = first + tid; i < end; i += kSelectThreads) {
-      const uint32_t k = weight_key(w[i]);
-      if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[k >> shift & (kBins - 1)], 1u);
-    }
-    __syncthreads();
-    if (wave == 0) {
-      // Lane l holds bins 255 - 4 l .. 252 - 4 l; counts above them by a scan.
-      uint32_t c[4], sum = 0;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) sum += c[j] = hist[kBins - 1 - 4 * lane - j];
-      uint32_t upto = sum;
-#pragma unroll
-      for (int off = 1; off < 64; off <<= 1) {
-        const uint32_t x = __shfl_up(upto, off);
-        upto += lane >= off ? x : 0;
-      }
-      uint32_t above = upto - sum;
-      // The bin that holds the left-th largest (left >= 1); with left = 0 none is needed.
-      if (left > above && left <= upto) {
-        for (int j = 0; j < 4; ++j) {
-          if (left <= above + c[j]) {
-            digit_s = kBins - 1 - 4 * lane - j;
-            left_s = left - above;
-            break;
-          }
-          above += c[j];
-        }
-      } else if (left == 0 && lane == 0) {
-        digit_s = kBins - 1;
-        left_s = 0;
-      }
-    }
-    __syncthreads();
-    prefix |= digit_s << shift;
-    left = left_s;
-    __syncthreads();
+// Whether a key has the digits before digit d of the border found so far.
+template <int d>
+__device__ __forceinline__ bool in_prefix(uint32_t key, uint32_t prefix) {
+  if constexpr (d == 0) {
+    return true;
+  } else {
+    return (key ^ prefix) >> kDigitShift[d - 1] == 0;
   }
+}
+template <int d>
+__device__ __forceinline__ uint32_t digit_of(uint32_t key) {
+  return key >> kDigitShift[d] & (bins(d) - 1);
+}
 
-  // Kept positions in order: sinks, candidates, recent ones.
-  int32_t* kept = p.kept + (int64_t)h * p.keep;
-  float* kept_w = p.kept_weights ? p.kept_weights + (int64_t)h * p.keep : nullptr;
-  auto put = [&](int at, int pos) {
+// `left` of the candidates with the digits in `prefix` stay.
+struct Border {
+  uint32_t prefix, left;
+};
+
+// Adds digit d: the bin that holds the left-th largest of those candidates,
+// count(bin) being their histogram.  Every thread calls it and gets the result;
+// with left = 0 it is the highest digit, so that no key lies above the border.
+template <int d, class Count>
+__device__ __forceinline__ void find_digit(Count count, Border& x) {
+  constexpr int EACH = bins(d) / kSelectThreads;
+  __shared__ uint32_t totals[kSelectWaves], found[2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int top = bins(d) - 1 - EACH * tid;  // this thread's bins, downwards
+  uint32_t c[EACH], sum = 0;
+#pragma unroll
+  for (int j = 0; j < EACH; ++j) sum += c[j] = count(top - j);
+  uint32_t upto = sum;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const uint32_t y = __shfl_up(upto, off);
+    upto += lane >= off ? y : 0;
+  }
+  if (lane == 63) totals[wave] = upto;
+  if (tid == 0) {
+    found[0] = bins(d) - 1;
+    found[1] = 0;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kSelectWaves; ++w) upto += w < wave ? totals[w] : 0;
+  uint32_t above = upto - sum;
+  if (x.left > above && x.left <= upto) {
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+      if (x.left > above && x.left <= above + c[j]) {
+        found[0] = top - j;
+        found[1] = x.left - above;
+      }
+      above += c[j];
+    }
+  }
+  __syncthreads();
+  x.prefix |= found[0] << kDigitShift[d];
+  x.left = found[1];
+  __syncthreads();
+}
+
+struct Output {
+  int32_t* kept;
+  float* kept_weights;
+  __device__ __forceinline__ void put(int at, int pos, float w) const {
     kept[at] = pos;
-    if (kept_w) kept_w[at] = w[pos];
-  };
-  for (int i = tid; i < p.sinks; i += kSelectThreads) put(i, i);
-  for (int i = tid; i < p.recent; i += kSelectThreads) put(p.keep - p.recent + i, end + i);
-  uint32_t equal_before = 0;
-  int at0 = p.sinks;
-  const uint64_t below = (1ull << lane) - 1;
-  for (int i0 = first; i0 < end; i0 += kSelectThreads) {
-    const int i = i0 + tid;
-    const uint32_t k = i < end ? weight_key(w[i]) : 0;
-    const bool equal = i < end && k == prefix;
-    const uint64_t eq = __builtin_amdgcn_ballot_w64(equal);
-    if (lane == 0) counts[0][wave] = __builtin_popcountll(eq);
-    __syncthreads();
-    uint32_t eq_at = equal_before + __builtin_popcountll(eq & below), eq_all = 0;
-    for (int x = 0; x < kSelectWaves; ++x) {
-      eq_at += x < wave ? counts[0][x] : 0;
-      eq_all += counts[0][x];
-    }
-    const bool stays = i < end && (k > prefix || (equal && eq_at < left));
-    const uint64_t st = __builtin_amdgcn_ballot_w64(stays);
-    if (lane == 0) counts[1][wave] = __builtin_popcountll(st);
-    __syncthreads();
-    uint32_t at = __builtin_popcountll(st & below), all = 0;
-    for (int x = 0; x < kSelectWaves; ++x) {
-      at += x < wave ? counts[1][x] : 0;
-      all += counts[1][x];
-    }
-    if (stays) put(at0 + at, i);
-    at0 += all;
-    equal_before += eq_all;
+    if (kept_weights) kept_weights[at] = w;
+  }
+};
+__device__ __forceinline__ Output output_of(const EvictLaunch& p, int h) {
+  return Output{p.kept + (int64_t)h * p.keep, p.kept_weights ? p.kept_weights + (int64_t)h * p.keep : nullptr};
+}
+__device__ __forceinline__ void put_always_kept(const EvictLaunch& p, const Output& out, const float* w, int64_t first,
+                                                int64_t step) {
+  for (int64_t i = first; i < p.sinks; i += step) out.put((int)i, (int)i, w[i]);
+  for (int64_t i = first; i < p.recent; i += step) {
+    const int pos = p.n - p.recent + (int)i;
+    out.put(p.keep - p.recent + (int)i, pos, w[pos]);
   }
 }
 
-// Copies the kept positions' keys and values: one workgroup per 64 positions of
-// dst and KV head.  A kept key is one row; a kept value's dims are spread over as
-// many rows of V, where neighbouring kept positions share lines.
-template <int D>
-__global__ __launch_bounds__(256) void evict_copy_kernel(const EvictLaunch p) {
-  constexpr int T = 64, CHUNKS = D / 8;
-  __shared__ int64_t src_block[T];  // first element of the source block's head, K and V alike
-  __shared__ int src_slot[T];
-  const int tid = threadIdx.x, h = blockIdx.y;
-  const int pos0 = blockIdx.x * T;
-  const int count = min(T, p.keep - pos0);
-  if (tid < count) {
-    const int pos = p.kept[(int64_t)h * p.keep + pos0 + tid];
-    const int lb = pos / p.src_block_size;
-    src_block[tid] = ((int64_t)p.src_table[lb] * p.h_kv + h) * D * p.src_block_size;
-    src_slot[tid] = pos - lb * p.src_block_size;
+// Writes those that stay of 1024 ROUNDS consecutive candidates, in order:
+// candidate r 1024 + tid is key[r], w[r] at position pos0 + r 1024 + tid, the
+// first `count` exist.  above and equal: how many candidates above the border and
+// equal to it have come before; moved on by this call.  at0: output position of
+// the first candidate that stays.
+template <int ROUNDS>
+__device__ __forceinline__ void compact(const uint32_t (&key)[ROUNDS], const float (&w)[ROUNDS], int pos0, int count,
+                                        const Border& border, int at0, uint32_t& above, uint32_t& equal,
+                                        const Output& out) {
+  constexpr int SLOTS = ROUNDS * kSelectWaves;
+  static_assert(SLOTS <= kSelectThreads, "a thread for every (round, wave)");
+  __shared__ uint32_t above_n[SLOTS + 1], equal_n[SLOTS + 1], totals[2][kSelectWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const uint64_t below = (1ull << lane) - 1;
+  // Counts of every (round, wave), then the sums before each.
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) {
+    const bool live = r * kSelectThreads + tid < count;
+    const uint64_t gt = __builtin_amdgcn_ballot_w64(live && key[r] > border.prefix);
+    const uint64_t eq = __builtin_amdgcn_ballot_w64(live && key[r] == border.prefix);
+    if (lane == 0) {
+      above_n[r * kSelectWaves + wave] = __builtin_popcountll(gt);
+      equal_n[r * kSelectWaves + wave] = __builtin_popcountll(eq);
+    }
   }
   __syncthreads();
+  const uint32_t a0 = tid < SLOTS ? above_n[tid] : 0, b0 = tid < SLOTS ? equal_n[tid] : 0;
+  uint32_t a = a0, b = b0;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const uint32_t y = __shfl_up(a, off), z = __shfl_up(b, off);
+    a += lane >= off ? y : 0;
+    b += lane >= off ? z : 0;
+  }
+  if (lane == 63) {
+    totals[0][wave] = a;
+    totals[1][wave] = b;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < kSelectWaves; ++x) {
+    a += x < wave ? totals[0][x] : 0;
+    b += x < wave ? totals[1][x] : 0;
+  }
+  if (tid < SLOTS) {
+    above_n[tid] = a - a0;
+    equal_n[tid] = b - b0;
+  }
+  if (tid == kSelectThreads - 1) {
+    above_n[SLOTS] = a;
+    equal_n[SLOTS] = b;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) {
+    const int i = r * kSelectThreads + tid;
+    const bool live = i < count;
+    const bool gt = live && key[r] > border.prefix, eq = live && key[r] == border.prefix;
+    const uint32_t gt_at = above + above_n[r * kSelectWaves + wave] + __builtin_popcountll(__builtin_amdgcn_ballot_w64(gt) & below);
+    const uint32_t eq_at = equal + equal_n[r * kSelectWaves + wave] + __builtin_popcountll(__builtin_amdgcn_ballot_w64(eq) & below);
+    // Of the equal ones the first `left` stay.
+    if (gt || (eq && eq_at < border.left)) out.put(at0 + (int)(gt_at + min(eq_at, border.left)), pos0 + i, w[r]);
+  }
+  above += above_n[SLOTS];
+  equal += equal_n[SLOTS];
+  __syncthreads();
+}
+
+// ---- One workgroup per head ----
+template <int ROUNDS>
+__global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const EvictLaunch p) {
+  __shared__ uint32_t hist[kMostBins];
+  const int tid = threadIdx.x, h = blockIdx.x;
+  const float* w = p.weights + h * p.weight_stride;
+  const int first = p.sinks, count = p.n - p.recent - p.sinks;
+  float x[ROUNDS];
+  uint32_t key[ROUNDS];
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) {
+    const int i = r * kSelectThreads + tid;
+    x[r] = i < count ? w[first + i] : 0.f;
+  }
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) key[r] = weight_key(x[r]);
+  const Output out = output_of(p, h);
+  put_always_kept(p, out, w, tid, kSelectThreads);
+  Border border{0, (uint32_t)(p.keep - p.sinks - p.recent)};
+  auto digit = [&](auto dd) __attribute__((always_inline)) {
+    constexpr int d = decltype(dd)::value;
+    for (int i = tid; i < bins(d); i += kSelectThreads) hist[i] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r)
+      if (r * kSelectThreads + tid < count && in_prefix<d>(key[r], border.prefix)) atomicAdd(&hist[digit_of<d>(key[r])], 1u);
+    __syncthreads();
+    find_digit<d>([&](int bin) { return hist[bin]; }, border);
+  };
+  digit(std::integral_constant<int, 0>());
+  digit(std::integral_constant<int, 1>());
+  digit(std::integral_constant<int, 2>());
+  uint32_t above = 0, equal = 0;
+  compact<ROUNDS>(key, x, first, count, border, p.sinks, above, equal, out);
+}
+
+// ---- p.chunks workgroups per head ----
+// Each takes an even run of the candidates.  Every launch finds the digit that
+// the one before has counted, every workgroup for itself (it reads 128 KiB at
+// most, from the L2), and counts the next.  The first and the last digit are
+// counted per chunk, so nothing needs clearing beforehand and the last launch
+// knows how many of the chunks before its own stay; the second is counted with
+// atomics in memory that the first launch clears.
+struct ChunkCounts {  // of one head
+  uint32_t* first;    // [chunks][bins(0)]
+  uint32_t* second;   // [bins(1)]
+  uint32_t* third;    // [chunks][bins(2)]
+  uint32_t* above;    // [chunks]: candidates above the first two digits of the border
+  uint32_t* border;   // prefix and left behind the first, then the second digit
+};
+__device__ __forceinline__ ChunkCounts counts_of(const EvictLaunch& p, int h) {
+  uint32_t* x = p.ws + (int64_t)h * evict_head_words(p.chunks);
+  ChunkCounts c;
+  c.first = x;
+  c.second = c.first + p.chunks * bins(0);
+  c.third = c.second + bins(1);
+  c.above = c.third + p.chunks * bins(2);
+  c.border = c.above + p.chunks;
+  return c;
+}
+static_assert(bins(0) == kEvictFirstBins && bins(1) == kEvictSecondBins && bins(2) == kEvictThirdBins, "workspace layout");
+
+struct Chunk {
+  const float* w;  // of candidate 0
+  int begin, end;  // its candidates
+};
+__device__ __forceinline__ Chunk chunk_of(const EvictLaunch& p, int h, int chunk) {
+  const int64_t all = p.n - p.recent - p.sinks;
+  return Chunk{p.weights + h * p.weight_stride + p.sinks, (int)(all * chunk / p.chunks), (int)(all * (chunk + 1) / p.chunks)};
+}
+
+__global__ __launch_bounds__(kSelectThreads) void evict_first_kernel(const EvictLaunch p) {
+  __shared__ uint32_t hist[bins(0)];
+  const int tid = threadIdx.x, chunk = blockIdx.x, h = blockIdx.y;
+  const ChunkCounts c = counts_of(p, h);
+  const Chunk x = chunk_of(p, h, chunk);
+  hist[tid] = 0;
+  if (chunk == 0)
+    for (int i = tid; i < bins(1); i += kSelectThreads) c.second[i] = 0;
+  put_always_kept(p, output_of(p, h), x.w - p.sinks, (int64_t)chunk * kSelectThreads + tid,
+                  (int64_t)p.chunks * kSelectThreads);
+  __syncthreads();
+  for (int i = x.begin + tid; i < x.end; i += kSelectThreads) atomicAdd(&hist[digit_of<0>(weight_key(x.w[i]))], 1u);
+  __syncthreads();
+  c.first[chunk * bins(0) + tid] = hist[tid];
+}
+static_assert(bins(0) == kSelectThreads && bins(2) == kSelectThreads, "a thread per bin of the first and last digit");
+
+__global__ __launch_bounds__(kSelectThreads) void evict_second_kernel(const EvictLaunch p) {
+  __shared__ uint32_t hist[bins(1)];
+  const int tid = threadIdx.x, chunk = blockIdx.x, h = blockIdx.y;
+  const ChunkCounts c = counts_of(p, h);
+  const Chunk x = chunk_of(p, h, chunk);
+  for (int i = tid; i < bins(1); i += kSelectThreads) hist[i] = 0;
+  Border border{0, (uint32_t)(p.keep - p.sinks - p.recent)};
+  find_digit<0>([&](int bin) {
+    uint32_t v[kEvictMaxChunks], sum = 0;  // all loads in flight
+#pragma unroll
+    for (int y = 0; y < kEvictMaxChunks; ++y) v[y] = y < p.chunks ? c.first[y * bins(0) + bin] : 0;
+#pragma unroll
+    for (int y = 0; y < kEvictMaxChunks; ++y) sum += v[y];
+    return sum;
+  }, border);
+  if (chunk == 0 && tid == 0) {
+    c.border[0] = border.prefix;
+    c.border[1] = border.left;
+  }
+  for (int i = x.begin + tid; i < x.end; i += kSelectThreads) {
+    const uint32_t key = weight_key(x.w[i]);
+    if (in_prefix<1>(key, border.prefix)) atomicAdd(&hist[digit_of<1>(key)], 1u);
+  }
+  __syncthreads();
+  for (int i = tid; i < bins(1); i += kSelectThreads)
+    if (hist[i] != 0) atomicAdd(&c.second[i], hist[i]);
+}
+
+__global__ __launch_bounds__(kSelectThreads) void evict_third_kernel(const EvictLaunch p) {
+  __shared__ uint32_t hist[bins(2)], above_s;
+  const int tid = threadIdx.x, chunk = blockIdx.x, h = blockIdx.y;
+  const ChunkCounts c = counts_of(p, h);
+  const Chunk x = chunk_of(p, h, chunk);
+  hist[tid] = 0;
+  if (tid == 0) above_s = 0;
+  Border border{c.border[0], c.border[1]};
+  find_digit<1>([&](int bin) { return c.second[bin]; }, border);
+  if (chunk == 0 && tid == 0) {
+    c.border[2] = border.prefix;
+    c.border[3] = border.left;
+  }
+  uint32_t above = 0;
+  for (int i = x.begin + tid; i < x.end; i += kSelectThreads) {
+    const uint32_t key = weight_key(x.w[i]);
+    if (in_prefix<2>(key, border.prefix)) {
+      atomicAdd(&hist[digit_of<2>(key)], 1u);
+    } else {
+      above += key > border.prefix;
+    }
+  }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) above += __shfl_xor(above, off);
+  if ((tid & 63) == 0) atomicAdd(&above_s, above);
+  __syncthreads();
+  c.third[chunk * bins(2) + tid] = hist[tid];
+  if (tid == 0) c.above[chunk] = above_s;
+}
+
+__global__ __launch_bounds__(kSelectThreads) void evict_compact_kernel(const EvictLaunch p) {
+  constexpr int ROUNDS = 4;
+  __shared__ uint32_t above_s, equal_s;
+  const int tid = threadIdx.x, chunk = blockIdx.x, h = blockIdx.y;
+  const ChunkCounts c = counts_of(p, h);
+  const Chunk x = chunk_of(p, h, chunk);
+  if (tid == 0) above_s = equal_s = 0;
+  // Thread t looks at bin 1023 - t: in all chunks, and in those before this one.
+  const int bin = bins(2) - 1 - tid;
+  uint32_t counts[kEvictMaxChunks], sum = 0, before = 0;
+#pragma unroll
+  for (int y = 0; y < kEvictMaxChunks; ++y) counts[y] = y < p.chunks ? c.third[y * bins(2) + bin] : 0;
+  Border border{c.border[2], c.border[3]};
+  float w[ROUNDS];
+  auto load = [&](int i0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+      const int i = r * kSelectThreads + tid;
+      w[r] = i < x.end - i0 ? x.w[i0 + i] : 0.f;
+    }
+  };
+  load(x.begin);
+#pragma unroll
+  for (int y = 0; y < kEvictMaxChunks; ++y) {
+    sum += counts[y];
+    before += y < chunk ? counts[y] : 0;
+  }
+  find_digit<2>([&](int) { return sum; }, border);
+  const int digit = (int)digit_of<2>(border.prefix);
+  uint32_t above = bin > digit ? before : 0;
+  for (int y = tid; y < chunk; y += kSelectThreads) above += c.above[y];
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) above += __shfl_xor(above, off);
+  if ((tid & 63) == 0) atomicAdd(&above_s, above);
+  if (bin == digit) equal_s = before;
+  __syncthreads();
+  above = above_s;
+  uint32_t equal = equal_s;
+  const Output out = output_of(p, h);
+  for (int i0 = x.begin; i0 < x.end; i0 += ROUNDS * kSelectThreads) {
+    uint32_t key[ROUNDS];
+    const int count = min(x.end - i0, ROUNDS * kSelectThreads);
+    if (i0 > x.begin) load(i0);
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) key[r] = weight_key(w[r]);
+    compact<ROUNDS>(key, w, p.sinks + i0, count, border, p.sinks, above, equal, out);
+  }
+}
+
+// ---- Copy ----
+// One workgroup per 64 positions of dst, KV head and 32 dims.  A kept key is one
+// row.  A kept value's dims lie in as many rows of V, where neighbouring kept
+// positions share lines: a wavefront takes one dim of the 64 positions at a time.
+template <int D>
+__global__ __launch_bounds__(256) void evict_copy_kernel(const EvictLaunch p) {
+  constexpr int T = 64, DIMS = 32;
+  const int tid = threadIdx.x, h = blockIdx.y, dim0 = blockIdx.z * DIMS;
+  const int pos0 = blockIdx.x * T;
+  const int count = min(T, p.keep - pos0);
+  const int32_t* kept = p.kept + (int64_t)h * p.keep + pos0;
+  auto source = [&](int r, int* slot) __attribute__((always_inline)) {  // first element of the block's head
+    const int pos = kept[min(r, count - 1)];
+    const int lb = pos / p.src_block_size;
+    *slot = pos - lb * p.src_block_size;
+    return ((int64_t)p.src_table[lb] * p.h_kv + h) * D * p.src_block_size;
+  };
   const int lb = pos0 / p.dst_block_size;  // 64 positions lie in one block
   const int slot0 = pos0 - lb * p.dst_block_size;
   const int64_t dst = ((int64_t)p.dst_table[lb] * p.h_kv + h) * D * p.dst_block_size;
-#pragma unroll 4
-  for (int i = tid; i < count * CHUNKS; i += 256) {
-    const int r = i / CHUNKS, c = i % CHUNKS;
-    *reinterpret_cast<u32x4*>(p.k_dst + dst + (int64_t)(slot0 + r) * D + c * 8) =
-        *reinterpret_cast<const u32x4*>(p.k_src + src_block[r] + (int64_t)src_slot[r] * D + c * 8);
+  const int kr = tid / (DIMS / 8), kc = dim0 + tid % (DIMS / 8) * 8;  // K: row and first dim
+  const int vr = tid & (T - 1), ve = dim0 + tid / T;                  // V: position and first dim, 4 apart
+  int k_slot, v_slot;
+  const uint16_t* k = p.k_src + source(kr, &k_slot);
+  const uint16_t* v = p.v_src + source(vr, &v_slot) + v_slot;
+  const u32x4 key = *reinterpret_cast<const u32x4*>(k + (int64_t)k_slot * D + kc);
+  uint16_t value[DIMS / 4];
+#pragma unroll
+  for (int i = 0; i < DIMS / 4; ++i) value[i] = v[(int64_t)(ve + 4 * i) * p.src_block_size];
+  if (kr < count) *reinterpret_cast<u32x4*>(p.k_dst + dst + (int64_t)(slot0 + kr) * D + kc) = key;
+  if (vr < count) {
+#pragma unroll
+    for (int i = 0; i < DIMS / 4; ++i) p.v_dst[dst + (int64_t)(ve + 4 * i) * p.dst_block_size + slot0 + vr] = value[i];
   }
-  const int r = tid & (T - 1), e0 = tid / T;
-  if (r >= count) return;
-  const uint16_t* v = p.v_src + src_block[r] + src_slot[r];
-  uint16_t* o = p.v_dst + dst + slot0 + r;
-#pragma unroll 16
-  for (int e = e0; e < D; e += 256 / T) o[(int64_t)e * p.dst_block_size] = v[(int64_t)e * p.src_block_size];
+}
+
+template <int D>
+void launch_copy(const EvictLaunch& p, hipStream_t stream) {
+  hipLaunchKernelGGL(evict_copy_kernel<D>, dim3((p.keep + 63) / 64, p.h_kv, D / 32), dim3(256), 0, stream, p);
 }
 
 }  // namespace
 
 hipError_t launch_kv_evict(const EvictLaunch& p, int head_dim, hipStream_t stream) {
-  hipLaunchKernelGGL(evict_select_kernel, dim3(p.h_kv), dim3(kSelectThreads), 0, stream, p);
-  const dim3 grid((p.keep + 63) / 64, p.h_kv), block(256);
-  if (head_dim == 128) {
-    hipLaunchKernelGGL(evict_copy_kernel<128>, grid, block, 0, stream, p);
+  const dim3 block(kSelectThreads);
+  const int candidates = p.n - p.sinks - p.recent;
+  if (p.chunks > 0) {
+    const dim3 grid(p.chunks, p.h_kv);
+    hipLaunchKernelGGL(evict_first_kernel, grid, block, 0, stream, p);
+    hipLaunchKernelGGL(evict_second_kernel, grid, block, 0, stream, p);
+    hipLaunchKernelGGL(evict_third_kernel, grid, block, 0, stream, p);
+    hipLaunchKernelGGL(evict_compact_kernel, grid, block, 0, stream, p);
+  } else if (candidates <= 4 * kSelectThreads) {
+    hipLaunchKernelGGL(evict_select_kernel<4>, dim3(p.h_kv), block, 0, stream, p);
   } else {
-    hipLaunchKernelGGL(evict_copy_kernel<64>, grid, block, 0, stream, p);
+    hipLaunchKernelGGL(evict_select_kernel<kEvictOneGroup / kSelectThreads>, dim3(p.h_kv), block, 0, stream, p);
+  }
+  if (head_dim == 128) {
+    launch_copy<128>(p, stream);
+  } else {
+    launch_copy<64>(p, stream);
   }
   return hipGetLastError();
 }

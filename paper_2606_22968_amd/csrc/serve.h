@@ -91,10 +91,9 @@ struct WindowLaunch {
   float scale_log2;
 };
 
-// One launch of the key weight kernel.  A workgroup's eight wavefronts are
-// key_waves (1, 2, 4 or 8) along the keys, 64 each, times 8 / key_waves along
-// the rows.
-constexpr int kWeightKeys = 64;   // keys of a wavefront
+// One launch of the key weight kernel: a workgroup's eight wavefronts hold 64 keys
+// each and walk one of row_parts even cuts of the rows that see some of them.
+constexpr int kWeightKeys = 64;
 constexpr int kWeightWaves = 8;
 struct KeyWeightsLaunch {
   const uint16_t* q;
@@ -115,8 +114,7 @@ struct KeyWeightsLaunch {
   int32_t block_size;
   uint32_t block_magic;
   int32_t block_shift;
-  int32_t key_waves;
-  int32_t key_blocks;       // ceil((P + L) / (key_waves * 64))
+  int32_t key_blocks;       // ceil((P + L) / 512)
   int32_t row_parts;
   float scale_log2;
 };
@@ -135,6 +133,15 @@ struct DecodeKeyWeightsLaunch {
   float scale_log2;
 };
 
+// Selection: up to kEvictOneGroup candidates by one workgroup per head (chunks
+// = 0), more by `chunks` of them, with counts in the workspace.
+constexpr int kEvictOneGroup = 16384;
+constexpr int kEvictMaxChunks = 32;
+constexpr int kEvictFirstBins = 1024, kEvictSecondBins = 4096, kEvictThirdBins = 1024;
+// 32-bit words of workspace per head.
+constexpr int64_t evict_head_words(int chunks) {
+  return (int64_t)chunks * (kEvictFirstBins + kEvictThirdBins + 1) + kEvictSecondBins + 4;
+}
 struct EvictLaunch {
   const uint16_t* k_src;
   const uint16_t* v_src;
@@ -153,6 +160,8 @@ struct EvictLaunch {
   int32_t h_kv;
   int32_t src_block_size;
   int32_t dst_block_size;
+  int32_t chunks;
+  uint32_t* ws;
 };
 
 hipError_t launch_decode_append(const DecodeAppendLaunch& p, int head_dim, hipStream_t stream);

@@ -202,7 +202,13 @@ size_t window_workspace(const mocap::WindowLaunch& p, int32_t head_dim) {
 
 // ---- Key weights ----
 
-mocap_status plan_weights(int64_t prefix_len, int32_t chunk_len, int32_t h_q, int32_t h_kv, mocap::KeyWeightsLaunch* p) {
+// A row tile (32 rows by 512 keys), fixed work of a workgroup, and the join of row
+// parts; the fewest tiles of a part.
+constexpr double kWeightTileUs128 = 0.75, kWeightTileUs64 = 0.55, kWeightGroupUs = 4.0, kWeightJoinUs = 4.0;
+constexpr int64_t kWeightMinTiles = 4, kWeightMaxParts = 64, kWeightMaxRounds = 4;
+
+mocap_status plan_weights(int64_t prefix_len, int32_t chunk_len, int32_t h_q, int32_t h_kv, int32_t head_dim,
+                          mocap::KeyWeightsLaunch* p) {
   const int64_t group = h_q / h_kv, rows = chunk_len * group, n = prefix_len + chunk_len;
   if (rows > ((int64_t)1 << 31) - 1024) return MOCAP_ERR_UNSUPPORTED;
   int cus = 0;
@@ -214,18 +220,41 @@ mocap_status plan_weights(int64_t prefix_len, int32_t chunk_len, int32_t h_q, in
   p->h_kv = h_kv;
   p->group = (int32_t)group;
   block_divider((uint32_t)group, &p->group_magic, &p->group_shift);
-  // As many wavefronts along the keys as leave a workgroup for every compute unit.
-  p->key_waves = 8;
-  while (p->key_waves > 1 && ceil_div(n, p->key_waves * mocap::kWeightKeys) * h_kv < cus) p->key_waves /= 2;
-  p->key_blocks = (int32_t)ceil_div(n, p->key_waves * mocap::kWeightKeys);
+  const int64_t block_keys = mocap::kWeightKeys * mocap::kWeightWaves;
+  p->key_blocks = (int32_t)ceil_div(n, block_keys);
+  // Parts: one workgroup per compute unit at a time, a round costs its longest
+  // one's row tiles plus fixed work.
+  const int64_t wgs = (int64_t)p->key_blocks * h_kv, tiles = ceil_div(rows, 32);
+  if (wgs > kMaxGroups || h_kv > 65535) return MOCAP_ERR_UNSUPPORTED;
+  const double tile_us = head_dim == 128 ? kWeightTileUs128 : kWeightTileUs64;
+  double best_us = INFINITY;
   p->row_parts = 1;
-  if ((int64_t)p->key_blocks * h_kv > kMaxGroups) return MOCAP_ERR_UNSUPPORTED;
+  for (int64_t parts = 1; parts <= std::min<int64_t>(kWeightMaxParts, ceil_div(tiles, kWeightMinTiles)); ++parts) {
+    if (parts > 1 && wgs * parts > kWeightMaxRounds * cus) break;
+    double us = (double)ceil_div(wgs * parts, cus) * (ceil_div(tiles, parts) * tile_us + kWeightGroupUs);
+    if (parts > 1) us += kWeightJoinUs + 8.0 * parts * h_kv * n / kWindowMergeBytesPerUs;
+    if (us < best_us * 0.98) {
+      best_us = us;
+      p->row_parts = (int32_t)parts;
+    }
+  }
   return MOCAP_OK;
 }
 
 size_t weights_workspace(const mocap::KeyWeightsLaunch& p) {
   if (p.row_parts <= 1) return 0;
   return (size_t)p.row_parts * p.h_kv * ((size_t)p.prefix_len + p.chunk_len) * sizeof(float);
+}
+
+// ---- Eviction ----
+
+constexpr int64_t kEvictMaxPositions = (int64_t)1 << 30;  // its kernels step over positions in 32 bits
+
+// The workspace is sized for all n positions as candidates; sinks and recent
+// ones only make them fewer.
+int32_t evict_chunks(int64_t candidates) {
+  if (candidates <= mocap::kEvictOneGroup) return 0;
+  return (int32_t)std::min<int64_t>(mocap::kEvictMaxChunks, ceil_div(candidates, 4096));
 }
 
 mocap_status check_chunk(int64_t prefix_len, int32_t chunk_len) {
@@ -391,7 +420,7 @@ mocap_status mocap_key_weights_workspace_size(int64_t prefix_len, int32_t chunk_
   *bytes_out = 0;
   if (chunk_len == 0) return MOCAP_OK;
   mocap::KeyWeightsLaunch p;
-  st = plan_weights(prefix_len, chunk_len, h_q, h_kv, &p);
+  st = plan_weights(prefix_len, chunk_len, h_q, h_kv, head_dim, &p);
   if (st == MOCAP_OK) *bytes_out = weights_workspace(p);
   return st;
 }
@@ -406,7 +435,7 @@ mocap_status mocap_key_weights(const mocap_kv_store* kv, const int32_t* block_ta
   if (chunk_len == 0) return MOCAP_OK;
   if (!lse || !weights || !aligned4(lse) || !aligned4(weights) || !aligned4(prev)) return MOCAP_ERR_INVALID_ARG;
   mocap::KeyWeightsLaunch p;
-  st = plan_weights(prefix_len, chunk_len, h_q, h_kv, &p);
+  st = plan_weights(prefix_len, chunk_len, h_q, h_kv, head_dim, &p);
   if (st != MOCAP_OK) return st;
   if (p.row_parts > 1 && (!workspace || !aligned16(workspace) || workspace_bytes < weights_workspace(p)))
     return MOCAP_ERR_WORKSPACE;
@@ -461,8 +490,9 @@ mocap_status mocap_decode_key_weights(const mocap_kv_store* kv, const int32_t* b
 mocap_status mocap_kv_evict_workspace_size(int64_t n, int32_t h_kv, int32_t keep, size_t* bytes_out) {
   if (bytes_out == nullptr || n < 0 || n > kMaxPositions || h_kv <= 0 || keep < 0 || keep > n || (n > 0 && keep == 0))
     return MOCAP_ERR_INVALID_ARG;
-  if (h_kv > 65535) return MOCAP_ERR_UNSUPPORTED;
-  *bytes_out = 0;
+  if (h_kv > 65535 || n > kEvictMaxPositions) return MOCAP_ERR_UNSUPPORTED;
+  const int32_t chunks = evict_chunks(n);
+  *bytes_out = chunks > 0 ? (size_t)h_kv * mocap::evict_head_words(chunks) * sizeof(uint32_t) : 0;
   return MOCAP_OK;
 }
 
@@ -511,6 +541,8 @@ mocap_status mocap_kv_evict(const mocap_kv_store* src, const int32_t* src_table,
   p.h_kv = src->h_kv;
   p.src_block_size = src->block_size;
   p.dst_block_size = dst->block_size;
+  p.chunks = evict_chunks(n - sinks - recent);
+  p.ws = static_cast<uint32_t*>(workspace);
   return mocap::launch_kv_evict(p, src->head_dim, static_cast<hipStream_t>(stream)) == hipSuccess ? MOCAP_OK
                                                                                                   : MOCAP_ERR_HIP;
 }

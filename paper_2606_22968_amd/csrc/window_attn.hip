@@ -77,10 +77,16 @@ __global__ __launch_bounds__(kAttnThreads, 2) void window_attn_kernel(const Wind
   constexpr int BUF_ELEMS = 2 * K_ELEMS;
   constexpr int LOADS = K_ELEMS / 8 / (kAttnThreads / 2);
   constexpr int STAGES = 4;
-  __shared__ __attribute__((aligned(1024))) uint16_t lds[STAGES * BUF_ELEMS];
-  __shared__ int found[STAGES];  // the stage's tile holds non-finite values
+  // One array for the ring and what lies beside it: with several, the compiler
+  // tells them apart, takes every read of the ring to depend on the copies in
+  // flight, and waits for those (143 us instead of 1xx for 2048 tokens in a window
+  // of 4096).
+  constexpr int ROW_BITS = kWindowRows * MD;  // words
+  __shared__ __attribute__((aligned(1024))) uint16_t lds[STAGES * BUF_ELEMS + 2 * (STAGES + 2 * ROW_BITS)];
+  int* const found = reinterpret_cast<int*>(lds + STAGES * BUF_ELEMS);  // the stage's tile holds non-finite values
   // Dims of the workgroup's rows that receive +infinity or -infinity (NaN: both), as bits.
-  __shared__ uint32_t plus[kWindowRows][MD], minus[kWindowRows][MD];
+  uint32_t* const plus = reinterpret_cast<uint32_t*>(found + STAGES);
+  uint32_t* const minus = plus + ROW_BITS;
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -209,13 +215,14 @@ __global__ __launch_bounds__(kAttnThreads, 2) void window_attn_kernel(const Wind
   // key they see is noted, and in LDS the values become 0.  A lane notes half of
   // its row's dims.  Every wavefront calls this for the same tiles.
   bool apart = false;
+  const int row_bits = (wave * kAttnWaveRows + l32) * MD;
   auto set_apart = [&](int i) __attribute__((always_inline)) {
     uint16_t* vl = lds + (i % STAGES) * BUF_ELEMS + K_ELEMS;
     const int k0 = tiles.at(i) * kTileKeys;
 #pragma unroll 1
     for (int x = half * (MD / 2); x < (half + 1) * (MD / 2); ++x) {
-      uint32_t up = apart ? plus[wave * kAttnWaveRows + l32][x] : 0u;
-      uint32_t down = apart ? minus[wave * kAttnWaveRows + l32][x] : 0u;
+      uint32_t up = apart ? plus[row_bits + x] : 0u;
+      uint32_t down = apart ? minus[row_bits + x] : 0u;
 #pragma unroll 1
       for (int bit = 0; bit < 32; ++bit) {
         const int e = x * 32 + bit;
@@ -231,8 +238,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void window_attn_kernel(const Wind
           }
         }
       }
-      plus[wave * kAttnWaveRows + l32][x] = up;
-      minus[wave * kAttnWaveRows + l32][x] = down;
+      plus[row_bits + x] = up;
+      minus[row_bits + x] = down;
     }
     apart = true;
     lds_barrier();
@@ -448,8 +455,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void window_attn_kernel(const Wind
   const int64_t part_row = (int64_t)range * L * p.h_q + out_row;
 #pragma unroll
   for (int md = 0; md < MD; ++md) {
-    const uint32_t up = apart ? plus[wave * kAttnWaveRows + l32][md] : 0u;
-    const uint32_t down = apart ? minus[wave * kAttnWaveRows + l32][md] : 0u;
+    const uint32_t up = apart ? plus[row_bits + md] : 0u;
+    const uint32_t down = apart ? minus[row_bits + md] : 0u;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int dim = md * 32 + j * 8 + half * 4;

@@ -264,11 +264,14 @@ def test_key_weight_blocks(host):
     for P, L, h_kv in ((0, 1, 8), (0, 2048, 8), (30720, 2048, 8), (1 << 20, 1, 1), (100, 3, 1), (5000, 64, 2)):
         kv = store(h_kv=h_kv, block_size=1 << 16)
         assert weights(host, kv=kv, P=P, L=L, h_q=4 * h_kv, h_kv=h_kv, stride=1 << 22, n_table=1 << 10) == 0
-        out = (ctypes.c_int * 3)()
+        out = (ctypes.c_int * 2)()
         host.record_weights(out)
-        key_waves, key_blocks, parts = out
-        assert key_waves in (1, 2, 4, 8) and key_blocks * key_waves * 64 >= P + L > (key_blocks - 1) * key_waves * 64
-        assert parts >= 1
+        key_blocks, parts = out
+        assert key_blocks * 512 >= P + L > (key_blocks - 1) * 512
+        size = ctypes.c_size_t(0)
+        assert host.mocap_key_weights_workspace_size(P, L, 4 * h_kv, h_kv, 128, ctypes.byref(size)) == 0
+        assert size.value == (0 if parts == 1 else parts * h_kv * (P + L) * 4)
+        assert parts == 1 or parts * 4 <= -(-L * 4 // 32) + 3
 
 
 @pytest.mark.parametrize("src", ["decode_attn.hip", "window_attn.hip", "key_weights.hip", "kv_evict.hip"])
