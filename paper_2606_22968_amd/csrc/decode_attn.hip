@@ -9,8 +9,8 @@
 //   * Work is cut by what is there and not by sequence (see SeqBatch): a
 //     workgroup takes one part of one sequence for one KV head and up to 16 or 32
 //     of its query heads, and every part has about the same number of tiles.
-//   * A part's four wavefronts take its keys in turn, 32 at a time, each with a
-//     softmax state of its own, so there is no barrier before the end.
+//   * A part's four wavefronts take its 64-key tiles in turn, each with a softmax
+//     state of its own, so there is no barrier before the end.
 //   * Scores are computed transposed, S^T = K Q^T, with
 //     v_mfma_f32_16x16x32_bf16: 16 keys by 16 query heads.  Lane l then holds
 //     head l % 16 and four keys of each product.  The K rows of a pair of
@@ -29,34 +29,33 @@ namespace {
 
 constexpr int kDecodeWaves = 4;
 constexpr int kDecodeThreads = 64 * kDecodeWaves;
-constexpr int kStepKeys = 32;
 
 // ---- Append ----
-// One thread per 16 bytes of a position's K and V.  V is stored with the
-// positions contiguous, so each of its values goes to a line of its own.
+// One thread per 16 bytes of a position's K and V, small workgroups for many
+// compute units.  V is stored with the positions contiguous, so each of its values
+// goes to a line of its own.  Bound by latency: lengths, table, stores.
 template <int D>
-__global__ __launch_bounds__(256) void decode_append_kernel(const DecodeAppendLaunch p) {
+__global__ __launch_bounds__(64) void decode_append_kernel(const DecodeAppendLaunch p) {
   constexpr int CHUNKS = D / 8;
   const int b = blockIdx.x;
+  const int i = blockIdx.y * 64 + threadIdx.x;
+  if (i >= p.h_kv * CHUNKS) return;
+  const int h = i / CHUNKS, c = i % CHUNKS;
+  const int64_t src = ((int64_t)b * p.h_kv + h) * D + c * 8;
+  const u32x4 k = *reinterpret_cast<const u32x4*>(p.k + src);
+  const u32x4 v = *reinterpret_cast<const u32x4*>(p.v + src);
   const int64_t n = p.seq_lens[b];
   if (n <= 0 || n > p.table_stride * p.block_size) return;
   const uint32_t pos = (uint32_t)(n - 1);
   const uint32_t lb = pos / (uint32_t)p.block_size;
   const int64_t slot = pos - lb * (uint32_t)p.block_size;
-  const int64_t block = p.tables[b * p.table_stride + lb];
-  for (int i = blockIdx.y * 256 + threadIdx.x; i < p.h_kv * CHUNKS; i += gridDim.y * 256) {
-    const int h = i / CHUNKS, c = i % CHUNKS;
-    const int64_t src = ((int64_t)b * p.h_kv + h) * D + c * 8;
-    const int64_t head = (block * p.h_kv + h) * D * p.block_size;
-    const u32x4 k = *reinterpret_cast<const u32x4*>(p.k + src);
-    const u32x4 v = *reinterpret_cast<const u32x4*>(p.v + src);
-    *reinterpret_cast<u32x4*>(p.k_pool + head + slot * D + c * 8) = k;
+  const int64_t head = ((int64_t)p.tables[b * p.table_stride + lb] * p.h_kv + h) * D * p.block_size;
+  *reinterpret_cast<u32x4*>(p.k_pool + head + slot * D + c * 8) = k;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      uint16_t* dst = p.v_pool + head + (int64_t)(c * 8 + 2 * w) * p.block_size + slot;
-      dst[0] = (uint16_t)(v[w] & 0xFFFFu);
-      dst[p.block_size] = (uint16_t)(v[w] >> 16);
-    }
+  for (int w = 0; w < 4; ++w) {
+    uint16_t* dst = p.v_pool + head + (int64_t)(c * 8 + 2 * w) * p.block_size + slot;
+    dst[0] = (uint16_t)(v[w] & 0xFFFFu);
+    dst[p.block_size] = (uint16_t)(v[w] >> 16);
   }
 }
 
@@ -75,12 +74,14 @@ __global__ __launch_bounds__(kDecodeThreads) void decode_attn_kernel(const Decod
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g4 = lane >> 4;
 
-  // Logical order: item, KV head, block of query heads.
-  const int per_item = p.h_kv * p.row_blocks;
-  const int item = blockIdx.x / per_item;
-  const int in_item = blockIdx.x - item * per_item;
-  const int kv_head = in_item / p.row_blocks;
-  const int head0 = (in_item - kv_head * p.row_blocks) * (NT * 16);  // of the group
+  // Logical order: item, KV head; the blocks of query heads that read the same
+  // keys are 8 workgroups apart, on one XCD.
+  const int stripe = blockIdx.x / (8 * p.row_blocks), in_stripe = blockIdx.x - stripe * 8 * p.row_blocks;
+  const int work = stripe * 8 + (in_stripe & 7);
+  const int item = work / p.h_kv;
+  const int kv_head = work - item * p.h_kv;
+  const int head0 = (in_stripe >> 3) * (NT * 16);  // of the group
+  if (item >= p.seqs.items) return;
   const SeqPart w = locate_item(p.seqs, lane, item);
   if (w.seq == p.seqs.batch) return;
   int begin, end;
@@ -100,28 +101,33 @@ __global__ __launch_bounds__(kDecodeThreads) void decode_attn_kernel(const Decod
   const const_i32_ptr table = (const_i32_ptr)(p.seqs.tables + w.seq * p.seqs.table_stride);
   const int bs = p.seqs.block_size;
   const int64_t head_stride = (int64_t)D * bs;
-  const int k_lane = (8 * (l16 >> 2) + (l16 & 3)) * D + g4 * 8;  // key of the first product; the second's is 4 on
+  // The K rows of products 0 and 1 of a 32-key half: keys 8 (l16 / 4) + l16 % 4, and 4 on.
+  const int k_lane = (8 * (l16 >> 2) + (l16 & 3)) * D + g4 * 8;
   const int v_lane = l16 * bs + g4 * 8;
 
-  struct Tile {
-    bf16x8 k[2][KS], v[MD];
+  struct Source {
+    const uint16_t *k, *v;
   };
-  auto step_key = [&](int i) __attribute__((always_inline)) {  // first key of step i of the part
-    return w.span.tile(begin + (i >> 1)) * kTileKeys + (i & 1) * kStepKeys;
-  };
-  auto fetch = [&](int i, Tile& x) __attribute__((always_inline)) {
-    const int pos = step_key(i);
+  auto locate = [&](int i) __attribute__((always_inline)) {  // tile i of the part
+    const int pos = w.span.tile(begin + i) * kTileKeys;
     const int lb = (int)((__umulhi((uint32_t)pos, p.seqs.block_magic) + (uint32_t)pos) >> p.seqs.block_shift);
     const int slot = pos - lb * bs;
     const int64_t base = ((int64_t)table[lb] * p.h_kv + kv_head) * head_stride;
-    const uint16_t* k = p.k_pool + base + (int64_t)slot * D + k_lane;
-    const uint16_t* v = p.v_pool + base + slot + v_lane;
+    return Source{p.k_pool + base + (int64_t)slot * D + k_lane, p.v_pool + base + slot + v_lane};
+  };
+  bf16x8 k[4][KS], v[2][MD];  // of a tile: K by product, V by 32-key half
+  auto fetch_k = [&](const uint16_t* src) __attribute__((always_inline)) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < 4; ++h)
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) x.k[h][ks] = *reinterpret_cast<const bf16x8*>(k + h * 4 * D + ks * 32);
+      for (int ks = 0; ks < KS; ++ks)
+        k[h][ks] = *reinterpret_cast<const bf16x8*>(src + ((h >> 1) * 32 + (h & 1) * 4) * D + ks * 32);
+  };
+  auto fetch_v = [&](const uint16_t* src) __attribute__((always_inline)) {
 #pragma unroll
-    for (int md = 0; md < MD; ++md) x.v[md] = *reinterpret_cast<const bf16x8*>(v + (int64_t)md * 16 * bs);
+    for (int md = 0; md < MD; ++md)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) v[h][md] = *reinterpret_cast<const bf16x8*>(src + (int64_t)md * 16 * bs + h * 32);
   };
 
   f32x4 oacc[NT][MD];
@@ -135,49 +141,59 @@ __global__ __launch_bounds__(kDecodeThreads) void decode_attn_kernel(const Decod
   }
   const float sl2 = p.scale_log2;
 
-  // Steps of this wavefront; the last tile's second half may lie past the end.
-  const int steps = 2 * (end - begin);
-  Tile cur;
-  if (wave < steps) fetch(wave, cur);
-  for (int i = wave; i < steps; i += kDecodeWaves) {
-    Tile next;
-    const bool more = i + kDecodeWaves < steps;
-    if (more) fetch(i + kDecodeWaves, next);
-    const int key0 = step_key(i);
-    // Hidden keys of this lane's eight, key0 + 8 g4 .. + 7, as bits.
-    uint32_t hidden = 0;
-    const bool masked = key0 + kStepKeys > w.span.len || (key0 < w.span.low && key0 + kStepKeys > w.span.sink_end);
-    if (masked) {
+  // A wavefront's tiles: wave, wave + 4, ...  The next tile's K is requested as
+  // soon as this one's is used up, its V likewise.
+  const int tiles = end - begin;
+  if (wave < tiles) {
+    const Source first = locate(wave);
+    fetch_k(first.k);
+    fetch_v(first.v);
+  }
+  for (int i = wave; i < tiles; i += kDecodeWaves) {
+    const bool more = i + kDecodeWaves < tiles;
+    const Source next = locate(more ? i + kDecodeWaves : i);
+    f32x4 s[NT][4];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int key = key0 + g4 * 8 + e;
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        s[t][h] = f32x4{};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+          s[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[h][ks], qf[t][ks], s[t][h], 0, 0, 0);
+      }
+    if (more) fetch_k(next.k);
+    // Score e of a lane belongs to key key0 + 32 (e / 8) + 8 g4 + e % 8; hidden ones as bits.
+    const int key0 = w.span.tile(begin + i) * kTileKeys;
+    uint32_t hidden = 0;
+    if (key0 + kTileKeys > w.span.len || (key0 < w.span.low && key0 + kTileKeys > w.span.sink_end)) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int key = key0 + (e >> 3) * 32 + g4 * 8 + (e & 7);
         const bool seen = key < w.span.len && (key < w.span.sink_end || key >= w.span.low);
         hidden |= seen ? 0u : 1u << e;
       }
       // What a hidden position holds may be NaN; its probability is 0.
 #pragma unroll
-      for (int md = 0; md < MD; ++md) {
-        u32x4 x = __builtin_bit_cast(u32x4, cur.v[md]);
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          x[e] &= (hidden >> (2 * e) & 1 ? 0u : 0x0000FFFFu) | (hidden >> (2 * e + 1) & 1 ? 0u : 0xFFFF0000u);
-        cur.v[md] = __builtin_bit_cast(bf16x8, x);
-      }
+        for (int md = 0; md < MD; ++md) {
+          u32x4 x = __builtin_bit_cast(u32x4, v[h][md]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            x[e] &= (hidden >> (8 * h + 2 * e) & 1 ? 0u : 0x0000FFFFu) | (hidden >> (8 * h + 2 * e + 1) & 1 ? 0u : 0xFFFF0000u);
+          v[h][md] = __builtin_bit_cast(bf16x8, x);
+        }
     }
+    bf16x8 hi[NT][2], lo[NT][2];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      f32x4 s[2] = {f32x4{}, f32x4{}};
+      float x[16];
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        s[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cur.k[0][ks], qf[t][ks], s[0], 0, 0, 0);
-        s[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cur.k[1][ks], qf[t][ks], s[1], 0, 0, 0);
-      }
-      float x[8];  // of keys key0 + 8 g4 + e
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = hidden >> e & 1 ? -INFINITY : s[e >> 2][e & 3];
+      for (int e = 0; e < 16; ++e) x[e] = hidden >> e & 1 ? -INFINITY : s[t][e >> 2][e & 3];
       float mx = x[0];
 #pragma unroll
-      for (int e = 1; e < 8; ++e) mx = fmaxf(mx, x[e]);
+      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, x[e]);
       const float m_new = fmaxf(m_run[t], quad_rows_max(mx) * sl2);
       const float ref = m_new == -INFINITY ? 0.f : m_new;
       // The accumulators are scaled only when some row's maximum has grown.
@@ -188,27 +204,31 @@ __global__ __launch_bounds__(kDecodeThreads) void decode_attn_kernel(const Decod
         for (int md = 0; md < MD; ++md) oacc[t][md] *= f;
         m_run[t] = m_new;
       }
-      float e2[8], lo[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        e2[e] = __builtin_amdgcn_exp2f(fmaf(x[e], sl2, -ref));
-        l_run[t] += e2[e];
-        lo[e] = e2[e] - (float)(__bf16)e2[e];
-      }
-      u32x4 ph, pl;
+      for (int h = 0; h < 2; ++h) {
+        u32x4 ph, pl;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        ph[e] = pack_bf16x2(e2[2 * e], e2[2 * e + 1]);
-        pl[e] = pack_bf16x2(lo[2 * e], lo[2 * e + 1]);
-      }
-      const bf16x8 hi8 = __builtin_bit_cast(bf16x8, ph), lo8 = __builtin_bit_cast(bf16x8, pl);
-#pragma unroll
-      for (int md = 0; md < MD; ++md) {
-        oacc[t][md] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cur.v[md], hi8, oacc[t][md], 0, 0, 0);
-        oacc[t][md] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cur.v[md], lo8, oacc[t][md], 0, 0, 0);
+        for (int e = 0; e < 4; ++e) {
+          const float a = __builtin_amdgcn_exp2f(fmaf(x[8 * h + 2 * e], sl2, -ref));
+          const float b = __builtin_amdgcn_exp2f(fmaf(x[8 * h + 2 * e + 1], sl2, -ref));
+          l_run[t] += a + b;
+          ph[e] = pack_bf16x2(a, b);
+          pl[e] = pack_bf16x2(a - __uint_as_float(ph[e] << 16), b - __uint_as_float(ph[e] & 0xFFFF0000u));
+        }
+        hi[t][h] = __builtin_bit_cast(bf16x8, ph);
+        lo[t][h] = __builtin_bit_cast(bf16x8, pl);
       }
     }
-    cur = next;
+#pragma unroll
+    for (int md = 0; md < MD; ++md)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          oacc[t][md] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[h][md], hi[t][h], oacc[t][md], 0, 0, 0);
+          oacc[t][md] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[h][md], lo[t][h], oacc[t][md], 0, 0, 0);
+        }
+    if (more) fetch_v(next.v);
   }
 
   // The wavefronts' partials meet in LDS.  Lane l holds head l % 16 and dims
@@ -264,43 +284,86 @@ __global__ __launch_bounds__(kDecodeThreads) void decode_attn_kernel(const Decod
 }
 
 // ---- Join ----
-// One wavefront per (sequence, query head) that was cut: lse = ln sum exp lse_r,
-// o = sum exp(lse_r - lse) o_r over its parts r, in order.
+// One workgroup per (sequence, query head) that was cut: lse = ln sum exp lse_r,
+// o = sum exp(lse_r - lse) o_r over its parts r, in order.  Bound by the chain of
+// loads: every wavefront takes a quarter of the parts, lane r the LSE of its r-th,
+// forms 64 weights together, and requests the partials of 8 (head_dim 128: 16)
+// parts at once, the first before any weight is known.
 template <int D>
 __global__ __launch_bounds__(kDecodeThreads) void decode_join_kernel(const DecodeAttnLaunch p) {
-  constexpr int QUADS = D / 4, SIDE = 64 / QUADS;  // parts read at a time
-  const int lane = threadIdx.x & 63;
-  const int64_t at = (int64_t)blockIdx.x * kDecodeWaves + (threadIdx.x >> 6);
-  if (at >= (int64_t)p.seqs.batch * p.h_q) return;
+  constexpr int QUADS = D / 4, SIDE = 64 / QUADS;  // parts read side by side
+  constexpr int kAhead = 8;
+  __shared__ float wave_m[kDecodeWaves], wave_z[kDecodeWaves];
+  __shared__ __attribute__((aligned(16))) f32x4 wave_o[kDecodeWaves][QUADS];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t at = blockIdx.x;
   const int seq = (int)(at / p.h_q), head = (int)(at - (int64_t)seq * p.h_q);
   int first;
   const SeqPart w = parts_of(p.seqs, lane, seq, &first);
   if (w.parts == 1) return;
+  const int begin = w.parts * wave / kDecodeWaves, end = w.parts * (wave + 1) / kDecodeWaves;
   const int quad = lane % QUADS, side = lane / QUADS;
   const float* lse = p.ws_lse + (int64_t)first * p.h_q + head;
   const float* o = p.ws_o + ((int64_t)first * p.h_q + head) * D + quad * 4;
-  float m = -INFINITY;
-  for (int r = lane; r < w.parts; r += 64) m = fmaxf(m, lse[(int64_t)r * p.h_q]);
+  f32x4 v[kAhead];
+  auto fetch = [&](int r0) __attribute__((always_inline)) {  // parts r0 + side, ...
 #pragma unroll
-  for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
+    for (int j = 0; j < kAhead; ++j)
+      v[j] = *reinterpret_cast<const f32x4*>(o + (int64_t)min(r0 + j * SIDE + side, w.parts - 1) * p.h_q * D);
+  };
+  auto load_lse = [&](int r) { return r < end ? lse[(int64_t)r * p.h_q] : -INFINITY; };
+  fetch(begin);
+  float lr = load_lse(begin + lane);
+  float m = lr;
+  for (int r = begin + lane + 64; r < end; r += 64) m = fmaxf(m, load_lse(r));
+  m = wave_largest(m);
   float z = 0.f;
   f32x4 acc = f32x4{};
-  for (int r = side; r < w.parts; r += SIDE) {
-    const float lr = lse[(int64_t)r * p.h_q];
-    const f32x4 v = *reinterpret_cast<const f32x4*>(o + (int64_t)r * p.h_q * D);
-    const bool used = lr != -INFINITY;
-    const float f = used ? expf(lr - m) : 0.f;
-    z += f;
+  for (int r0 = begin; r0 < end; r0 += 64) {
+    if (r0 > begin) lr = load_lse(r0 + lane);
+    const float weight = lr != -INFINITY ? expf(lr - m) : 0.f;  // NaN reaches the result
+    z += weight;
+    const int n = min(64, end - r0);
+    for (int i0 = 0; i0 < n; i0 += kAhead * SIDE) {
+      if (r0 + i0 > begin) fetch(r0 + i0);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] = fmaf(f, used ? v[e] : 0.f, acc[e]);
+      for (int j = 0; j < kAhead; ++j) {
+        // Lanes past the last part hold a weight of 0.
+        float f = 0.f;
+#pragma unroll
+        for (int x = 0; x < SIDE; ++x) {
+          const float fx = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(weight), (i0 + j * SIDE + x) & 63));
+          f = side == x ? fx : f;
+        }
+        const bool used = f != 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] = fmaf(used ? f : 0.f, used ? v[j][e] : 0.f, acc[e]);
+      }
+    }
   }
+  z = wave_total(z);
 #pragma unroll
-  for (int off = 32; off >= QUADS; off >>= 1) {
-    z += __shfl_xor(z, off);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], off);
+  for (int e = 0; e < 4; ++e) acc[e] = SIDE == 2 ? lane_pair_sum(acc[e]) : quad_rows_sum(acc[e]);
+  if (lane == 0) {
+    wave_m[wave] = m;
+    wave_z[wave] = z;
   }
-  if (side != 0) return;
+  if (side == 0) wave_o[wave][quad] = acc;
+  __syncthreads();
+  if (threadIdx.x >= QUADS) return;
+  m = wave_m[0];
+#pragma unroll
+  for (int x = 1; x < kDecodeWaves; ++x) m = fmaxf(m, wave_m[x]);
+  z = 0.f;
+  acc = f32x4{};
+#pragma unroll
+  for (int x = 0; x < kDecodeWaves; ++x) {
+    // A wavefront without parts, or whose parts have no keys, has a sum of 0.
+    const float f = wave_z[x] != 0.f ? expf(wave_m[x] - m) : 0.f;
+    z += f != 0.f ? f * wave_z[x] : 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] += f != 0.f ? f * wave_o[x][quad][e] : 0.f;
+  }
   const float inv = z == 0.f ? 0.f : 1.f / z;
   bf16x4 out;
 #pragma unroll
@@ -311,16 +374,15 @@ __global__ __launch_bounds__(kDecodeThreads) void decode_join_kernel(const Decod
 
 template <int D>
 void launch(const DecodeAttnLaunch& p, hipStream_t stream) {
-  const dim3 grid((unsigned)((int64_t)p.seqs.items * p.h_kv * p.row_blocks)), block(kDecodeThreads);
-  if (p.group <= 16) {
+  const int64_t work = ((int64_t)p.seqs.items * p.h_kv + 7) / 8 * 8;
+  const dim3 grid((unsigned)(work * p.row_blocks)), block(kDecodeThreads);
+  if (p.group <= 16 * p.row_blocks) {
     hipLaunchKernelGGL((decode_attn_kernel<D, 1>), grid, block, 0, stream, p);
   } else {
     hipLaunchKernelGGL((decode_attn_kernel<D, 2>), grid, block, 0, stream, p);
   }
   if (!p.may_split) return;
-  const int64_t rows = (int64_t)p.seqs.batch * p.h_q;
-  hipLaunchKernelGGL((decode_join_kernel<D>), dim3((unsigned)((rows + kDecodeWaves - 1) / kDecodeWaves)), block, 0,
-                     stream, p);
+  hipLaunchKernelGGL((decode_join_kernel<D>), dim3((unsigned)(p.seqs.batch * p.h_q)), block, 0, stream, p);
 }
 
 }  // namespace
@@ -336,7 +398,7 @@ hipError_t launch_decode_attn(const DecodeAttnLaunch& p, int head_dim, hipStream
 
 hipError_t launch_decode_append(const DecodeAppendLaunch& p, int head_dim, hipStream_t stream) {
   const int chunks = p.h_kv * (head_dim / 8);
-  const dim3 grid(p.batch, (chunks + 255) / 256), block(256);
+  const dim3 grid(p.batch, (chunks + 63) / 64), block(64);
   if (head_dim == 128) {
     hipLaunchKernelGGL(decode_append_kernel<128>, grid, block, 0, stream, p);
   } else {

@@ -9,10 +9,12 @@ namespace mocap {
 // Sequences of a batch and how their visible 64-key tiles are cut into items.
 // A sequence's tiles are those that hold a visible key, in order: the sinks'
 // tiles, then the window's.  With T the tiles of all sequences, a part has at
-// most max(min_tiles, ceil(T / target)) tiles, a sequence with c tiles is cut
-// evenly into ceil(c / that) parts (one, if it has none), and the items are the
-// parts of all sequences in order.  `items` bounds their number for any lengths:
-// sum ceil(c_b / part) <= T / part + batch <= target + batch.
+// most max(T / target + 1, few) tiles, where few is min_tiles, or down to
+// least_tiles when T / fill is less (when parts of min_tiles leave compute units
+// free); a sequence with c tiles is cut evenly into ceil(c / that) parts (one, if
+// it has none), and the items are the parts of all sequences in order.  `items`
+// bounds their number for any lengths: sum ceil(c_b / part) <= T / part + batch
+// <= target + batch.
 struct SeqBatch {
   const int32_t* tables;    // [batch][table_stride]
   const int32_t* seq_lens;  // [batch]
@@ -22,7 +24,9 @@ struct SeqBatch {
   int32_t window;           // 0: all keys
   int32_t sinks;            // 0 when window is 0
   int32_t target;
+  int32_t fill;
   int32_t min_tiles;
+  int32_t least_tiles;
   int32_t items;
   int32_t block_size;
   uint32_t block_magic;     // as in AttnLaunch

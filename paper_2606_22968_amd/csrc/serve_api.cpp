@@ -43,15 +43,24 @@ mocap_status check_heads(int32_t h_q, int32_t h_kv, int32_t head_dim) {
 
 // ---- Batches of sequences ----
 
-// How many workgroups a launch that reads a batch aims at per compute unit, and
-// the fewest tiles of a part.
-constexpr int kDecodeGroupsPerCu = 4;
-constexpr int kDecodeMinTiles = 8;
+// How a batch is cut (see SeqBatch).  More parts even out sequences of different
+// lengths and keep more loads in flight, fewer save their fixed work and the join.
+//   * At most about 5 workgroups per compute unit, for groups of more than 16 heads,
+//     which have one wavefront per SIMD, 3 (four sequences of up to 131072 tokens,
+//     64/8/128 heads: 294 us at 5, 302 at 8, 328 at 4; 60 of 9000, 32/1/128: 74 us at
+//     3, 87 at 5); 16 for key weights, whose parts need no join (16 sequences of up to
+//     32768 tokens: 135 us at 8, 130 at 16).
+//   * Parts of at least 8 tiles; of 16 where no sequence has more or they fill the
+//     device uncut (64 of 1024 tokens: 57 us cut, 49 uncut); down to 4 where parts of
+//     8 leave compute units without one (one of 2048 tokens: 17.0 and 13.7 us).
+constexpr int kDecodeGroupsPerCu = 5, kDecodeWideGroupsPerCu = 3, kDecodeWeightGroupsPerCu = 16;
+constexpr int kDecodeTiles = 8, kDecodeLeastTiles = 4, kDecodeUncutTiles = 16;
 constexpr int kDecodeHeads = 32;  // query heads of a workgroup, at most
 
-// Fills in how a batch's tiles are cut: per_item workgroups work on an item.
+// Fills in how a batch's tiles are cut: per_item workgroups work on an item; join:
+// parts are joined by a second launch.
 mocap_status plan_batch(int32_t batch, int64_t max_len, int64_t window, int64_t sinks, int64_t per_item,
-                        int32_t min_tiles, mocap::SeqBatch* s, bool* may_split) {
+                        int groups_per_cu, bool join, mocap::SeqBatch* s, bool* may_split) {
   int cus = 0;
   const mocap_status st = device_cu_count(&cus);
   if (st != MOCAP_OK) return st;
@@ -62,12 +71,16 @@ mocap_status plan_batch(int32_t batch, int64_t max_len, int64_t window, int64_t 
   s->max_len = (int32_t)max_len;
   s->window = (int32_t)window;
   s->sinks = (int32_t)(window > 0 ? std::min(sinks, max_len) : 0);
-  s->target = (int32_t)ceil_div((int64_t)cus * kDecodeGroupsPerCu, per_item);
-  s->min_tiles = min_tiles;
-  const int64_t items = std::min<int64_t>((int64_t)s->target + batch, batch * std::max<int64_t>(1, ceil_div(most, min_tiles)));
-  if (items * per_item > kMaxGroups) return MOCAP_ERR_UNSUPPORTED;
+  s->target = (int32_t)ceil_div((int64_t)cus * groups_per_cu, per_item);
+  s->fill = (int32_t)ceil_div(cus, per_item);
+  const bool uncut = join && (most <= kDecodeUncutTiles || (int64_t)batch * per_item >= 2 * cus);
+  s->min_tiles = uncut ? kDecodeUncutTiles : kDecodeTiles;
+  s->least_tiles = uncut ? kDecodeUncutTiles : kDecodeLeastTiles;
+  const int64_t items =
+      std::min<int64_t>((int64_t)s->target + batch, batch * std::max<int64_t>(1, ceil_div(most, s->least_tiles)));
+  if (items * per_item > kMaxGroups - 8 * per_item) return MOCAP_ERR_UNSUPPORTED;
   s->items = (int32_t)items;
-  *may_split = most > min_tiles;
+  *may_split = most > s->least_tiles;
   return MOCAP_OK;
 }
 
@@ -133,8 +146,9 @@ mocap_status plan_decode(int32_t batch, int64_t max_len, int32_t h_q, int32_t h_
   p->h_kv = h_kv;
   p->group = h_q / h_kv;
   p->row_blocks = (int32_t)ceil_div(p->group, p->group <= 16 ? 16 : kDecodeHeads);
-  if ((int64_t)batch * h_q > 2 * kMaxGroups) return MOCAP_ERR_UNSUPPORTED;
-  return plan_batch(batch, max_len, window, sinks, (int64_t)h_kv * p->row_blocks, kDecodeMinTiles, &p->seqs, &p->may_split);
+  if ((int64_t)batch * h_q > kMaxGroups) return MOCAP_ERR_UNSUPPORTED;
+  return plan_batch(batch, max_len, window, sinks, (int64_t)h_kv * p->row_blocks,
+                    p->group <= 16 ? kDecodeGroupsPerCu : kDecodeWideGroupsPerCu, true, &p->seqs, &p->may_split);
 }
 
 size_t decode_workspace(const mocap::DecodeAttnLaunch& p, int32_t head_dim) {
@@ -288,7 +302,7 @@ mocap_status mocap_decode_append(const mocap_kv_store* kv, const int32_t* block_
   const mocap_status st = check_batch(kv, block_tables, table_stride, seq_lens, batch, 0);
   if (st != MOCAP_OK || batch == 0) return st;
   if (!k || !v || !aligned16(k) || !aligned16(v)) return MOCAP_ERR_INVALID_ARG;
-  if (batch > kMaxGroups) return MOCAP_ERR_UNSUPPORTED;
+  if (batch > kMaxGroups || kv->h_kv > 65535 * 16) return MOCAP_ERR_UNSUPPORTED;
   MOCAP_DEBUG_CHECK_BATCH(kv, block_tables, table_stride, seq_lens, batch, (int64_t)table_stride * kv->block_size, 1, 0);
   mocap::DecodeAppendLaunch p;
   p.k = static_cast<const uint16_t*>(k);
@@ -469,7 +483,7 @@ mocap_status mocap_decode_key_weights(const mocap_kv_store* kv, const int32_t* b
     return MOCAP_ERR_INVALID_ARG;
   mocap::DecodeKeyWeightsLaunch p;
   bool may_split;
-  st = plan_batch(batch, max_len, 0, 0, h_kv, kDecodeMinTiles, &p.seqs, &may_split);
+  st = plan_batch(batch, max_len, 0, 0, h_kv, kDecodeWeightGroupsPerCu, false, &p.seqs, &may_split);
   if (st != MOCAP_OK) return st;
   MOCAP_DEBUG_CHECK_BATCH(kv, block_tables, table_stride, seq_lens, batch, max_len, 0, 0);
   set_tables(kv, block_tables, table_stride, seq_lens, &p.seqs);

@@ -47,8 +47,9 @@ hipError_t hipDeviceGetAttribute(int* value, hipDeviceAttribute_t, int) {
 int record_launches() { return launches; }
 // How the last batch is cut.
 void record_batch(int* out) {
-  const int v[] = {seqs.target, seqs.min_tiles, seqs.items, seqs.window, seqs.sinks, seqs.max_len};
-  for (int i = 0; i < 6; ++i) out[i] = v[i];
+  const int v[] = {seqs.target, seqs.fill,  seqs.min_tiles, seqs.least_tiles,
+                   seqs.items,  seqs.window, seqs.sinks,    seqs.max_len};
+  for (int i = 0; i < 8; ++i) out[i] = v[i];
 }
 void record_window(int* out) {
   const int v[] = {window.row_blocks, window.n_ranges, window.total_wgs, window.window, window.sinks};

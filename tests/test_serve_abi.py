@@ -212,7 +212,7 @@ def test_items_hold_any_lengths(host):
     split that the plan rules out never happens."""
     rng = random.Random(5)
     for _ in range(400):
-        batch = rng.choice((1, 2, 3, 17, 64, 65, 200))
+        batch = rng.choice((1, 2, 3, 17, 64, 65, 200, 600))
         h_kv = rng.choice((1, 2, 8))
         group = rng.choice((1, 4, 16, 20, 64))
         max_len = rng.choice((0, 1, 64, 512, 513, 3000, 20000))
@@ -220,9 +220,9 @@ def test_items_hold_any_lengths(host):
         kv = store(h_kv=h_kv)
         assert decode(host, kv=kv, stride=100, batch=batch, max_len=max_len, h_q=h_kv * group, h_kv=h_kv, window=win,
                       sinks=sinks) == 0
-        out = (ctypes.c_int * 6)()
+        out = (ctypes.c_int * 8)()
         host.record_batch(out)
-        target, min_tiles, items, w, s, _ = out
+        target, fill, min_tiles, least, items, w, s, _ = out
         assert (w, s) == ((0, 0) if win == 0 or win >= max_len else (win, min(sinks, max_len)))
         size = ctypes.c_size_t(0)
         assert host.mocap_decode_attn_workspace_size(batch, max_len, h_kv * group, h_kv, 128, win, sinks,
@@ -230,7 +230,8 @@ def test_items_hold_any_lengths(host):
         for lens in ([max_len] * batch, [0] * batch, [1] * (batch - 1) + [max_len],
                      [rng.randint(0, max_len) for _ in range(batch)]):
             counts = [tiles_of(n, w, s) for n in lens]
-            per = max(min_tiles, -(-sum(counts) // target))
+            total = sum(counts)
+            per = max(min(min_tiles, max(least, total // fill + 1)), total // target + 1)
             parts = [max(1, -(-c // per)) for c in counts]
             assert sum(parts) <= items
             assert size.value > 0 or max(parts) == 1
