@@ -330,81 +330,190 @@ __global__ __launch_bounds__(256) void key_weights_join_kernel(const KeyWeightsL
   p.weights[at] = (p.prev != nullptr && key < p.prefix_len ? p.prev[at] : 0.f) + w;
 }
 
-// ---- One row per sequence ----
-// Bound by HBM (every key once).  A wavefront takes 64 keys at a time, all of
-// them in flight, in registers: S = Q K^T with v_mfma_f32_16x16x32_bf16, 16 query
-// heads by 16 keys, so lane l holds key l % 16 and four heads of each product;
-// groups of more heads go through the same keys 16 at a time.
-constexpr int kDecodeWaves = 4;
+// ---- Few rows ----
+// One row per sequence of a batch, or a chunk of few rows.  Bound by HBM: every key
+// once.  A workgroup keeps up to 128 rows in LDS, as the A operands of their
+// products; a wavefront takes 64 keys at a time, all of them in flight, straight
+// from the store in registers: S = Q K^T with v_mfma_f32_16x16x32_bf16, 16 rows by 16
+// keys, so lane l holds key l % 16 and four rows of each product.
+constexpr int kFewWaves = 4;
+constexpr int kFewBlock = 128;  // rows kept at a time
 
+struct FewRows {
+  const uint16_t* q;       // row r of the group: token r / G, head r % G
+  const uint16_t* k_pool;
+  const float* lse;        // of head h, token t: lse[h lse_head + t]
+  const float* prev;       // of the KV head, or null
+  float* weights;
+  const_i32_ptr table;
+  int64_t lse_head;
+  int rows, group, h_q, h_kv, kv_head, block_size, len, prefix;
+  uint32_t block_magic, group_magic;
+  int block_shift, group_shift;
+  float scale_log2;
+};
+
+// The weights of the keys of tiles begin, begin + 1, .. end - 1.
 template <int D>
-__global__ __launch_bounds__(64 * kDecodeWaves) void decode_key_weights_kernel(const DecodeKeyWeightsLaunch p) {
-#if defined(__HIP_DEVICE_COMPILE__)
+__device__ __forceinline__ void few_rows(const FewRows& x, int begin, int end) {
   constexpr int KS = D / 32;
-  const int tid = threadIdx.x;
-  const int lane = tid & 63;
+  __shared__ __attribute__((aligned(16))) u32x4 rows_q[kFewBlock / 16 * KS * 64];  // [16 rows][k-step][lane]
+  __shared__ __attribute__((aligned(16))) float rows_l2[kFewBlock];
+  const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g4 = lane >> 4;
-  const int item = blockIdx.x / p.h_kv;
-  const int kv_head = blockIdx.x - item * p.h_kv;
-  const SeqPart x = locate_item(p.seqs, lane, item);
-  if (x.seq == p.seqs.batch) return;
-  int begin, end;
-  part_range(x, &begin, &end);
-
-  const const_i32_ptr table = (const_i32_ptr)(p.seqs.tables + x.seq * p.seqs.table_stride);
-  const int bs = p.seqs.block_size;
-  const int64_t q0 = (int64_t)x.seq * p.h_q + kv_head * p.group;
-  const int64_t w0 = ((int64_t)x.seq * p.h_kv + kv_head) * p.weight_stride;
-  const float sl2 = p.scale_log2;
-  for (int t = begin + wave; t < end; t += kDecodeWaves) {
-    const int pos = t * kTileKeys;
-    const int lb = (int)div_by((uint32_t)pos, p.seqs.block_magic, p.seqs.block_shift);
-    const int64_t slot = pos - lb * bs;
-    const uint16_t* k = p.k_pool + (((int64_t)table[lb] * p.h_kv + kv_head) * bs + slot + l16) * D + g4 * 8;
-    bf16x8 kf[4][KS];
+  // Row r sees key j if r >= (j - prefix) G.
+  auto first_row = [&](int j) { return (int)min((int64_t)max(j - x.prefix, 0) * x.group, (int64_t)x.rows); };
+  for (int block = 0; block < x.rows; block += kFewBlock) {
+    const int count = min(kFewBlock, x.rows - block), tiles16 = (count + 15) / 16;
+    if (block > 0) __syncthreads();
+    for (int i = tid; i < tiles16 * KS * 64; i += 64 * kFewWaves) {
+      // Rows past the last take it, with an LSE of +infinity (a weight of 0).
+      const int r = min(block + i / (KS * 64) * 16 + (i & 15), x.rows - 1);
+      const int token = (int)div_by((uint32_t)r, x.group_magic, x.group_shift);
+      const int dim = i / 64 % KS * 32 + (i >> 4 & 3) * 8;
+      rows_q[i] = *reinterpret_cast<const u32x4*>(x.q + ((int64_t)token * x.h_q + r - token * x.group) * D + dim);
+    }
+    if (tid < kFewBlock) {
+      const int r = min(block + tid, x.rows - 1);
+      const int token = (int)div_by((uint32_t)r, x.group_magic, x.group_shift);
+      const float v = x.lse[(r - token * x.group) * x.lse_head + token];
+      rows_l2[tid] = tid < count && v != -INFINITY ? v * kLog2e : INFINITY;
+    }
+    __syncthreads();
+    for (int t = begin + wave; t < end; t += kFewWaves) {
+      const int pos = t * kTileKeys;
+      const int lb = (int)div_by((uint32_t)pos, x.block_magic, x.block_shift);
+      const int64_t slot = pos - lb * x.block_size;
+      const uint16_t* k =
+          x.k_pool + (((int64_t)x.table[lb] * x.h_kv + x.kv_head) * x.block_size + slot + l16) * D + g4 * 8;
+      bf16x8 kf[4][KS];
 #pragma unroll
-    for (int b = 0; b < 4; ++b)
+      for (int b = 0; b < 4; ++b)
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) kf[b][ks] = *reinterpret_cast<const bf16x8*>(k + b * 16 * D + ks * 32);
-    const int key = pos + lane;
-    const bool live = key < x.span.len;
-    const float old = live && p.prev != nullptr && key < x.span.len - 1 ? p.prev[w0 + key] : 0.f;
-    float w = 0.f;  // of key pos + lane
-    for (int h0 = 0; h0 < p.group; h0 += 16) {
-      const uint16_t* q = p.q + (q0 + min(h0 + l16, p.group - 1)) * D + g4 * 8;
-      bf16x8 qf[KS];
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(q + ks * 32);
-      float l2[4];  // of heads h0 + 4 g4 + e
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int head = h0 + g4 * 4 + e;
-        const float v = p.lse[q0 + min(head, p.group - 1)];
-        l2[e] = head < p.group && v != -INFINITY ? v * kLog2e : INFINITY;
+        for (int ks = 0; ks < KS; ++ks) kf[b][ks] = *reinterpret_cast<const bf16x8*>(k + b * 16 * D + ks * 32);
+      const int key = pos + lane;
+      // What the key had: from former queries, then from the rows before this block.
+      float old = 0.f;
+      if (block > 0) {
+        old = key < x.len ? x.weights[key] : 0.f;
+      } else if (x.prev != nullptr) {
+        old = key < x.prefix ? x.prev[key] : 0.f;
       }
+      float w[4] = {0.f, 0.f, 0.f, 0.f};  // of key pos + 16 b + l16, from this lane's rows
+      // Rows that see no key of the tile are left out; those from `full` on see all.
+      const int from = max(0, first_row(pos) - block) / 16, full = first_row(pos + kTileKeys - 1) - block;
+      for (int rt = from; rt < tiles16; ++rt) {
+        bf16x8 qf[KS];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) qf[ks] = __builtin_bit_cast(bf16x8, rows_q[(rt * KS + ks) * 64 + lane]);
+        const f32x4 l2 = *reinterpret_cast<const f32x4*>(&rows_l2[rt * 16 + g4 * 4]);
+        const bool masked = rt * 16 < full || rt * 16 + 16 > count;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          f32x4 s = f32x4{};
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[ks], kf[b][ks], s, 0, 0, 0);
+          f32x4 v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = __builtin_amdgcn_exp2f(fmaf(s[e], x.scale_log2, -l2[e]));
+          if (masked) {
+            const int seen_from = first_row(pos + b * 16 + l16) - block;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int r = rt * 16 + g4 * 4 + e;
+              v[e] = r >= seen_from && r < count ? v[e] : 0.f;
+            }
+          }
+          w[b] += (v[0] + v[1]) + (v[2] + v[3]);
+        }
+      }
+      float total = 0.f;  // of key pos + lane
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
-        f32x4 s = f32x4{};
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[ks], kf[b][ks], s, 0, 0, 0);
-        float sum = 0.f;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float v = __builtin_amdgcn_exp2f(fmaf(s[e], sl2, -l2[e]));
-          sum += h0 + g4 * 4 + e < p.group ? v : 0.f;
-        }
-        sum = quad_rows_sum(sum);
-        w += g4 == b ? sum : 0.f;
+        const float sum = quad_rows_sum(w[b]);
+        total = g4 == b ? sum : total;
       }
+      if (key < x.len) x.weights[key] = old + total;
     }
-    if (live) p.weights[w0 + key] = old + w;
   }
+}
+
+template <int D>
+__global__ __launch_bounds__(64 * kFewWaves) void decode_key_weights_kernel(const DecodeKeyWeightsLaunch p) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const int item = blockIdx.x / p.h_kv;
+  const int kv_head = blockIdx.x - item * p.h_kv;
+  const SeqPart w = locate_item(p.seqs, threadIdx.x & 63, item);
+  if (w.seq == p.seqs.batch) return;
+  int begin, end;
+  part_range(w, &begin, &end);
+  const int64_t row0 = (int64_t)w.seq * p.h_q + kv_head * p.group;
+  const int64_t at = ((int64_t)w.seq * p.h_kv + kv_head) * p.weight_stride;
+  FewRows x;
+  x.q = p.q + row0 * D;
+  x.k_pool = p.k_pool;
+  x.lse = p.lse + row0;
+  x.prev = p.prev != nullptr ? p.prev + at : nullptr;
+  x.weights = p.weights + at;
+  x.table = (const_i32_ptr)(p.seqs.tables + w.seq * p.seqs.table_stride);
+  x.lse_head = 1;
+  x.rows = x.group = p.group;
+  x.h_q = p.h_q;
+  x.h_kv = p.h_kv;
+  x.kv_head = kv_head;
+  x.block_size = p.seqs.block_size;
+  x.len = w.span.len;
+  x.prefix = w.span.len - 1;
+  x.block_magic = p.seqs.block_magic;
+  x.block_shift = p.seqs.block_shift;
+  x.group_magic = p.group_magic;
+  x.group_shift = p.group_shift;
+  x.scale_log2 = p.scale_log2;
+  few_rows<D>(x, begin, end);
+#endif  // __HIP_DEVICE_COMPILE__
+}
+
+// A chunk of few rows: key_blocks workgroups per KV head take even runs of tiles.
+template <int D>
+__global__ __launch_bounds__(64 * kFewWaves) void few_key_weights_kernel(const KeyWeightsLaunch p) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const int part = blockIdx.x / p.h_kv;
+  const int kv_head = blockIdx.x - part * p.h_kv;
+  const int n = p.prefix_len + p.chunk_len, tiles = (n + kTileKeys - 1) / kTileKeys;
+  const int begin = (int)((int64_t)tiles * part / p.key_blocks), end = (int)((int64_t)tiles * (part + 1) / p.key_blocks);
+  FewRows x;
+  x.q = p.q + (int64_t)kv_head * p.group * D;
+  x.k_pool = p.k_pool;
+  x.lse = p.lse + (int64_t)kv_head * p.group * p.chunk_len;
+  x.prev = p.prev != nullptr ? p.prev + kv_head * p.weight_stride : nullptr;
+  x.weights = p.weights + kv_head * p.weight_stride;
+  x.table = (const_i32_ptr)p.table;
+  x.lse_head = p.chunk_len;
+  x.rows = p.chunk_len * p.group;
+  x.group = p.group;
+  x.h_q = p.h_q;
+  x.h_kv = p.h_kv;
+  x.kv_head = kv_head;
+  x.block_size = p.block_size;
+  x.len = n;
+  x.prefix = p.prefix_len;
+  x.block_magic = p.block_magic;
+  x.block_shift = p.block_shift;
+  x.group_magic = p.group_magic;
+  x.group_shift = p.group_shift;
+  x.scale_log2 = p.scale_log2;
+  few_rows<D>(x, begin, end);
 #endif  // __HIP_DEVICE_COMPILE__
 }
 
 template <int D>
 void launch(const KeyWeightsLaunch& p, hipStream_t stream) {
+  if (p.few) {
+    hipLaunchKernelGGL((few_key_weights_kernel<D>), dim3((unsigned)((int64_t)p.key_blocks * p.h_kv)),
+                       dim3(64 * kFewWaves), 0, stream, p);
+    return;
+  }
   const dim3 grid((unsigned)((int64_t)p.key_blocks * p.row_parts * p.h_kv)), block(64 * kWeightWaves);
   hipLaunchKernelGGL((key_weights_kernel<D>), grid, block, 0, stream, p);
   if (p.row_parts > 1) {
@@ -425,7 +534,7 @@ hipError_t launch_key_weights(const KeyWeightsLaunch& p, int head_dim, hipStream
 }
 
 hipError_t launch_decode_key_weights(const DecodeKeyWeightsLaunch& p, int head_dim, hipStream_t stream) {
-  const dim3 grid((unsigned)((int64_t)p.seqs.items * p.h_kv)), block(64 * kDecodeWaves);
+  const dim3 grid((unsigned)((int64_t)p.seqs.items * p.h_kv)), block(64 * kFewWaves);
   if (head_dim == 128) {
     hipLaunchKernelGGL(decode_key_weights_kernel<128>, grid, block, 0, stream, p);
   } else {

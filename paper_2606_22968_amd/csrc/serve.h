@@ -118,7 +118,8 @@ struct KeyWeightsLaunch {
   int32_t block_size;
   uint32_t block_magic;
   int32_t block_shift;
-  int32_t key_blocks;       // ceil((P + L) / 512)
+  bool few;                 // the kernel for few rows
+  int32_t key_blocks;       // ceil((P + L) / 512); few: workgroups of a KV head
   int32_t row_parts;
   float scale_log2;
 };
@@ -134,6 +135,8 @@ struct DecodeKeyWeightsLaunch {
   int32_t h_q;
   int32_t h_kv;
   int32_t group;
+  uint32_t group_magic;
+  int32_t group_shift;
   float scale_log2;
 };
 

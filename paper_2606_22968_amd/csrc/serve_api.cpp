@@ -219,6 +219,9 @@ size_t window_workspace(const mocap::WindowLaunch& p, int32_t head_dim) {
 // A row tile (32 rows by 512 keys), fixed work of a workgroup, and the join of row
 // parts; the fewest tiles of a part.
 constexpr double kWeightTileUs128 = 0.75, kWeightTileUs64 = 0.55, kWeightGroupUs = 4.0, kWeightJoinUs = 4.0;
+// Up to this many rows the keys stream past the rows instead: 65501 keys of 8 heads
+// of 128, 4, 64, 128 and 256 rows: 24, 27, 33 and 60 us, and 33, 37, 41 and 58.
+constexpr int64_t kWeightFewRows = 128, kWeightFewGroupsPerCu = 4;
 constexpr int64_t kWeightMinTiles = 4, kWeightMaxParts = 64, kWeightMaxRounds = 4;
 
 mocap_status plan_weights(int64_t prefix_len, int32_t chunk_len, int32_t h_q, int32_t h_kv, int32_t head_dim,
@@ -234,6 +237,13 @@ mocap_status plan_weights(int64_t prefix_len, int32_t chunk_len, int32_t h_q, in
   p->h_kv = h_kv;
   p->group = (int32_t)group;
   block_divider((uint32_t)group, &p->group_magic, &p->group_shift);
+  p->few = rows <= kWeightFewRows;
+  if (p->few) {
+    // Every wavefront a tile at least; about four workgroups per compute unit.
+    p->key_blocks = (int32_t)std::min(ceil_div(n, 4 * kTileKeys), ceil_div((int64_t)cus * kWeightFewGroupsPerCu, h_kv));
+    p->row_parts = 1;
+    return (int64_t)p->key_blocks * h_kv > kMaxGroups ? MOCAP_ERR_UNSUPPORTED : MOCAP_OK;
+  }
   const int64_t block_keys = mocap::kWeightKeys * mocap::kWeightWaves;
   p->key_blocks = (int32_t)ceil_div(n, block_keys);
   // Parts: one workgroup per compute unit at a time, a round costs its longest
@@ -496,6 +506,7 @@ mocap_status mocap_decode_key_weights(const mocap_kv_store* kv, const int32_t* b
   p.h_q = h_q;
   p.h_kv = h_kv;
   p.group = h_q / h_kv;
+  block_divider((uint32_t)p.group, &p.group_magic, &p.group_shift);
   p.scale_log2 = (float)((double)scale * 1.4426950408889634);
   return mocap::launch_decode_key_weights(p, head_dim, static_cast<hipStream_t>(stream)) == hipSuccess ? MOCAP_OK
                                                                                                        : MOCAP_ERR_HIP;

@@ -56,8 +56,8 @@ void record_window(int* out) {
   for (int i = 0; i < 5; ++i) out[i] = v[i];
 }
 void record_weights(int* out) {
-  const int v[] = {weights.key_blocks, weights.row_parts};
-  for (int i = 0; i < 2; ++i) out[i] = v[i];
+  const int v[] = {weights.few, weights.key_blocks, weights.row_parts};
+  for (int i = 0; i < 3; ++i) out[i] = v[i];
 }
 
 }  // extern "C"

@@ -262,12 +262,16 @@ def test_window_ranges(host):
 
 
 def test_key_weight_blocks(host):
-    for P, L, h_kv in ((0, 1, 8), (0, 2048, 8), (30720, 2048, 8), (1 << 20, 1, 1), (100, 3, 1), (5000, 64, 2)):
+    for P, L, h_kv in ((0, 1, 8), (0, 2048, 8), (30720, 2048, 8), (1 << 20, 1, 1), (100, 3, 1), (5000, 64, 2), (5000, 32, 2), (5000, 33, 2)):
         kv = store(h_kv=h_kv, block_size=1 << 16)
         assert weights(host, kv=kv, P=P, L=L, h_q=4 * h_kv, h_kv=h_kv, stride=1 << 22, n_table=1 << 10) == 0
-        out = (ctypes.c_int * 2)()
+        out = (ctypes.c_int * 3)()
         host.record_weights(out)
-        key_blocks, parts = out
+        few, key_blocks, parts = out
+        assert few == (4 * L <= 128)
+        if few:
+            assert parts == 1 and 1 <= key_blocks <= -(-(P + L) // 64)
+            continue
         assert key_blocks * 512 >= P + L > (key_blocks - 1) * 512
         size = ctypes.c_size_t(0)
         assert host.mocap_key_weights_workspace_size(P, L, 4 * h_kv, h_kv, 128, ctypes.byref(size)) == 0
