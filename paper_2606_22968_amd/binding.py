@@ -541,54 +541,71 @@ def mocap_lbcp_refine_e2e(seq_len: int, num_chunks: int, num_stages: int, align:
 
 # ---- After the prefill (mocap_serve.h) ----
 
-def _workspace(workspace: Optional[torch.Tensor]):
+def _need(t: torch.Tensor, dtype, name: str, ndim: Optional[int], device: int) -> int:
+    """The address of a contiguous tensor of this type on the current device, where the call enqueues its work."""
+    if type(t) is torch.Tensor and t.dtype is dtype and t.get_device() == device and t.is_contiguous() and \
+            (ndim is None or t.dim() == ndim):
+        return t.data_ptr()
+    _require(t, dtype, name, ndim)
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}, but the current device is cuda:{device}")
+    return t.data_ptr()
+
+
+def _workspace(workspace: Optional[torch.Tensor], device: int):
     if workspace is None:
         return None, 0
-    _require(workspace, workspace.dtype if isinstance(workspace, torch.Tensor) else None, "workspace")
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    if not isinstance(workspace, torch.Tensor):
+        raise TypeError("workspace must be a torch.Tensor")
+    return _need(workspace, workspace.dtype, "workspace", None, device), workspace.numel() * workspace.element_size()
 
 
-def _one_device(*tensors) -> None:
-    """Every tensor on the current device, where the call enqueues its work."""
-    device = _raw_device()
-    for t in tensors:
-        if t is not None and t.device.index != device:
-            raise ValueError(f"a tensor on {t.device}, but the current device is cuda:{device}")
+def _stream_on(stream, device: int) -> Optional[int]:
+    """The handle of `stream`, or of the current stream, which must be the current device's."""
+    if stream is None:
+        return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
+    if stream.device.index != device:
+        raise ValueError(f"the stream is on {stream.device}, but the current device is cuda:{device}")
+    return stream.cuda_stream
 
 
-def _batch(store: KvStore, block_tables: torch.Tensor, seq_lens: torch.Tensor, max_len: Optional[int], window: int = 0,
-           sinks: int = 0) -> int:
-    """Checks a batch's tables and lengths; returns max_len."""
-    _require(block_tables, torch.int32, "block_tables", 2)
-    _require(seq_lens, torch.int32, "seq_lens", 1)
-    if block_tables.shape[0] != seq_lens.shape[0]:
+def _store_on(store: KvStore, device: int) -> mocap_kv_store:
+    """The store's descriptor, of pools on the current device."""
+    _need(store.k_pool, torch.bfloat16, "k_pool", 4, device)
+    _need(store.v_pool, torch.bfloat16, "v_pool", 4, device)
+    return store.descriptor()
+
+
+def _batch(store: KvStore, block_tables: torch.Tensor, seq_lens: torch.Tensor, max_len: Optional[int], device: int,
+           window: int = 0, sinks: int = 0):
+    """Checks a batch's tables and lengths; returns their addresses, batch, table_stride and max_len."""
+    tables_ptr = _need(block_tables, torch.int32, "block_tables", 2, device)
+    lens_ptr = _need(seq_lens, torch.int32, "seq_lens", 1, device)
+    batch, stride = block_tables.shape
+    if seq_lens.shape[0] != batch:
         raise ValueError("block_tables must be [batch][table_stride] and seq_lens [batch]")
-    _one_device(store.k_pool, store.v_pool, block_tables, seq_lens)
-    capacity = block_tables.shape[1] * store.block_size
-    max_len = min(capacity, (1 << 31) - 128) if max_len is None else int(max_len)
+    max_len = min(stride * store.block_size, (1 << 31) - 128) if max_len is None else int(max_len)
     if _check_tables:
         for table, n in zip(block_tables.cpu(), seq_lens.tolist()):
             n = min(n, max_len)
             low = max(0, n - window) if window > 0 else 0
             mocap_check_block_table(table, 0, max(0, min(sinks, low)), store.block_size, store.num_blocks)
             mocap_check_block_table(table, low, max(low, n), store.block_size, store.num_blocks)
-    return max_len
+    return tables_ptr, lens_ptr, batch, stride, max_len
 
 
 def mocap_decode_append(store: KvStore, block_tables: torch.Tensor, seq_lens: torch.Tensor, k: torch.Tensor,
                         v: torch.Tensor, stream=None) -> None:
     """Stores row b of k and v (bf16 [batch][h_kv][head_dim]) at position seq_lens[b] - 1 of sequence b."""
-    _batch(store, block_tables, seq_lens, None)
-    batch = seq_lens.shape[0]
-    for name, t in (("k", k), ("v", v)):
-        _require(t, torch.bfloat16, name, 3)
-        if tuple(t.shape) != (batch, store.h_kv, store.head_dim):
-            raise ValueError("k/v must be [batch][h_kv][head_dim] of the store")
-    _one_device(k, v)
-    desc = store.descriptor()
-    _check(load_library().mocap_decode_append(
-        ctypes.byref(desc), block_tables.data_ptr(), block_tables.shape[1], seq_lens.data_ptr(), batch, k.data_ptr(),
-        v.data_ptr(), _stream_handle(stream)), "mocap_decode_append")
+    device = _raw_device()
+    tables_ptr, lens_ptr, batch, stride, _ = _batch(store, block_tables, seq_lens, None, device)
+    k_ptr = _need(k, torch.bfloat16, "k", 3, device)
+    v_ptr = _need(v, torch.bfloat16, "v", 3, device)
+    if k.shape != v.shape or k.shape != (batch, store.h_kv, store.head_dim):
+        raise ValueError("k/v must be [batch][h_kv][head_dim] of the store")
+    desc = _store_on(store, device)
+    _check(load_library().mocap_decode_append(ctypes.byref(desc), tables_ptr, stride, lens_ptr, batch, k_ptr, v_ptr,
+                                              _stream_on(stream, device)), "mocap_decode_append")
 
 
 def mocap_decode_attn_workspace_size(batch: int, h_q: int, h_kv: int, head_dim: int, max_len: int, window: int = 0,
@@ -604,20 +621,20 @@ def mocap_decode_attn(store: KvStore, block_tables: torch.Tensor, seq_lens: torc
                       max_len: Optional[int], scale: float, o: torch.Tensor, lse: torch.Tensor,
                       workspace: Optional[torch.Tensor] = None, window: int = 0, sinks: int = 0, stream=None) -> None:
     """q, o: bf16 [batch][h_q][head_dim]; lse: fp32 [batch][h_q]; max_len None: what the tables hold."""
-    max_len = _batch(store, block_tables, seq_lens, max_len, int(window), int(sinks))
-    _require(q, torch.bfloat16, "q", 3)
-    _require(o, torch.bfloat16, "o", 3)
-    _require(lse, torch.float32, "lse", 2)
-    batch, h_q, head_dim = q.shape
-    if batch != seq_lens.shape[0] or o.shape != q.shape or tuple(lse.shape) != (batch, h_q):
+    device = _raw_device()
+    window, sinks = int(window), int(sinks)
+    tables_ptr, lens_ptr, batch, stride, max_len = _batch(store, block_tables, seq_lens, max_len, device, window, sinks)
+    q_ptr = _need(q, torch.bfloat16, "q", 3, device)
+    o_ptr = _need(o, torch.bfloat16, "o", 3, device)
+    lse_ptr = _need(lse, torch.float32, "lse", 2, device)
+    rows, h_q, head_dim = q.shape
+    if rows != batch or o.shape != q.shape or lse.shape != (batch, h_q):
         raise ValueError("q and o must be [batch][h_q][head_dim] and lse [batch][h_q]")
-    _one_device(q, o, lse, workspace)
-    ws_ptr, ws_bytes = _workspace(workspace)
-    desc = store.descriptor()
+    ws_ptr, ws_bytes = _workspace(workspace, device)
+    desc = _store_on(store, device)
     _check(load_library().mocap_decode_attn(
-        ctypes.byref(desc), block_tables.data_ptr(), block_tables.shape[1], seq_lens.data_ptr(), batch, max_len,
-        q.data_ptr(), h_q, store.h_kv, head_dim, float(scale), int(window), int(sinks), o.data_ptr(), lse.data_ptr(),
-        ws_ptr, ws_bytes, _stream_handle(stream)), "mocap_decode_attn")
+        ctypes.byref(desc), tables_ptr, stride, lens_ptr, batch, max_len, q_ptr, h_q, store.h_kv, head_dim, scale, window,
+        sinks, o_ptr, lse_ptr, ws_ptr, ws_bytes, _stream_on(stream, device)), "mocap_decode_attn")
 
 
 def mocap_window_attn_workspace_size(prefix_len: int, chunk_len: int, h_q: int, h_kv: int, head_dim: int, window: int,
@@ -635,23 +652,24 @@ def mocap_window_attn(store: KvStore, block_table: torch.Tensor, q: torch.Tensor
                       window: int, sinks: int, o: torch.Tensor, lse: torch.Tensor,
                       workspace: Optional[torch.Tensor] = None, num_splits: int = 0, stream=None) -> None:
     """As mocap_chunk_attn, each row seeing its last `window` positions and the first `sinks`."""
-    _require(block_table, torch.int32, "block_table", 1)
-    _require(q, torch.bfloat16, "q", 3)
-    _require(o, torch.bfloat16, "o", 3)
-    _require(lse, torch.float32, "lse", 2)
+    device = _raw_device()
+    table_ptr = _need(block_table, torch.int32, "block_table", 1, device)
+    q_ptr = _need(q, torch.bfloat16, "q", 3, device)
+    o_ptr = _need(o, torch.bfloat16, "o", 3, device)
+    lse_ptr = _need(lse, torch.float32, "lse", 2, device)
     chunk_len, h_q, head_dim = q.shape
-    if o.shape != q.shape or tuple(lse.shape) != (h_q, chunk_len):
+    if o.shape != q.shape or lse.shape != (h_q, chunk_len):
         raise ValueError("o must match q and lse must be [h_q][chunk_len]")
-    _one_device(store.k_pool, store.v_pool, block_table, q, o, lse, workspace)
-    ws_ptr, ws_bytes = _workspace(workspace)
-    end = int(prefix_len) + chunk_len
-    _maybe_check(store, block_table, 0, min(int(sinks), end))
-    _maybe_check(store, block_table, max(0, int(prefix_len) - int(window) + 1), end)
-    desc = store.descriptor()
+    ws_ptr, ws_bytes = _workspace(workspace, device)
+    prefix_len, window, sinks = int(prefix_len), int(window), int(sinks)
+    end = prefix_len + chunk_len
+    _maybe_check(store, block_table, 0, min(sinks, end))
+    _maybe_check(store, block_table, max(0, prefix_len - window + 1), end)
+    desc = _store_on(store, device)
     _check(load_library().mocap_window_attn(
-        ctypes.byref(desc), block_table.data_ptr(), block_table.numel(), q.data_ptr(), int(prefix_len), chunk_len, h_q,
-        store.h_kv, head_dim, float(scale), int(window), int(sinks), o.data_ptr(), lse.data_ptr(), ws_ptr, ws_bytes,
-        int(num_splits), _stream_handle(stream)), "mocap_window_attn")
+        ctypes.byref(desc), table_ptr, block_table.shape[0], q_ptr, prefix_len, chunk_len, h_q, store.h_kv, head_dim,
+        scale, window, sinks, o_ptr, lse_ptr, ws_ptr, ws_bytes, int(num_splits), _stream_on(stream, device)),
+        "mocap_window_attn")
 
 
 def mocap_key_weights_workspace_size(prefix_len: int, chunk_len: int, h_q: int, h_kv: int, head_dim: int) -> int:
@@ -662,18 +680,21 @@ def mocap_key_weights_workspace_size(prefix_len: int, chunk_len: int, h_q: int, 
     return nbytes.value
 
 
-def _same_or_apart(prev: Optional[torch.Tensor], weights: torch.Tensor, ndim: int) -> Optional[int]:
-    """prev's address; prev must be weights' memory exactly, or none of it."""
-    _require(weights, torch.float32, "weights", ndim)
+def _weights(prev: Optional[torch.Tensor], weights: torch.Tensor, shape: tuple, device: int):
+    """The addresses of prev (or None) and weights, [*shape][stride] both; prev must be weights' memory exactly, or
+    none of it."""
+    w_ptr = _need(weights, torch.float32, "weights", len(shape) + 1, device)
+    if weights.shape[:-1] != shape:
+        raise ValueError(f"weights must be [{']['.join(map(str, shape))}][stride]")
     if prev is None:
-        return None
-    _require(prev, torch.float32, "prev", ndim)
+        return None, w_ptr
+    p_ptr = _need(prev, torch.float32, "prev", len(shape) + 1, device)
     if prev.shape != weights.shape:
         raise ValueError("prev must have the shape of weights")
-    a, b, n = prev.data_ptr(), weights.data_ptr(), 4 * weights.numel()
-    if a != b and a < b + n and b < a + n:
+    size = 4 * weights.numel()
+    if p_ptr != w_ptr and p_ptr < w_ptr + size and w_ptr < p_ptr + size:
         raise ValueError("prev must be weights itself or not overlap it")
-    return a
+    return p_ptr, w_ptr
 
 
 def mocap_key_weights(store: KvStore, block_table: torch.Tensor, q: torch.Tensor, prefix_len: int, scale: float,
@@ -681,23 +702,21 @@ def mocap_key_weights(store: KvStore, block_table: torch.Tensor, q: torch.Tensor
                       workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """q: bf16 [chunk_len][h_q][head_dim]; lse: fp32 [h_q][chunk_len]; prev, weights: fp32 [h_kv][stride], stride at
     least prefix_len + chunk_len."""
-    _require(block_table, torch.int32, "block_table", 1)
-    _require(q, torch.bfloat16, "q", 3)
-    _require(lse, torch.float32, "lse", 2)
+    device = _raw_device()
+    table_ptr = _need(block_table, torch.int32, "block_table", 1, device)
+    q_ptr = _need(q, torch.bfloat16, "q", 3, device)
+    lse_ptr = _need(lse, torch.float32, "lse", 2, device)
     chunk_len, h_q, head_dim = q.shape
-    if tuple(lse.shape) != (h_q, chunk_len):
+    if lse.shape != (h_q, chunk_len):
         raise ValueError("lse must be [h_q][chunk_len]")
-    prev_ptr = _same_or_apart(prev, weights, 2)
-    if weights.shape[0] != store.h_kv:
-        raise ValueError("weights must be [h_kv][stride]")
-    _one_device(store.k_pool, store.v_pool, block_table, q, lse, prev, weights, workspace)
-    ws_ptr, ws_bytes = _workspace(workspace)
+    prev_ptr, w_ptr = _weights(prev, weights, (store.h_kv,), device)
+    ws_ptr, ws_bytes = _workspace(workspace, device)
     _maybe_check(store, block_table, 0, int(prefix_len) + chunk_len)
-    desc = store.descriptor()
+    desc = _store_on(store, device)
     _check(load_library().mocap_key_weights(
-        ctypes.byref(desc), block_table.data_ptr(), block_table.numel(), q.data_ptr(), int(prefix_len), chunk_len, h_q,
-        store.h_kv, head_dim, float(scale), lse.data_ptr(), prev_ptr, weights.data_ptr(), weights.shape[1], ws_ptr,
-        ws_bytes, _stream_handle(stream)), "mocap_key_weights")
+        ctypes.byref(desc), table_ptr, block_table.shape[0], q_ptr, int(prefix_len), chunk_len, h_q, store.h_kv,
+        head_dim, scale, lse_ptr, prev_ptr, w_ptr, weights.shape[1], ws_ptr, ws_bytes, _stream_on(stream, device)),
+        "mocap_key_weights")
 
 
 def mocap_decode_key_weights(store: KvStore, block_tables: torch.Tensor, seq_lens: torch.Tensor, q: torch.Tensor,
@@ -705,21 +724,18 @@ def mocap_decode_key_weights(store: KvStore, block_tables: torch.Tensor, seq_len
                              weights: torch.Tensor, stream=None) -> None:
     """q: bf16 [batch][h_q][head_dim]; lse: fp32 [batch][h_q]; prev, weights: fp32 [batch][h_kv][stride], stride at
     least max_len (None: what the tables hold)."""
-    max_len = _batch(store, block_tables, seq_lens, max_len)
-    _require(q, torch.bfloat16, "q", 3)
-    _require(lse, torch.float32, "lse", 2)
-    batch, h_q, head_dim = q.shape
-    if batch != seq_lens.shape[0] or tuple(lse.shape) != (batch, h_q):
+    device = _raw_device()
+    tables_ptr, lens_ptr, batch, stride, max_len = _batch(store, block_tables, seq_lens, max_len, device)
+    q_ptr = _need(q, torch.bfloat16, "q", 3, device)
+    lse_ptr = _need(lse, torch.float32, "lse", 2, device)
+    rows, h_q, head_dim = q.shape
+    if rows != batch or lse.shape != (batch, h_q):
         raise ValueError("q must be [batch][h_q][head_dim] and lse [batch][h_q]")
-    prev_ptr = _same_or_apart(prev, weights, 3)
-    if tuple(weights.shape[:2]) != (batch, store.h_kv):
-        raise ValueError("weights must be [batch][h_kv][stride]")
-    _one_device(q, lse, prev, weights)
-    desc = store.descriptor()
+    prev_ptr, w_ptr = _weights(prev, weights, (batch, store.h_kv), device)
+    desc = _store_on(store, device)
     _check(load_library().mocap_decode_key_weights(
-        ctypes.byref(desc), block_tables.data_ptr(), block_tables.shape[1], seq_lens.data_ptr(), batch, max_len,
-        q.data_ptr(), h_q, store.h_kv, head_dim, float(scale), lse.data_ptr(), prev_ptr, weights.data_ptr(),
-        weights.shape[2], _stream_handle(stream)), "mocap_decode_key_weights")
+        ctypes.byref(desc), tables_ptr, stride, lens_ptr, batch, max_len, q_ptr, h_q, store.h_kv, head_dim, scale,
+        lse_ptr, prev_ptr, w_ptr, weights.shape[2], _stream_on(stream, device)), "mocap_decode_key_weights")
 
 
 def mocap_kv_evict_workspace_size(n: int, h_kv: int, keep: int) -> int:
@@ -735,24 +751,23 @@ def mocap_kv_evict(src: KvStore, src_table: torch.Tensor, dst: KvStore, dst_tabl
                    stream=None) -> None:
     """weights: fp32 [h_kv][stride], stride at least n; kept: int32 [h_kv][keep]; kept_weights: fp32 [h_kv][keep] or
     None."""
-    _require(src_table, torch.int32, "src_table", 1)
-    _require(dst_table, torch.int32, "dst_table", 1)
-    _require(weights, torch.float32, "weights", 2)
-    _require(kept, torch.int32, "kept", 2)
-    if weights.shape[0] != src.h_kv or tuple(kept.shape) != (src.h_kv, keep):
+    device = _raw_device()
+    src_ptr = _need(src_table, torch.int32, "src_table", 1, device)
+    dst_ptr = _need(dst_table, torch.int32, "dst_table", 1, device)
+    w_ptr = _need(weights, torch.float32, "weights", 2, device)
+    kept_ptr = _need(kept, torch.int32, "kept", 2, device)
+    if weights.shape[0] != src.h_kv or kept.shape != (src.h_kv, keep):
         raise ValueError("weights must be [h_kv][stride] and kept [h_kv][keep]")
+    kw_ptr = None
     if kept_weights is not None:
-        _require(kept_weights, torch.float32, "kept_weights", 2)
+        kw_ptr = _need(kept_weights, torch.float32, "kept_weights", 2, device)
         if kept_weights.shape != kept.shape:
             raise ValueError("kept_weights must be [h_kv][keep]")
-    _one_device(src.k_pool, src.v_pool, dst.k_pool, dst.v_pool, src_table, dst_table, weights, kept, kept_weights,
-                workspace)
-    ws_ptr, ws_bytes = _workspace(workspace)
+    ws_ptr, ws_bytes = _workspace(workspace, device)
     _maybe_check(src, src_table, 0, int(n))
     _maybe_check(dst, dst_table, 0, int(keep))
-    from_desc, to_desc = src.descriptor(), dst.descriptor()
+    from_desc, to_desc = _store_on(src, device), _store_on(dst, device)
     _check(load_library().mocap_kv_evict(
-        ctypes.byref(from_desc), src_table.data_ptr(), src_table.numel(), ctypes.byref(to_desc), dst_table.data_ptr(),
-        dst_table.numel(), int(n), int(keep), int(sinks), int(recent), weights.data_ptr(), weights.shape[1],
-        kept.data_ptr(), kept_weights.data_ptr() if kept_weights is not None else None, ws_ptr, ws_bytes,
-        _stream_handle(stream)), "mocap_kv_evict")
+        ctypes.byref(from_desc), src_ptr, src_table.shape[0], ctypes.byref(to_desc), dst_ptr, dst_table.shape[0], int(n),
+        int(keep), int(sinks), int(recent), w_ptr, weights.shape[1], kept_ptr, kw_ptr, ws_ptr, ws_bytes,
+        _stream_on(stream, device)), "mocap_kv_evict")
