@@ -220,8 +220,10 @@ size_t window_workspace(const mocap::WindowLaunch& p, int32_t head_dim) {
 // parts; the fewest tiles of a part.
 constexpr double kWeightTileUs128 = 0.75, kWeightTileUs64 = 0.55, kWeightGroupUs = 4.0, kWeightJoinUs = 4.0;
 // Up to this many rows the keys stream past the rows instead: 65501 keys of 8 heads
-// of 128, 4, 64, 128 and 256 rows: 24, 27, 33 and 60 us, and 33, 37, 41 and 58.
-constexpr int64_t kWeightFewRows = 128, kWeightFewGroupsPerCu = 4;
+// of 128 by 4, 64, 128 and 256 rows, 29, 31, 37 and 60 us against 38, 42, 46 and 63;
+// 8000 keys, 8.2, -, 10.7 and 17.8 against 8.4, -, 10.3 and 14.9.  Three of its
+// workgroups fit a compute unit (four or six of them per unit: 38 and 41 us for 37).
+constexpr int64_t kWeightFewRows = 128, kWeightFewGroupsPerCu = 3;
 constexpr int64_t kWeightMinTiles = 4, kWeightMaxParts = 64, kWeightMaxRounds = 4;
 
 mocap_status plan_weights(int64_t prefix_len, int32_t chunk_len, int32_t h_q, int32_t h_kv, int32_t head_dim,
@@ -239,7 +241,7 @@ mocap_status plan_weights(int64_t prefix_len, int32_t chunk_len, int32_t h_q, in
   block_divider((uint32_t)group, &p->group_magic, &p->group_shift);
   p->few = rows <= kWeightFewRows;
   if (p->few) {
-    // Every wavefront a tile at least; about four workgroups per compute unit.
+    // Every wavefront a tile at least; about three workgroups per compute unit.
     p->key_blocks = (int32_t)std::min(ceil_div(n, 4 * kTileKeys), ceil_div((int64_t)cus * kWeightFewGroupsPerCu, h_kv));
     p->row_parts = 1;
     return (int64_t)p->key_blocks * h_kv > kMaxGroups ? MOCAP_ERR_UNSUPPORTED : MOCAP_OK;
