@@ -50,7 +50,8 @@ extern "C" {
  * written for n_b <= 0 or n_b > table_stride * block_size.  The positions
  * written must be distinct slots.
  * Errors: INVALID_ARG for null/misaligned pointers or negative sizes;
- * UNSUPPORTED as mocap_kv_append, or for more than 2^24 workgroups.
+ * UNSUPPORTED as mocap_kv_append, or for a batch of 2^23 or
+ * h_kv * head_dim beyond 2^25.
  */
 mocap_status mocap_decode_append(const mocap_kv_store* kv, const int32_t* block_tables, int32_t table_stride,
                                  const int32_t* seq_lens, int32_t batch, const void* k, const void* v, void* stream);
@@ -90,8 +91,9 @@ mocap_status mocap_decode_attn_workspace_size(int32_t batch, int64_t max_len, in
  * and partials are fp32; the probabilities enter the P*V product as the sum of
  * two bf16 values (2^-17 relative).
  * Errors: as mocap_chunk_attn (INVALID_ARG also for a negative window or sinks,
- * a max_len beyond the tables, or null seq_lens); WORKSPACE when the workspace
- * is missing or too small.
+ * a max_len beyond the tables, or null seq_lens); UNSUPPORTED also for a block of
+ * 2^30 or more values per head, or batch * h_q of 2^23; WORKSPACE when the
+ * workspace is missing or too small.
  */
 mocap_status mocap_decode_attn(const mocap_kv_store* kv, const int32_t* block_tables, int32_t table_stride,
                                const int32_t* seq_lens, int32_t batch, int64_t max_len, const void* q, int32_t h_q,
@@ -119,7 +121,8 @@ mocap_status mocap_window_attn_workspace_size(int64_t prefix_len, int32_t chunk_
  *   mocap_chunk_attn
  *
  * Non-finite keys and values reach exactly the rows that see them.
- * Errors: as mocap_chunk_attn, plus INVALID_ARG for window < 1 or sinks < 0.
+ * Errors: as mocap_chunk_attn, plus INVALID_ARG for window < 1 or sinks < 0, and
+ * UNSUPPORTED for a block of 2^30 or more values per head.
  */
 mocap_status mocap_window_attn(const mocap_kv_store* kv, const int32_t* block_table, int32_t n_table, const void* q,
                                int64_t prefix_len, int32_t chunk_len, int32_t h_q, int32_t h_kv, int32_t head_dim,
@@ -155,7 +158,9 @@ mocap_status mocap_key_weights_workspace_size(int64_t prefix_len, int32_t chunk_
  *   workspace     device scratch of workspace_bytes, NULL when the size is 0
  *
  * Sums are fp32, added in a fixed order.  L = 0 is a no-op.
- * Errors: as mocap_chunk_attn; INVALID_ARG for a weight_stride below P + L.
+ * Errors: as mocap_chunk_attn; INVALID_ARG for a weight_stride below P + L, or a
+ * prev that overlaps weights without being it; UNSUPPORTED also for more than
+ * 65535 KV heads with more than 128 rows, or 128 rows of Q beyond 2 GiB.
  */
 mocap_status mocap_key_weights(const mocap_kv_store* kv, const int32_t* block_table, int32_t n_table, const void* q,
                                int64_t prefix_len, int32_t chunk_len, int32_t h_q, int32_t h_kv, int32_t head_dim,
@@ -184,7 +189,7 @@ mocap_status mocap_decode_key_weights(const mocap_kv_store* kv, const int32_t* b
 /*
  * mocap_kv_evict_workspace_size -- workspace bytes of mocap_kv_evict.
  * Errors: INVALID_ARG for a null bytes_out or malformed sizes; UNSUPPORTED for
- * more than 65535 heads or 2^30 positions.
+ * more than 65535 heads or 2^30 - 64 positions.
  */
 mocap_status mocap_kv_evict_workspace_size(int64_t n, int32_t h_kv, int32_t keep, size_t* bytes_out);
 
@@ -215,9 +220,10 @@ mocap_status mocap_kv_evict_workspace_size(int64_t n, int32_t h_kv, int32_t keep
  *
  * Slots of dst at position keep and beyond are left as they were.
  * Errors: INVALID_ARG for null/misaligned pointers, malformed sizes, stores that
- * differ in h_kv or head_dim, tables that are too short, or dst = src (see
- * above); UNSUPPORTED as mocap_kv_evict_workspace_size, or for a head_dim or
- * block size the store does not have; WORKSPACE when the workspace is missing or too small; HIP if a launch fails.
+ * differ in h_kv or head_dim, tables that are too short, dst = src (see above),
+ * or kept_weights that overlap weights; UNSUPPORTED as mocap_kv_evict_workspace_size, or for a head_dim or
+ * block_size that mocap_kv_append does not take; WORKSPACE when the workspace is
+ * missing or too small; HIP if a launch fails.
  */
 mocap_status mocap_kv_evict(const mocap_kv_store* src, const int32_t* src_table, int32_t n_src_table,
                             const mocap_kv_store* dst, const int32_t* dst_table, int32_t n_dst_table, int64_t n,

@@ -766,6 +766,10 @@ def mocap_kv_evict(src: KvStore, src_table: torch.Tensor, dst: KvStore, dst_tabl
     ws_ptr, ws_bytes = _workspace(workspace, device)
     _maybe_check(src, src_table, 0, int(n))
     _maybe_check(dst, dst_table, 0, int(keep))
+    if _check_tables and (src.k_pool.data_ptr() == dst.k_pool.data_ptr() or src.v_pool.data_ptr() == dst.v_pool.data_ptr()):
+        used = [t[:-(-n_pos // s.block_size)].tolist() for s, t, n_pos in ((src, src_table, n), (dst, dst_table, keep))]
+        if set(used[0]) & set(used[1]):
+            raise ValueError("dst_table names a block that src_table uses")
     from_desc, to_desc = _store_on(src, device), _store_on(dst, device)
     _check(load_library().mocap_kv_evict(
         ctypes.byref(from_desc), src_ptr, src_table.shape[0], ctypes.byref(to_desc), dst_ptr, dst_table.shape[0], int(n),

@@ -388,7 +388,8 @@ __global__ __launch_bounds__(256) void evict_copy_kernel(const EvictLaunch p) {
   const int count = min(T, p.keep - pos0);
   const int32_t* kept = p.kept + (int64_t)h * p.keep + pos0;
   auto source = [&](int r, int* slot) __attribute__((always_inline)) {  // first element of the block's head
-    const int pos = kept[min(r, count - 1)];
+    // (In range also where the weights were written to while positions were chosen.)
+    const int pos = max(0, min(kept[min(r, count - 1)], p.n - 1));
     const int lb = pos / p.src_block_size;
     *slot = pos - lb * p.src_block_size;
     return ((int64_t)p.src_table[lb] * p.h_kv + h) * D * p.src_block_size;

@@ -34,6 +34,22 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Integer and fp32 arrays are read and written value by value.
 bool aligned4(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 3u) == 0; }
 
+// Whether [a, a + a_values) and [b, b + b_values) of 4-byte values share memory.
+using wide = unsigned __int128;
+bool overlap(const void* a, wide a_values, const void* b, wide b_values) {
+  const wide x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + 4 * b_values && y < x + 4 * a_values;
+}
+
+// Values of rows `rows` of an array with this stride, the last of `used` values.
+wide extent(int64_t rows, int64_t stride, int64_t used) { return (wide)(rows - 1) * (wide)stride + (wide)used; }
+
+// The attention kernels step through a block's values of one KV head with 32-bit
+// byte offsets.
+bool block_too_large(const mocap_kv_store* kv) {
+  return (int64_t)kv->head_dim * kv->block_size > ((int64_t)1 << 30) - 1;
+}
+
 bool valid_scale(float scale) { return scale > 0.f && std::isfinite(scale); }
 
 mocap_status check_heads(int32_t h_q, int32_t h_kv, int32_t head_dim) {
@@ -230,6 +246,9 @@ mocap_status plan_weights(int64_t prefix_len, int32_t chunk_len, int32_t h_q, in
                           mocap::KeyWeightsLaunch* p) {
   const int64_t group = h_q / h_kv, rows = chunk_len * group, n = prefix_len + chunk_len;
   if (rows > ((int64_t)1 << 31) - 1024) return MOCAP_ERR_UNSUPPORTED;
+  // A stage's rows (128, of 128 / group + 2 tokens at most) are addressed with 32-bit
+  // byte offsets.
+  if ((128 / group + 2) * h_q * head_dim * 2 > ((int64_t)1 << 31) - 1) return MOCAP_ERR_UNSUPPORTED;
   int cus = 0;
   const mocap_status st = device_cu_count(&cus);
   if (st != MOCAP_OK) return st;
@@ -274,7 +293,8 @@ size_t weights_workspace(const mocap::KeyWeightsLaunch& p) {
 
 // ---- Eviction ----
 
-constexpr int64_t kEvictMaxPositions = (int64_t)1 << 30;  // its kernels step over positions in 32 bits
+// Its kernels step over positions in 32 bits, its grids have four threads a position.
+constexpr int64_t kEvictMaxPositions = ((int64_t)1 << 30) - 64;
 
 // The workspace is sized for all n positions as candidates; sinks and recent
 // ones only make them fewer.
@@ -314,7 +334,7 @@ mocap_status mocap_decode_append(const mocap_kv_store* kv, const int32_t* block_
   const mocap_status st = check_batch(kv, block_tables, table_stride, seq_lens, batch, 0);
   if (st != MOCAP_OK || batch == 0) return st;
   if (!k || !v || !aligned16(k) || !aligned16(v)) return MOCAP_ERR_INVALID_ARG;
-  if (batch > kMaxGroups || kv->h_kv > 65535 * 16) return MOCAP_ERR_UNSUPPORTED;
+  if (batch > kMaxGroups || (int64_t)kv->h_kv * (kv->head_dim / 8) > 65535 * 64) return MOCAP_ERR_UNSUPPORTED;
   MOCAP_DEBUG_CHECK_BATCH(kv, block_tables, table_stride, seq_lens, batch, (int64_t)table_stride * kv->block_size, 1, 0);
   mocap::DecodeAppendLaunch p;
   p.k = static_cast<const uint16_t*>(k);
@@ -356,6 +376,7 @@ mocap_status mocap_decode_attn(const mocap_kv_store* kv, const int32_t* block_ta
     return MOCAP_ERR_INVALID_ARG;
   if (batch == 0) return MOCAP_OK;
   if (!q || !o || !lse || !aligned16(q) || !aligned16(o) || !aligned4(lse)) return MOCAP_ERR_INVALID_ARG;
+  if (block_too_large(kv)) return MOCAP_ERR_UNSUPPORTED;
   mocap::DecodeAttnLaunch p;
   st = plan_decode(batch, max_len, h_q, h_kv, window, sinks, &p);
   if (st != MOCAP_OK) return st;
@@ -405,6 +426,7 @@ mocap_status mocap_window_attn(const mocap_kv_store* kv, const int32_t* block_ta
   if (window < 1 || sinks < 0 || num_splits < 0) return MOCAP_ERR_INVALID_ARG;
   if (chunk_len == 0) return MOCAP_OK;
   if (!o || !lse || !aligned16(o) || !aligned4(lse)) return MOCAP_ERR_INVALID_ARG;
+  if (block_too_large(kv)) return MOCAP_ERR_UNSUPPORTED;
   mocap::WindowLaunch p;
   st = plan_window(prefix_len, chunk_len, h_q, h_kv, head_dim, window, sinks, num_splits, &p);
   if (st != MOCAP_OK) return st;
@@ -460,6 +482,8 @@ mocap_status mocap_key_weights(const mocap_kv_store* kv, const int32_t* block_ta
   if (weight_stride < prefix_len + chunk_len) return MOCAP_ERR_INVALID_ARG;
   if (chunk_len == 0) return MOCAP_OK;
   if (!lse || !weights || !aligned4(lse) || !aligned4(weights) || !aligned4(prev)) return MOCAP_ERR_INVALID_ARG;
+  const wide values = extent(h_kv, weight_stride, prefix_len + chunk_len);
+  if (prev != nullptr && prev != weights && overlap(prev, values, weights, values)) return MOCAP_ERR_INVALID_ARG;
   mocap::KeyWeightsLaunch p;
   st = plan_weights(prefix_len, chunk_len, h_q, h_kv, head_dim, &p);
   if (st != MOCAP_OK) return st;
@@ -493,6 +517,8 @@ mocap_status mocap_decode_key_weights(const mocap_kv_store* kv, const int32_t* b
   if (batch == 0) return MOCAP_OK;
   if (!q || !lse || !weights || !aligned16(q) || !aligned4(lse) || !aligned4(weights) || !aligned4(prev))
     return MOCAP_ERR_INVALID_ARG;
+  const wide values = extent((int64_t)batch * h_kv, weight_stride, max_len);
+  if (prev != nullptr && prev != weights && overlap(prev, values, weights, values)) return MOCAP_ERR_INVALID_ARG;
   mocap::DecodeKeyWeightsLaunch p;
   bool may_split;
   st = plan_batch(batch, max_len, 0, 0, h_kv, kDecodeWeightGroupsPerCu, false, &p.seqs, &may_split);
@@ -544,6 +570,9 @@ mocap_status mocap_kv_evict(const mocap_kv_store* src, const int32_t* src_table,
       !aligned4(kept_weights))
     return MOCAP_ERR_INVALID_ARG;
   if ((src->k_pool == dst->k_pool || src->v_pool == dst->v_pool) && src_table == dst_table) return MOCAP_ERR_INVALID_ARG;
+  if (kept_weights != nullptr &&
+      overlap(weights, extent(src->h_kv, weight_stride, n), kept_weights, (wide)src->h_kv * (wide)keep))
+    return MOCAP_ERR_INVALID_ARG;
   size_t need = 0;
   st = mocap_kv_evict_workspace_size(n, src->h_kv, keep, &need);
   if (st != MOCAP_OK) return st;

@@ -79,7 +79,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void window_attn_kernel(const Wind
   constexpr int STAGES = 4;
   // One array for the ring and what lies beside it: with several, the compiler
   // tells them apart, takes every read of the ring to depend on the copies in
-  // flight, and waits for those (143 us instead of 1xx for 2048 tokens in a window
+  // flight, and waits for those (143 instead of 141 us for 2048 tokens in a window
   // of 4096).
   constexpr int ROW_BITS = kWindowRows * MD;  // words
   __shared__ __attribute__((aligned(1024))) uint16_t lds[STAGES * BUF_ELEMS + 2 * (STAGES + 2 * ROW_BITS)];

@@ -191,3 +191,25 @@ def test_refused_calls_write_nothing(gpu):
         call(w=weights[:1])
     torch.cuda.synchronize()
     assert (dst.k_pool == 7.0).all() and (dst.v_pool == 7.0).all()
+
+
+def test_table_checks_refuse_a_shared_block(gpu):
+    """Into the same pool: a block of the source is no block of the result."""
+    src, tables, _, _ = make_store(330, [300], 64, 1, 64, spare=4)
+    weights = weights_of("heavy", 1, 300, 331)
+    kept = torch.full((1, 70), 7, dtype=torch.int32, device="cuda")
+    free = [b for b in range(src.num_blocks) if b not in tables[0].tolist()]
+    binding.set_table_checks(True)
+    try:
+        for other in (int(tables[0, 0]), int(tables[0, 4])):
+            table = torch.tensor([free[0], other], dtype=torch.int32).cuda()
+            with pytest.raises(ValueError, match="block"):
+                binding.mocap_kv_evict(src, tables[0], src, table, 300, 70, 0, 0, weights, kept)
+        torch.cuda.synchronize()
+        assert (kept == 7).all()
+        table = torch.tensor(free[:2], dtype=torch.int32).cuda()
+        binding.mocap_kv_evict(src, tables[0], src, table, 300, 70, 0, 0, weights, kept)
+    finally:
+        binding.set_table_checks(False)
+    torch.cuda.synchronize()
+    assert kept[0].tolist() == expected(weights[0].cpu(), 300, 70, 0, 0)

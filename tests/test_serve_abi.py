@@ -18,13 +18,12 @@ FAKE, MIS, INVALID, UNSUPPORTED, WORKSPACE = 0x10000, 0x10002, 1, 2, 3
 BIG = 1 << 40
 
 
-@pytest.fixture(scope="module")
-def host(mocap_lib, tmp_path_factory):
+def recording_build(mocap_lib, folder, *flags):
     if not os.path.exists(build.HIPCC):
         pytest.skip("hipcc not available")
-    out = str(tmp_path_factory.mktemp("serve") / "libserve_record.so")
+    out = str(folder / "libserve_record.so")
     sources = [os.path.join(build.CSRC, "serve_api.cpp"), os.path.join(ROOT, "tests", "serve_record.cpp")]
-    cmd = [build.HIPCC, *build.FLAGS, "-x", "hip", *sources, "-shared", "-Wl,-Bsymbolic", "-o", out]
+    cmd = [build.HIPCC, *build.FLAGS, *flags, "-x", "hip", *sources, "-shared", "-Wl,-Bsymbolic", "-o", out]
     res = subprocess.run(cmd, capture_output=True, text=True)
     assert res.returncode == 0, res.stderr[-2000:]
     lib = ctypes.CDLL(out)
@@ -32,6 +31,11 @@ def host(mocap_lib, tmp_path_factory):
         f, real = getattr(lib, name), getattr(mocap_lib.load_library(), name)
         f.restype, f.argtypes = real.restype, real.argtypes
     return lib
+
+
+@pytest.fixture(scope="module")
+def host(mocap_lib, tmp_path_factory):
+    return recording_build(mocap_lib, tmp_path_factory.mktemp("serve"))
 
 
 def store(num_blocks=64, block_size=256, h_kv=8, head_dim=128, k=FAKE, v=FAKE):
@@ -283,3 +287,74 @@ def test_key_weight_blocks(host):
 def test_kernels_keep_their_values_in_registers(src, tmp_path):
     for name, r in resource_report(src, str(tmp_path)).items():
         assert r.get("VGPRs Spill", 0) == 0 and r.get("ScratchSize [bytes/lane]", 0) == 0, f"{name}: {r}"
+
+
+def test_blocks_and_heads_beyond_32_bits(host):
+    """What a kernel addresses with 32-bit offsets is refused beyond them."""
+    def kv(**kwargs):
+        return store(num_blocks=2, **kwargs)
+    for d in (64, 128):
+        for block_size, status in (((1 << 30) // d - 64, 0), ((1 << 30) // d, UNSUPPORTED)):
+            big = kv(block_size=block_size, h_kv=1, head_dim=d)
+            assert window(host, kv=big, h_q=4, h_kv=1, d=d) == status
+            assert decode(host, kv=big, h_q=4, h_kv=1, d=d) == status
+            assert weights(host, kv=big, h_q=4, h_kv=1, d=d) == 0
+            assert decode_weights(host, kv=big, h_q=4, h_kv=1, d=d) == 0
+    for d, heads in ((64, 65535 * 8), (128, 65535 * 4)):
+        assert append(host, kv=kv(h_kv=heads, head_dim=d)) == 0
+        assert append(host, kv=kv(h_kv=heads + 1, head_dim=d)) == UNSUPPORTED
+    for group in (1, 3, 4, 64, 200):
+        h_kv = ((1 << 31) - 1) // ((128 // group + 2) * group * 256)
+        most = dict(kv=kv(h_kv=min(h_kv, 65535)), h_q=min(h_kv, 65535) * group, h_kv=min(h_kv, 65535))
+        assert weights(host, L=200, stride=1200, **most) == 0
+        more = dict(kv=kv(h_kv=h_kv + 1), h_q=(h_kv + 1) * group, h_kv=h_kv + 1)
+        assert weights(host, L=200, stride=1200, **more) == UNSUPPORTED
+    size = ctypes.c_size_t(0)
+    most = (1 << 30) - 64
+    assert host.mocap_kv_evict_workspace_size(most, 1, most, ctypes.byref(size)) == 0
+    assert host.mocap_kv_evict_workspace_size(most + 1, 1, 1, ctypes.byref(size)) == UNSUPPORTED
+
+
+def test_weights_that_overlap(host):
+    """prev is weights or apart from it; kept_weights is apart from weights."""
+    n = 4 * (7 * 1200 + 1100)  # bytes of 8 rows of 1100, 1200 apart
+    for prev, status in ((FAKE, 0), (FAKE + 4, INVALID), (FAKE + n - 4, INVALID), (FAKE + n, 0), (FAKE - n, 0),
+                         (FAKE - n + 4, INVALID)):
+        assert weights(host, stride=1200, prev=prev) == status
+    n = 4 * (31 * 5000 + 4096)
+    for prev, status in ((FAKE + n, 0), (FAKE + n - 4, INVALID), (FAKE, 0)):
+        assert decode_weights(host, prev=prev, w_stride=5000) == status
+    n = 4 * (7 * 5000 + 4096)
+    for kw, status in ((FAKE, INVALID), (FAKE + n, 0), (FAKE + n - 4, INVALID), (FAKE - 4 * 8 * 1000, 0),
+                       (FAKE - 4 * 8 * 1000 + 4, INVALID)):
+        assert evict(host, stride=5000, kw=kw) == status
+
+
+def test_debug_build_checks_the_tables(mocap_lib, tmp_path):
+    """The entries that a call uses, and those alone."""
+    lib = recording_build(mocap_lib, tmp_path, "-DMOCAP_DEBUG_TABLES")
+    kept = []
+
+    def ints(*values):
+        kept.append((ctypes.c_int32 * len(values))(*values))
+        return ctypes.addressof(kept[-1])
+    kv = store(num_blocks=4)
+    args = dict(kv=kv, stride=3, batch=2)
+    for table, lens, status in (((0, 1, 2, 3, 1, 0), (700, 700), 0), ((0, 1, 4, 3, 1, 0), (513, 1), INVALID),
+                                ((0, 1, 4, 3, 1, 0), (512, 1), 0), ((0, 1, 4, -1, 1, 0), (512, 0), 0),
+                                ((0, 1, 4, -1, 1, 0), (512, 1), INVALID), ((0, 0, 0, 0, 0, 0), (768, 768), 0)):
+        where = dict(tables=ints(*table), lens=ints(*lens))
+        assert decode(lib, max_len=768, **where, **args) == status
+        assert decode_weights(lib, max_len=768, **where, **args) == status
+    bad = dict(tables=ints(0, 9, 2, 0, 1, 2), lens=ints(700, 700))
+    assert decode(lib, max_len=768, window=100, sinks=4, **bad, **args) == 0
+    assert decode(lib, max_len=768, window=200, sinks=4, **bad, **args) == INVALID
+    assert decode(lib, max_len=768, window=100, sinks=257, **bad, **args) == INVALID
+    assert append(lib, **bad, **args) == 0  # position 699 is in the third block
+    assert append(lib, tables=bad["tables"], lens=ints(300, 0), **args) == INVALID
+    for table, status in (((0, 1, 2), 0), ((0, 9, 2), INVALID), ((0, 1, 1), INVALID)):
+        assert window(lib, kv=kv, table=ints(*table), n_table=3, P=500, L=200) == status
+        assert weights(lib, kv=kv, table=ints(*table), n_table=3, P=500, L=200) == status
+        assert evict(lib, src=kv, src_table=ints(*table), n_src=3, n=700, keep=300, dst_table=ints(0, 1)) == status
+    assert window(lib, kv=kv, table=ints(0, 9, 2), n_table=3, P=650, L=50, window=100) == 0
+    assert evict(lib, src=kv, src_table=ints(0, 1, 2), n_src=3, n=700, keep=300, dst=kv, dst_table=ints(0, 4)) == INVALID
