@@ -10,7 +10,16 @@
 // on the order of the atomics.
 //
 // Up to kEvictOneGroup candidates are held by one workgroup per head, which needs one
-// launch; more are cut into chunks, in four launches.
+// launch (8 heads of 128, 100 of 16384 positions kept: 17 us in all, 26 in chunks);
+// more are cut into chunks, in four launches, which is what a workgroup's registers
+// ask for (131072 positions: 27 of 111 us, bound by four chains of launch, load and
+// count; 8, 16, 32 and 64 chunks: 43, 34, 31 and 32 us with 256 kept).  Up to 4096
+// candidates a workgroup holds four a thread instead of sixteen (13.3 us and 16.0).
+//
+// Bounds: the copy by HBM, not by the bytes that stay but by the lines they lie in.
+// A value's dim lies in a line with 63 other positions', so at a share of 1/8 nearly
+// every line of V is read: 131072 positions to 16384, 8 heads of 128: 369 MB in
+// 84 us, 4.4 TB/s.
 #include "attn_device.h"
 #include "serve.h"
 
@@ -252,18 +261,53 @@ __device__ __forceinline__ Chunk chunk_of(const EvictLaunch& p, int h, int chunk
   return Chunk{p.weights + h * p.weight_stride + p.sinks, (int)(all * chunk / p.chunks), (int)(all * (chunk + 1) / p.chunks)};
 }
 
+// A thread's candidates of a chunk, in batches whose loads are all in flight: first()
+// asks for the first batch (before other work, where there is some), each() hands
+// every candidate's key to f.  (Loaded one by one: 70 instead of 63 us for 8
+// heads of 500000 positions, of which the copy takes 25.)
+struct Batches {
+  static constexpr int ROUNDS = 8;
+  const Chunk& x;
+  int tid;
+  float w[ROUNDS];
+  __device__ __forceinline__ Batches(const Chunk& chunk, int thread) : x(chunk), tid(thread) {}
+  __device__ __forceinline__ void load(int i0) {
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+      const int i = r * kSelectThreads + tid;
+      w[r] = i < x.end - i0 ? x.w[i0 + i] : 0.f;
+    }
+  }
+  __device__ __forceinline__ void first() { load(x.begin); }
+  template <class F>
+  __device__ __forceinline__ void each(F f) {
+    for (int i0 = x.begin; i0 < x.end; i0 += ROUNDS * kSelectThreads) {
+      uint32_t key[ROUNDS];
+#pragma unroll
+      for (int r = 0; r < ROUNDS; ++r) key[r] = weight_key(w[r]);
+      const int count = x.end - i0;
+      if (count > ROUNDS * kSelectThreads) load(i0 + ROUNDS * kSelectThreads);
+#pragma unroll
+      for (int r = 0; r < ROUNDS; ++r)
+        if (r * kSelectThreads + tid < count) f(key[r]);
+    }
+  }
+};
+
 __global__ __launch_bounds__(kSelectThreads) void evict_first_kernel(const EvictLaunch p) {
   __shared__ uint32_t hist[bins(0)];
   const int tid = threadIdx.x, chunk = blockIdx.x, h = blockIdx.y;
   const ChunkCounts c = counts_of(p, h);
   const Chunk x = chunk_of(p, h, chunk);
+  Batches batches(x, tid);
+  batches.first();
   hist[tid] = 0;
   if (chunk == 0)
     for (int i = tid; i < bins(1); i += kSelectThreads) c.second[i] = 0;
   put_always_kept(p, output_of(p, h), x.w - p.sinks, (int64_t)chunk * kSelectThreads + tid,
                   (int64_t)p.chunks * kSelectThreads);
   __syncthreads();
-  for (int i = x.begin + tid; i < x.end; i += kSelectThreads) atomicAdd(&hist[digit_of<0>(weight_key(x.w[i]))], 1u);
+  batches.each([&](uint32_t key) { atomicAdd(&hist[digit_of<0>(key)], 1u); });
   __syncthreads();
   c.first[chunk * bins(0) + tid] = hist[tid];
 }
@@ -274,12 +318,14 @@ __global__ __launch_bounds__(kSelectThreads) void evict_second_kernel(const Evic
   const int tid = threadIdx.x, chunk = blockIdx.x, h = blockIdx.y;
   const ChunkCounts c = counts_of(p, h);
   const Chunk x = chunk_of(p, h, chunk);
+  Batches batches(x, tid);
   for (int i = tid; i < bins(1); i += kSelectThreads) hist[i] = 0;
   Border border{0, (uint32_t)(p.keep - p.sinks - p.recent)};
   find_digit<0>([&](int bin) {
     uint32_t v[kEvictMaxChunks], sum = 0;  // all loads in flight
 #pragma unroll
     for (int y = 0; y < kEvictMaxChunks; ++y) v[y] = y < p.chunks ? c.first[y * bins(0) + bin] : 0;
+    batches.first();
 #pragma unroll
     for (int y = 0; y < kEvictMaxChunks; ++y) sum += v[y];
     return sum;
@@ -288,10 +334,9 @@ __global__ __launch_bounds__(kSelectThreads) void evict_second_kernel(const Evic
     c.border[0] = border.prefix;
     c.border[1] = border.left;
   }
-  for (int i = x.begin + tid; i < x.end; i += kSelectThreads) {
-    const uint32_t key = weight_key(x.w[i]);
+  batches.each([&](uint32_t key) {
     if (in_prefix<1>(key, border.prefix)) atomicAdd(&hist[digit_of<1>(key)], 1u);
-  }
+  });
   __syncthreads();
   for (int i = tid; i < bins(1); i += kSelectThreads)
     if (hist[i] != 0) atomicAdd(&c.second[i], hist[i]);
@@ -302,6 +347,8 @@ __global__ __launch_bounds__(kSelectThreads) void evict_third_kernel(const Evict
   const int tid = threadIdx.x, chunk = blockIdx.x, h = blockIdx.y;
   const ChunkCounts c = counts_of(p, h);
   const Chunk x = chunk_of(p, h, chunk);
+  Batches batches(x, tid);
+  batches.first();
   hist[tid] = 0;
   if (tid == 0) above_s = 0;
   Border border{c.border[0], c.border[1]};
@@ -311,14 +358,13 @@ __global__ __launch_bounds__(kSelectThreads) void evict_third_kernel(const Evict
     c.border[3] = border.left;
   }
   uint32_t above = 0;
-  for (int i = x.begin + tid; i < x.end; i += kSelectThreads) {
-    const uint32_t key = weight_key(x.w[i]);
+  batches.each([&](uint32_t key) {
     if (in_prefix<2>(key, border.prefix)) {
       atomicAdd(&hist[digit_of<2>(key)], 1u);
     } else {
       above += key > border.prefix;
     }
-  }
+  });
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) above += __shfl_xor(above, off);
   if ((tid & 63) == 0) atomicAdd(&above_s, above);
@@ -369,10 +415,14 @@ __global__ __launch_bounds__(kSelectThreads) void evict_compact_kernel(const Evi
   for (int i0 = x.begin; i0 < x.end; i0 += ROUNDS * kSelectThreads) {
     uint32_t key[ROUNDS];
     const int count = min(x.end - i0, ROUNDS * kSelectThreads);
-    if (i0 > x.begin) load(i0);
+    float now[ROUNDS];
 #pragma unroll
-    for (int r = 0; r < ROUNDS; ++r) key[r] = weight_key(w[r]);
-    compact<ROUNDS>(key, w, p.sinks + i0, count, border, p.sinks, above, equal, out);
+    for (int r = 0; r < ROUNDS; ++r) {
+      now[r] = w[r];
+      key[r] = weight_key(w[r]);
+    }
+    if (i0 + ROUNDS * kSelectThreads < x.end) load(i0 + ROUNDS * kSelectThreads);
+    compact<ROUNDS>(key, now, p.sinks + i0, count, border, p.sinks, above, equal, out);
   }
 }
 
