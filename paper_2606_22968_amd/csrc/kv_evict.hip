@@ -12,14 +12,14 @@
 // Up to kEvictOneGroup candidates are held by one workgroup per head, which needs one
 // launch (8 heads of 128, 100 of 16384 positions kept: 17 us in all, 26 in chunks);
 // more are cut into chunks, in four launches, which is what a workgroup's registers
-// ask for (131072 positions: 27 of 111 us, bound by four chains of launch, load and
+// ask for (131072 positions: 27 of 101 us, bound by four chains of launch, load and
 // count; 8, 16, 32 and 64 chunks: 43, 34, 31 and 32 us with 256 kept).  Up to 4096
 // candidates a workgroup holds four a thread instead of sixteen (13.3 us and 16.0).
 //
 // Bounds: the copy by HBM, not by the bytes that stay but by the lines they lie in.
 // A value's dim lies in a line with 63 other positions', so at a share of 1/8 nearly
 // every line of V is read: 131072 positions to 16384, 8 heads of 128: 369 MB in
-// 84 us, 4.4 TB/s.
+// 75 us, 4.9 TB/s.
 #include "attn_device.h"
 #include "serve.h"
 
@@ -427,9 +427,13 @@ __global__ __launch_bounds__(kSelectThreads) void evict_compact_kernel(const Evi
 }
 
 // ---- Copy ----
-// One workgroup per 64 positions of dst, KV head and 32 dims.  A kept key is one
-// row.  A kept value's dims lie in as many rows of V, where neighbouring kept
-// positions share lines: a wavefront takes one dim of the 64 positions at a time.
+// One workgroup per 64 positions of dst, KV head and D / 32-th of the work: a kept key
+// is one row, of which a workgroup copies whole ones (all keys' 32 dims instead, which
+// reads and writes every line in pieces at different times: 110.8 and 101.5 us for
+// 131072 positions to 16384, 206 and 164 to 65536); a kept value's dims lie in as many
+// rows of V, where neighbouring kept positions share lines: a wavefront takes one dim
+// of the 64 positions at a time, the workgroup 32 dims.  Giving neighbouring
+// positions, which share lines, to one XCD changes nothing (102, 168 us).
 template <int D>
 __global__ __launch_bounds__(256) void evict_copy_kernel(const EvictLaunch p) {
   constexpr int T = 64, DIMS = 32;
@@ -447,7 +451,7 @@ __global__ __launch_bounds__(256) void evict_copy_kernel(const EvictLaunch p) {
   const int lb = pos0 / p.dst_block_size;  // 64 positions lie in one block
   const int slot0 = pos0 - lb * p.dst_block_size;
   const int64_t dst = ((int64_t)p.dst_table[lb] * p.h_kv + h) * D * p.dst_block_size;
-  const int kr = tid / (DIMS / 8), kc = dim0 + tid % (DIMS / 8) * 8;  // K: row and first dim
+  const int kr = blockIdx.z * (DIMS * T / D) + tid / (D / 8), kc = tid % (D / 8) * 8;  // K: row and first dim
   const int vr = tid & (T - 1), ve = dim0 + tid / T;                  // V: position and first dim, 4 apart
   int k_slot, v_slot;
   const uint16_t* k = p.k_src + source(kr, &k_slot);
