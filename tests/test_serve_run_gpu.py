@@ -9,7 +9,7 @@ import torch
 
 from helpers import say
 from paper_2606_22968_amd import binding
-from serve_helpers import B, Attention, Weights, check_close, put, randn, take
+from serve_helpers import B, Attention, Weights, check_close, make_store, put, randn, take
 from test_evict_gpu import expected
 
 pytestmark = pytest.mark.gpu
@@ -245,3 +245,43 @@ def test_another_device_is_refused(gpu, monkeypatch):
     monkeypatch.undo()
     torch.cuda.synchronize()
     assert (out == 7.0).all() and (weights == 7.0).all() and (kept == 7).all()
+
+
+@pytest.mark.parametrize("h_q,h_kv,d", [(200, 1, 64), (258, 2, 128), (128, 1, 128)])
+def test_wide_groups(gpu, h_q, h_kv, d):
+    """More query heads on a KV head than any block of rows holds, in every call."""
+    say(f"[case] wide groups {h_q}/{h_kv}/{d}")
+    lens, scale = [700, 0, 65, 1], d ** -0.5
+    store, tables, ks, vs = make_store(520, lens, 64, h_kv, d)
+    q = randn(521, 4, h_q, d)
+    seq_lens = torch.tensor(lens, dtype=torch.int32).cuda()
+    o, lse = torch.zeros((4, h_q, d), dtype=torch.bfloat16, device="cuda"), torch.zeros((4, h_q), device="cuda")
+    binding.mocap_decode_attn(store, tables, seq_lens, q.cuda(), 700, scale, o, lse,
+                              scratch(binding.mocap_decode_attn_workspace_size(4, h_q, h_kv, d, 700)))
+    prev = torch.rand((4, h_kv, 700), generator=torch.Generator().manual_seed(522))
+    weights = prev.cuda()
+    binding.mocap_decode_key_weights(store, tables, seq_lens, q.cuda(), 700, scale, lse, weights, weights)
+    for b, n in enumerate(lens):
+        if n == 0:
+            assert (o[b] == 0).all() and (lse[b] == -float("inf")).all() and torch.equal(weights[b].cpu(), prev[b])
+            continue
+        ref = Attention(q[b:b + 1], ks[b], vs[b], n - 1, scale)
+        check_close(o[b:b + 1], ref.o, ref.o_bound(P_DECODE), f"row {b} o")
+        check_close(lse[b][:, None], ref.lse, ref.lse_bound(), f"row {b} lse")
+        ref = Weights(q[b:b + 1], ks[b], n - 1, scale, lse[b].cpu()[:, None], prev[b])
+        check_close(weights[b, :, :n], ref.w, ref.bound, f"row {b} weights")
+        assert torch.equal(weights[b, :, n:].cpu(), prev[b, :, n:])
+    for rows in (1, 7):
+        q, prefix = randn(523, rows, h_q, d), 700 - rows
+        o = torch.zeros((rows, h_q, d), dtype=torch.bfloat16, device="cuda")
+        lse = torch.zeros((h_q, rows), device="cuda")
+        size = binding.mocap_window_attn_workspace_size(prefix, rows, h_q, h_kv, d, 300, 4)[1]
+        binding.mocap_window_attn(store, tables[0], q.cuda(), prefix, scale, 300, 4, o, lse, scratch(size))
+        ref = Attention(q, ks[0], vs[0], prefix, scale, 300, 4)
+        check_close(o, ref.o, ref.o_bound(P_CHUNK), f"{rows} rows o")
+        check_close(lse, ref.lse, ref.lse_bound(), f"{rows} rows lse")
+        sums = torch.zeros((h_kv, 700), device="cuda")
+        size = binding.mocap_key_weights_workspace_size(prefix, rows, h_q, h_kv, d)
+        binding.mocap_key_weights(store, tables[0], q.cuda(), prefix, scale, lse, None, sums, scratch(size))
+        ref = Weights(q, ks[0], prefix, scale, lse.cpu())
+        check_close(sums, ref.w, ref.bound, f"{rows} rows weights")
