@@ -51,7 +51,7 @@ extern "C" {
  * written must be distinct slots.
  * Errors: INVALID_ARG for null/misaligned pointers or negative sizes;
  * UNSUPPORTED as mocap_kv_append, or for a batch of 2^23 or
- * h_kv * head_dim beyond 2^25.
+ * more, or h_kv * head_dim above 512 * 65535.
  */
 mocap_status mocap_decode_append(const mocap_kv_store* kv, const int32_t* block_tables, int32_t table_stride,
                                  const int32_t* seq_lens, int32_t batch, const void* k, const void* v, void* stream);
