@@ -96,7 +96,8 @@ struct WindowLaunch {
 };
 
 // One launch of the key weight kernel: a workgroup's eight wavefronts hold 64 keys
-// each and walk one of row_parts even cuts of the rows that see some of them.
+// each and walk an even cut of the row tiles that see some of them, part_tiles at
+// most.  Keys of the prefix are seen by all tiles, in row_parts cuts.
 constexpr int kWeightKeys = 64;
 constexpr int kWeightWaves = 8;
 struct KeyWeightsLaunch {
@@ -121,6 +122,8 @@ struct KeyWeightsLaunch {
   bool few;                 // the kernel for few rows
   int32_t key_blocks;       // ceil((P + L) / 512); few: workgroups of a KV head
   int32_t row_parts;
+  int32_t part_tiles;
+  int32_t head_wgs;         // workgroups of a KV head
   float scale_log2;
 };
 

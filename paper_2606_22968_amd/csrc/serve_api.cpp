@@ -233,14 +233,15 @@ size_t window_workspace(const mocap::WindowLaunch& p, int32_t head_dim) {
 // ---- Key weights ----
 
 // A row tile (32 rows by 512 keys), fixed work of a workgroup, and the join of row
-// parts; the fewest tiles of a part.
+// parts; the fewest tiles of a part, and the most parts (1000 tokens of 64/1/64 heads
+// without a prefix: 37 us at 64, 25 at 128, 24 at 256).
 constexpr double kWeightTileUs128 = 0.75, kWeightTileUs64 = 0.55, kWeightGroupUs = 4.0, kWeightJoinUs = 4.0;
 // Up to this many rows the keys stream past the rows instead: 65501 keys of 8 heads
 // of 128 by 4, 64, 128 and 256 rows, 29, 31, 37 and 60 us against 38, 42, 46 and 63;
 // 8000 keys, 8.2, -, 10.7 and 17.8 against 8.4, -, 10.3 and 14.9.  Three of its
 // workgroups fit a compute unit (four or six of them per unit: 38 and 41 us for 37).
 constexpr int64_t kWeightFewRows = 128, kWeightFewGroupsPerCu = 3;
-constexpr int64_t kWeightMinTiles = 4, kWeightMaxParts = 64, kWeightMaxRounds = 4;
+constexpr int64_t kWeightMinTiles = 4, kWeightMaxParts = 256, kWeightMaxRounds = 4;
 
 mocap_status plan_weights(int64_t prefix_len, int32_t chunk_len, int32_t h_q, int32_t h_kv, int32_t head_dim,
                           mocap::KeyWeightsLaunch* p) {
@@ -272,15 +273,27 @@ mocap_status plan_weights(int64_t prefix_len, int32_t chunk_len, int32_t h_q, in
   const int64_t wgs = (int64_t)p->key_blocks * h_kv, tiles = ceil_div(rows, 32);
   if (wgs > kMaxGroups || h_kv > 65535) return MOCAP_ERR_UNSUPPORTED;
   const double tile_us = head_dim == 128 ? kWeightTileUs128 : kWeightTileUs64;
-  double best_us = INFINITY;
+  // Key blocks that all rows see from their first key on; the others have the later
+  // rows only, and fewer parts of this many tiles.
+  const int64_t seen = std::min<int64_t>(p->key_blocks, prefix_len / block_keys + 1);
   p->row_parts = 1;
-  for (int64_t parts = 1; parts <= std::min<int64_t>(kWeightMaxParts, ceil_div(tiles, kWeightMinTiles)); ++parts) {
-    if (parts > 1 && wgs * parts > kWeightMaxRounds * cus) break;
-    double us = (double)ceil_div(wgs * parts, cus) * (ceil_div(tiles, parts) * tile_us + kWeightGroupUs);
-    if (parts > 1) us += kWeightJoinUs + 8.0 * parts * h_kv * n / kWindowMergeBytesPerUs;
+  p->part_tiles = (int32_t)tiles;
+  p->head_wgs = p->key_blocks;
+  double best_us = ceil_div(wgs, cus) * (tiles * tile_us + kWeightGroupUs);
+  for (int64_t parts = 2; parts <= std::min<int64_t>(kWeightMaxParts, ceil_div(tiles, kWeightMinTiles)); ++parts) {
+    if (std::max(seen * parts, (int64_t)p->key_blocks) * h_kv > kWeightMaxRounds * cus) break;
+    const int64_t most = ceil_div(tiles, parts);
+    int64_t head_wgs = seen * ceil_div(tiles, most);
+    for (int64_t b = seen; b < p->key_blocks; ++b)
+      head_wgs += ceil_div(tiles - (b * block_keys - prefix_len) * group / 32, most);
+    if (head_wgs * h_kv > kWeightMaxRounds * cus) break;
+    double us = (double)ceil_div(head_wgs * h_kv, cus) * (most * tile_us + kWeightGroupUs);
+    us += kWeightJoinUs + 8.0 * parts * h_kv * n / kWindowMergeBytesPerUs;
     if (us < best_us * 0.98) {
       best_us = us;
-      p->row_parts = (int32_t)parts;
+      p->row_parts = (int32_t)ceil_div(tiles, most);
+      p->part_tiles = (int32_t)most;
+      p->head_wgs = (int32_t)head_wgs;
     }
   }
   return MOCAP_OK;

@@ -66,5 +66,9 @@ void record_weights(int* out) {
   const int v[] = {weights.few, weights.key_blocks, weights.row_parts};
   for (int i = 0; i < 3; ++i) out[i] = v[i];
 }
+void record_weights_cut(int* out) {
+  const int v[] = {weights.row_parts, weights.part_tiles, weights.head_wgs};
+  for (int i = 0; i < 3; ++i) out[i] = v[i];
+}
 
 }  // extern "C"

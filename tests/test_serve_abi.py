@@ -283,6 +283,35 @@ def test_key_weight_blocks(host):
         assert parts == 1 or parts * 4 <= -(-L * 4 // 32) + 3
 
 
+def test_key_weight_parts(host):
+    """The workgroups of a KV head are the parts of all key blocks, counted from
+    the tiles of 32 rows that see a block's first key or a later one."""
+    rng = random.Random(7)
+    cut = 0
+    for _ in range(400):
+        P, L = rng.choice((0, 0, 1, 100, 511, 512, 1500, 40000)), rng.choice((33, 500, 513, 2048, 4096, 10000))
+        h_kv, group = rng.choice((1, 2, 8)), rng.choice((1, 3, 4, 64))
+        rows = L * group
+        if rows <= 128:
+            continue
+        kv = store(h_kv=h_kv, block_size=1 << 16)
+        assert weights(host, kv=kv, P=P, L=L, h_q=group * h_kv, h_kv=h_kv, stride=1 << 20, n_table=64) == 0
+        out = (ctypes.c_int * 3)()
+        host.record_weights_cut(out)
+        row_parts, part_tiles, head_wgs = out
+        tiles = -(-rows // 32)
+        parts = []
+        for block in range(-(-(P + L) // 512)):
+            first = max(0, block * 512 - P) * group // 32
+            assert first < tiles
+            parts.append(-(-(tiles - first) // part_tiles))
+        assert row_parts == max(parts) and head_wgs == sum(parts)
+        seen = min(len(parts), P // 512 + 1)
+        assert set(parts[:seen]) == {row_parts}
+        cut += len(set(parts)) > 1
+    assert cut > 20
+
+
 @pytest.mark.parametrize("src", ["decode_attn.hip", "window_attn.hip", "key_weights.hip", "kv_evict.hip"])
 def test_kernels_keep_their_values_in_registers(src, tmp_path):
     for name, r in resource_report(src, str(tmp_path)).items():
