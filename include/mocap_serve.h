@@ -120,7 +120,10 @@ mocap_status mocap_window_attn_workspace_size(int64_t prefix_len, int32_t chunk_
  *   window >= 1, sinks >= 0; other arguments, outputs and precision as in
  *   mocap_chunk_attn
  *
- * Non-finite keys and values reach exactly the rows that see them.
+ * Non-finite keys and values reach exactly the rows that see them.  (Where the
+ * window hides nothing, W >= P + L, mocap_chunk_attn gives the same rows in less
+ * time, but a non-finite value there also reaches rows of its 64-key tile that do
+ * not see it.)
  * Errors: as mocap_chunk_attn, plus INVALID_ARG for window < 1 or sinks < 0, and
  * UNSUPPORTED for a block of 2^30 or more values per head.
  */
