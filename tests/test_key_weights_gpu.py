@@ -8,7 +8,7 @@ import torch
 
 from helpers import say
 from paper_2606_22968_amd import binding
-from serve_helpers import Attention, Weights, check_close, make_store, randn
+from serve_helpers import U, Attention, Weights, check_close, make_store, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -238,3 +238,25 @@ def test_refused_calls_write_nothing(gpu):
     binding.mocap_key_weights(store, tables[0], empty, 100, 0.1, torch.zeros((4, 0), device="cuda"), None, weights)
     torch.cuda.synchronize()
     assert (weights == 7.0).all()
+
+
+def test_more_than_64_blocks_of_new_keys(gpu):
+    """A chunk so long that a workgroup looks for its part among more key blocks than a
+    wavefront has lanes: some keys of every block against the sum in 64 bits."""
+    rows, d, scale = 34000, 64, 0.125
+    store, tables, ks, _ = make_store(230, [rows], 256, 1, d)
+    q = randn(231, rows, 1, d)
+    lse = math.log(rows) + 0.1 * base(232, 1, rows)
+    weights = torch.full((1, rows), float("nan"), device="cuda")
+    size = binding.mocap_key_weights_workspace_size(0, rows, 1, 1, d)
+    assert size > 0
+    call(store, tables[0], q.cuda(), 0, scale, lse.cuda(), None, weights)
+    keys = torch.arange(0, rows, 211)
+    s = q[:, 0].double() @ ks[0][keys, 0].double().t() * scale
+    big = q[:, 0].double().abs() @ ks[0][keys, 0].double().abs().t() * scale
+    term = torch.exp(s - lse[0].double()[:, None]) * (torch.arange(rows)[:, None] >= keys)
+    # The bound of Weights: each term's argument and exponential, then the sum.
+    e = (d + 16) * U * big + 4 * U * lse[0].double().abs()[:, None] + 4 * U
+    bound = (e * term * (1 + 2 * e)).sum(0) + (rows / 16 + 34) * U * term.sum(0) + 1e-37
+    check_close(weights[0].cpu()[keys], term.sum(0), bound, "long chunk")
+    assert torch.isfinite(weights).all()
