@@ -598,7 +598,8 @@ def mocap_decode_append(store: KvStore, block_tables: torch.Tensor, seq_lens: to
                         v: torch.Tensor, stream=None) -> None:
     """Stores row b of k and v (bf16 [batch][h_kv][head_dim]) at position seq_lens[b] - 1 of sequence b."""
     device = _raw_device()
-    tables_ptr, lens_ptr, batch, stride, _ = _batch(store, block_tables, seq_lens, None, device)
+    # Only the entry of the last position is used.
+    tables_ptr, lens_ptr, batch, stride, _ = _batch(store, block_tables, seq_lens, None, device, window=1)
     k_ptr = _need(k, torch.bfloat16, "k", 3, device)
     v_ptr = _need(v, torch.bfloat16, "v", 3, device)
     if k.shape != v.shape or k.shape != (batch, store.h_kv, store.head_dim):

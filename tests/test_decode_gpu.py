@@ -326,3 +326,23 @@ def test_offsets_beyond_32_bits(gpu):
     binding.mocap_decode_append(store, tables, torch.tensor([257], dtype=torch.int32).cuda(), k, v)
     torch.cuda.synchronize()
     assert torch.equal(store.k_pool[blocks - 3, :, 0], k[0]) and torch.equal(store.v_pool[blocks - 3, :, :, 0], v[0])
+
+
+def test_table_checks_of_an_append(gpu):
+    """The entry of the last position alone: blocks that left a window may be gone."""
+    store, tables, _, _ = make_store(31, [200, 200], 64, 1, 64, fill=0.0)
+    tables[0, :3] = -1
+    k, v = randn(32, 2, 1, 64).cuda(), randn(33, 2, 1, 64).cuda()
+    binding.set_table_checks(True)
+    try:
+        with pytest.raises(binding.MocapError):
+            binding.mocap_decode_append(store, tables, torch.tensor([192, 0], dtype=torch.int32).cuda(), k, v)
+        torch.cuda.synchronize()
+        before = store.k_pool.clone()
+        binding.mocap_decode_append(store, tables, torch.tensor([193, 0], dtype=torch.int32).cuda(), k, v)
+    finally:
+        binding.set_table_checks(False)
+    torch.cuda.synchronize()
+    assert torch.equal(store.k_pool[tables[0, 3].long(), 0, 0], k[0, 0])
+    before[tables[0, 3].long(), 0, 0] = k[0, 0]
+    assert torch.equal(store.k_pool, before)
