@@ -364,11 +364,14 @@ __global__ __launch_bounds__(kDecodeThreads) void decode_join_kernel(const Decod
   acc = f32x4{};
 #pragma unroll
   for (int x = 0; x < kDecodeWaves; ++x) {
-    // A wavefront without parts, or whose parts have no keys, has a sum of 0.
-    const float f = wave_z[x] != 0.f ? expf(wave_m[x] - m) : 0.f;
-    z += f != 0.f ? f * wave_z[x] : 0.f;
+    // A wavefront without parts, or whose parts have no keys, has a sum of 0 and is left
+    // out.  A NaN part's maximum is not above the others', so its factor may be 0: it is
+    // the sum that tells whether the wavefront counts, and 0 times NaN reaches the result.
+    const bool counts = wave_z[x] != 0.f;
+    const float f = counts ? expf(wave_m[x] - m) : 0.f;
+    z += counts ? f * wave_z[x] : 0.f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] += f != 0.f ? f * wave_o[x][quad][e] : 0.f;
+    for (int e = 0; e < 4; ++e) acc[e] += counts ? f * wave_o[x][quad][e] : 0.f;
   }
   const float inv = z == 0.f ? 0.f : 1.f / z;
   bf16x4 out;

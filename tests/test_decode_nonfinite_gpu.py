@@ -1,0 +1,82 @@
+"""NaN and infinities in mocap_decode_attn: they reach exactly the rows that see
+them, whichever of a sequence's parts they lie in."""
+import math
+
+import pytest
+import torch
+
+from helpers import say
+from paper_2606_22968_amd import binding
+from serve_helpers import make_store, randn
+
+pytestmark = pytest.mark.gpu
+
+# Parts of four tiles at this load: 2 to 8 of them, and a sequence that is not cut.
+LENS = [256 * parts - 3 for parts in range(2, 9)] + [200]
+MAX_LEN = 2048
+HEADS = [(4, 2, 64), (4, 2, 128), (20, 1, 64), (20, 1, 128)]
+WINDOWS = [(0, 0), (1400, 70)]  # both wide enough for parts
+DIM = 9
+
+
+def attend(store, tables, lens, q, scale, window, sinks):
+    batch, h_q, d = q.shape
+    size = binding.mocap_decode_attn_workspace_size(batch, h_q, store.h_kv, d, MAX_LEN, window, sinks)
+    assert size > 0
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda").fill_(0xFF)
+    o = torch.empty((batch, h_q, d), dtype=torch.bfloat16, device="cuda")
+    lse = torch.empty((batch, h_q), dtype=torch.float32, device="cuda")
+    binding.mocap_decode_attn(store, tables, lens, q, MAX_LEN, scale, o, lse, ws, window, sinks)
+    return o.cpu(), lse.cpu()
+
+
+def sees(n, j, window, sinks):
+    return j < n and (window == 0 or j < sinks or j > n - 1 - window)
+
+
+def bits(x):
+    return x.contiguous().view(torch.int16 if x.dtype == torch.bfloat16 else torch.int32)
+
+
+def cases(h_q, h_kv, d, seed):
+    store, tables, ks, vs = make_store(seed, LENS, 64, h_kv, d)
+    q = randn(seed + 1, len(LENS), h_q, d)
+    # Even heads have a positive first dim, odd ones a negative one.
+    q[:, :, 0] = q[:, :, 0].abs() + 0.5
+    q[:, 1::2, 0] *= -1
+    return store, tables, torch.tensor(LENS, dtype=torch.int32).cuda(), q.cuda()
+
+
+@pytest.mark.parametrize("window,sinks", WINDOWS)
+@pytest.mark.parametrize("h_q,h_kv,d", HEADS)
+@pytest.mark.parametrize("kind", ["nan", "inf"])
+def test_a_nonfinite_key_in_every_tile(gpu, kind, h_q, h_kv, d, window, sinks):
+    """A key that is NaN, or whose score is +infinity for the even heads and -infinity for the odd ones, in one
+    tile of all sequences after the other: NaN in all of O and in the LSE of the heads with a NaN or +infinite
+    score, and of those alone."""
+    say(f"[case] decode {kind} key {h_q}/{h_kv}/{d} window={window} sinks={sinks}")
+    store, tables, lens, q = cases(h_q, h_kv, d, 400)
+    group = h_q // h_kv
+    o0, lse0 = attend(store, tables, lens, q, d ** -0.5, window, sinks)
+    assert torch.isfinite(o0.float()).all() and torch.isfinite(lse0).all()
+    for tile in range(MAX_LEN // 64):
+        j = tile * 64 + 5
+        rows = [b for b, n in enumerate(LENS) if j < n]
+        blocks = tables[rows, tile].long()
+        before = store.k_pool[blocks, 0, 5].clone()
+        if kind == "nan":
+            store.k_pool[blocks, 0, 5] = float("nan")
+        else:
+            store.k_pool[blocks, 0, 5, 0] = math.inf
+        o, lse = attend(store, tables, lens, q, d ** -0.5, window, sinks)
+        store.k_pool[blocks, 0, 5] = before
+        want = torch.zeros(len(LENS), h_q, dtype=torch.bool)
+        near = torch.zeros(len(LENS), h_q, dtype=torch.bool)  # heads that see the key
+        for b, n in enumerate(LENS):
+            if sees(n, j, window, sinks):
+                near[b, :group] = True
+                want[b, 0:group:1 if kind == "nan" else 2] = True
+        assert torch.equal(torch.isnan(lse), want), f"tile {tile}"
+        assert torch.equal(torch.isnan(o).all(-1), want) and torch.equal(torch.isnan(o).any(-1), want), f"tile {tile}"
+        assert torch.isfinite(lse[~want]).all() and torch.isfinite(o[~want].float()).all()
+        assert torch.equal(bits(o[~near]), bits(o0[~near])) and torch.equal(bits(lse[~near]), bits(lse0[~near]))
