@@ -125,11 +125,13 @@ __device__ __forceinline__ void put_always_kept(const EvictLaunch& p, const Outp
 // Writes those that stay of 1024 ROUNDS consecutive candidates, in order:
 // candidate r 1024 + tid is key[r], w[r] at position pos0 + r 1024 + tid, the
 // first `count` exist.  above and equal: how many candidates above the border and
-// equal to it have come before; moved on by this call.  at0: output position of
-// the first candidate that stays.
+// equal to it have come before; moved on by this call.  The candidates that stay
+// have the output positions at0 .. at0 + stay - 1, and nothing is written elsewhere:
+// in several launches each reads the weights anew, and weights that someone writes to
+// meanwhile can put more candidates above the border than were counted.
 template <int ROUNDS>
 __device__ __forceinline__ void compact(const uint32_t (&key)[ROUNDS], const float (&w)[ROUNDS], int pos0, int count,
-                                        const Border& border, int at0, uint32_t& above, uint32_t& equal,
+                                        const Border& border, int at0, uint32_t stay, uint32_t& above, uint32_t& equal,
                                         const Output& out) {
   constexpr int SLOTS = ROUNDS * kSelectWaves;
   static_assert(SLOTS <= kSelectThreads, "a thread for every (round, wave)");
@@ -183,7 +185,8 @@ __device__ __forceinline__ void compact(const uint32_t (&key)[ROUNDS], const flo
     const uint32_t gt_at = above + above_n[r * kSelectWaves + wave] + __builtin_popcountll(__builtin_amdgcn_ballot_w64(gt) & below);
     const uint32_t eq_at = equal + equal_n[r * kSelectWaves + wave] + __builtin_popcountll(__builtin_amdgcn_ballot_w64(eq) & below);
     // Of the equal ones the first `left` stay.
-    if (gt || (eq && eq_at < border.left)) out.put(at0 + (int)(gt_at + min(eq_at, border.left)), pos0 + i, w[r]);
+    const uint32_t at = gt_at + min(eq_at, border.left);
+    if ((gt || (eq && eq_at < border.left)) && at < stay) out.put(at0 + (int)at, pos0 + i, w[r]);
   }
   above += above_n[SLOTS];
   equal += equal_n[SLOTS];
@@ -208,7 +211,8 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const Evic
   for (int r = 0; r < ROUNDS; ++r) key[r] = weight_key(x[r]);
   const Output out = output_of(p, h);
   put_always_kept(p, out, w, tid, kSelectThreads);
-  Border border{0, (uint32_t)(p.keep - p.sinks - p.recent)};
+  const uint32_t stay = p.keep - p.sinks - p.recent;
+  Border border{0, stay};
   auto digit = [&](auto dd) __attribute__((always_inline)) {
     constexpr int d = decltype(dd)::value;
     for (int i = tid; i < bins(d); i += kSelectThreads) hist[i] = 0;
@@ -223,7 +227,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const Evic
   digit(std::integral_constant<int, 1>());
   digit(std::integral_constant<int, 2>());
   uint32_t above = 0, equal = 0;
-  compact<ROUNDS>(key, x, first, count, border, p.sinks, above, equal, out);
+  compact<ROUNDS>(key, x, first, count, border, p.sinks, stay, above, equal, out);
 }
 
 // ---- p.chunks workgroups per head ----
@@ -422,7 +426,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_compact_kernel(const Evi
       key[r] = weight_key(w[r]);
     }
     if (i0 + ROUNDS * kSelectThreads < x.end) load(i0 + ROUNDS * kSelectThreads);
-    compact<ROUNDS>(key, now, p.sinks + i0, count, border, p.sinks, above, equal, out);
+    compact<ROUNDS>(key, now, p.sinks + i0, count, border, p.sinks, p.keep - p.sinks - p.recent, above, equal, out);
   }
 }
 

@@ -213,3 +213,40 @@ def test_table_checks_refuse_a_shared_block(gpu):
         binding.set_table_checks(False)
     torch.cuda.synchronize()
     assert kept[0].tolist() == expected(weights[0].cpu(), 300, 70, 0, 0)
+
+
+def test_weights_written_to_meanwhile(gpu):
+    """Weights that another stream writes to while positions are chosen: which ones stay is then open, but nothing
+    is written outside the candidates' places of `kept` and `kept_weights`, and a later call is right."""
+    n, keep, sinks, recent, h_kv = 200000, 1000, 4, 64, 2
+    src, tables, ks, vs = make_store(340, [n], 256, h_kv, 64)
+    dst = binding.KvStore(6, 256, h_kv, 64, fill=7.0)
+    table = torch.tensor([3, 1, 4, 0], dtype=torch.int32).cuda()
+    few, many = torch.zeros(h_kv, n, device="cuda"), torch.full((h_kv, n), 2.0, device="cuda")
+    few[:, 5:2000] = 1.0
+    weights = few.clone()
+    # All that a head's candidates could be written to, had nothing stopped them.
+    kept_room = torch.full((h_kv * keep + n,), -7, dtype=torch.int32, device="cuda")
+    kw_room = torch.full((h_kv * keep + n,), -7.0, device="cuda")
+    kept, kw = kept_room[:h_kv * keep].view(h_kv, keep), kw_room[:h_kv * keep].view(h_kv, keep)
+    ws = torch.empty(binding.mocap_kv_evict_workspace_size(n, h_kv, keep), dtype=torch.uint8, device="cuda")
+    chooser, writer = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(100):
+        binding.mocap_kv_evict(src, tables[0], dst, table, n, keep, sinks, recent, weights, kept, kw, ws, stream=chooser)
+        with torch.cuda.stream(writer):
+            for _ in range(4):
+                weights.copy_(many)
+                weights.copy_(few)
+        with torch.cuda.stream(chooser):
+            # (One by one on the stream: the next call overwrites them.)
+            ends = kept[:, :sinks].clone(), kept[:, keep - recent:].clone()
+        chooser.synchronize()
+        assert (ends[0].cpu() == torch.arange(sinks, dtype=torch.int32)).all()
+        assert (ends[1].cpu() == torch.arange(n - recent, n, dtype=torch.int32)).all()
+    torch.cuda.synchronize()
+    assert (kept_room[h_kv * keep:] == -7).all() and (kw_room[h_kv * keep:] == -7.0).all()
+    weights.copy_(few)
+    binding.mocap_kv_evict(src, tables[0], dst, table, n, keep, sinks, recent, weights, kept, kw, ws)
+    torch.cuda.synchronize()
+    check(src, ks[0], vs[0], weights, n, keep, sinks, recent, dst, table, kept.cpu(), kw)
