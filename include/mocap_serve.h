@@ -19,6 +19,8 @@
  *     seq_lens holds; a sequence longer than max_len is taken to end there.
  *   - Block tables, lengths, positions and fp32 arrays (lse, weights) need only
  *     the alignment of their type, so rows of larger arrays may be passed.
+ *   - Outputs and the workspace must overlap no input and no other output, except
+ *     where a call says so, and inputs must stay as they are until a call is done.
  *   - Calls that are given a workspace share nothing else, so calls with
  *     different workspaces (and outputs) may run at the same time.  Two
  *     captured graphs whose replays can overlap need a workspace each.
@@ -216,7 +218,8 @@ mocap_status mocap_kv_evict_workspace_size(int64_t n, int32_t h_kv, int32_t keep
  *   n             positions (>= 0); 1 <= keep <= n, or n = keep = 0, a no-op;
  *                 sinks, recent >= 0, sinks + recent <= keep
  *   weights       device fp32 [h_kv][weight_stride], weight_stride >= n
- *   kept          device int32 [h_kv][keep]                           (output)
+ *   kept          device int32 [h_kv][keep]        (output; must overlap neither
+ *                 weights nor kept_weights)
  *   kept_weights  device fp32 [h_kv][keep], or NULL: the kept positions' weights
  *                 (output; must not overlap weights)
  *   workspace     device scratch of workspace_bytes, NULL when the size is 0

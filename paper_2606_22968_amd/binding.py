@@ -681,6 +681,10 @@ def mocap_key_weights_workspace_size(prefix_len: int, chunk_len: int, h_q: int, 
     return nbytes.value
 
 
+def _overlap(a: int, a_size: int, b: int, b_size: int) -> bool:
+    return a_size > 0 and b_size > 0 and a < b + b_size and b < a + a_size
+
+
 def _weights(prev: Optional[torch.Tensor], weights: torch.Tensor, shape: tuple, device: int):
     """The addresses of prev (or None) and weights, [*shape][stride] both; prev must be weights' memory exactly, or
     none of it."""
@@ -693,7 +697,7 @@ def _weights(prev: Optional[torch.Tensor], weights: torch.Tensor, shape: tuple, 
     if prev.shape != weights.shape:
         raise ValueError("prev must have the shape of weights")
     size = 4 * weights.numel()
-    if p_ptr != w_ptr and p_ptr < w_ptr + size and w_ptr < p_ptr + size:
+    if p_ptr != w_ptr and _overlap(p_ptr, size, w_ptr, size):
         raise ValueError("prev must be weights itself or not overlap it")
     return p_ptr, w_ptr
 
@@ -764,6 +768,10 @@ def mocap_kv_evict(src: KvStore, src_table: torch.Tensor, dst: KvStore, dst_tabl
         kw_ptr = _need(kept_weights, torch.float32, "kept_weights", 2, device)
         if kept_weights.shape != kept.shape:
             raise ValueError("kept_weights must be [h_kv][keep]")
+    # The positions are stored while the weights are still read.
+    size = 4 * kept.numel()
+    if _overlap(kept_ptr, size, w_ptr, 4 * weights.numel()) or (kw_ptr is not None and _overlap(kept_ptr, size, kw_ptr, size)):
+        raise ValueError("kept must not overlap weights or kept_weights")
     ws_ptr, ws_bytes = _workspace(workspace, device)
     _maybe_check(src, src_table, 0, int(n))
     _maybe_check(dst, dst_table, 0, int(keep))

@@ -250,3 +250,31 @@ def test_weights_written_to_meanwhile(gpu):
     binding.mocap_kv_evict(src, tables[0], dst, table, n, keep, sinks, recent, weights, kept, kw, ws)
     torch.cuda.synchronize()
     check(src, ks[0], vs[0], weights, n, keep, sinks, recent, dst, table, kept.cpu(), kw)
+
+
+def test_kept_on_the_weights_is_refused(gpu):
+    """Positions would be stored over weights that are still to be read."""
+    src, tables, _, _ = make_store(350, [500], 64, 2, 64)
+    dst = binding.KvStore(2, 64, 2, 64, fill=7.0)
+    table = torch.tensor([1, 0], dtype=torch.int32).cuda()
+    room = torch.rand(2 * 500 + 2 * 100, device="cuda")
+    before = room.clone()
+    weights, apart = room[:1000].view(2, 500), torch.zeros((2, 100), device="cuda")
+    for first in (0, 801, 999):
+        kept = room[first:first + 200].view(torch.int32).view(2, 100)
+        with pytest.raises(ValueError, match="overlap"):
+            binding.mocap_kv_evict(src, tables[0], dst, table, 500, 100, 4, 10, weights, kept, apart)
+    kept = torch.full((300,), -7, dtype=torch.int32, device="cuda")
+    as_floats = kept.view(torch.float32)
+    for at, kw_at in ((0, 100), (100, 0), (0, 0)):
+        with pytest.raises(ValueError, match="overlap"):
+            binding.mocap_kv_evict(src, tables[0], dst, table, 500, 100, 4, 10, weights, kept[at:at + 200].view(2, 100),
+                                   as_floats[kw_at:kw_at + 200].view(2, 100))
+    torch.cuda.synchronize()
+    assert torch.equal(room, before) and (kept == -7).all() and (dst.k_pool == 7.0).all()
+    # Right behind the weights.
+    kept = room[1000:].view(torch.int32).view(2, 100)
+    binding.mocap_kv_evict(src, tables[0], dst, table, 500, 100, 4, 10, weights, kept, apart)
+    torch.cuda.synchronize()
+    for h in range(2):
+        assert kept[h].tolist() == expected(weights[h].cpu(), 500, 100, 4, 10)
