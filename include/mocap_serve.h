@@ -89,9 +89,10 @@ mocap_status mocap_decode_attn_workspace_size(int32_t batch, int64_t max_len, in
  * fill the device, whatever the sequences' lengths are; the parts of a sequence
  * are joined by their log-sum-exp in a fixed order, so equal inputs give equal
  * bits.  A row without a sequence gives O = 0 and LSE = -infinity.  What hidden
- * or unwritten positions hold (NaN included) does not matter.  Scores, softmax
- * and partials are fp32; the probabilities enter the P*V product as the sum of
- * two bf16 values (2^-17 relative).
+ * or unwritten positions hold (NaN included) does not matter.  An infinite value
+ * is infinite in its dim of O for every row that sees it, NaN where both infinities
+ * meet.  Scores, softmax and partials are fp32; the probabilities enter the P*V
+ * product as the sum of two bf16 values (2^-17 relative).
  * Errors: as mocap_chunk_attn (INVALID_ARG also for a negative window or sinks,
  * a max_len beyond the tables, or null seq_lens); UNSUPPORTED also for a block of
  * 2^30 or more values per head, or batch * h_q of 2^23; WORKSPACE when the
@@ -122,7 +123,8 @@ mocap_status mocap_window_attn_workspace_size(int64_t prefix_len, int32_t chunk_
  *   window >= 1, sinks >= 0; other arguments, outputs and precision as in
  *   mocap_chunk_attn
  *
- * Non-finite keys and values reach exactly the rows that see them.  (Where the
+ * Non-finite keys and values reach exactly the rows that see them (an infinite
+ * value as infinity, or as NaN where its probability rounds to 0).  (Where the
  * window hides nothing, W >= P + L, mocap_chunk_attn gives the same rows in less
  * time, but a non-finite value there also reaches rows of its 64-key tile that do
  * not see it.)

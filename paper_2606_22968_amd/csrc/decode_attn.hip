@@ -21,7 +21,9 @@
 //     instruction takes 64 contiguous bytes of 16 rows, the rate of the vector
 //     cache, and nothing is used twice, so LDS has nothing to give.
 //   * MFMAs are busy 6% of the time, so precision is cheap: the probabilities go
-//     in as two bf16 values, p = hi + lo.
+//     in as two bf16 values, p = hi + lo.  lo is 0 or negative as often as not, which
+//     an infinite value turns into NaN or the other infinity; where an accumulator is
+//     not finite, the part's values are searched for what its dim gets by definition.
 // Measured: four sequences of 65537 to 131072 positions, 64/8/128 heads, 1.70 GB
 // in 293 us, 5.8 TB/s (a large copy runs at 5.1); 32 of 1 to 8192, 32/8/128, 340 MB
 // in 68 us and the join's 6; one of 572 positions, 9 us: lengths, table, keys and
@@ -73,6 +75,9 @@ __global__ __launch_bounds__(kDecodeThreads) void decode_attn_kernel(const Decod
   constexpr int MD = D / 16;  // 16-dim blocks of O
   __shared__ __attribute__((aligned(16))) float part_o[kDecodeWaves][NT * 16][D];
   __shared__ float part_m[kDecodeWaves][NT * 16], part_l[kDecodeWaves][NT * 16];
+  __shared__ uint32_t part_apart[kDecodeWaves];  // some accumulator is not finite
+  // What the part's values hold of each dim: 1 for +infinity, 2 for -infinity, both for NaN.
+  __shared__ uint32_t marks[D];
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -113,13 +118,18 @@ __global__ __launch_bounds__(kDecodeThreads) void decode_attn_kernel(const Decod
   struct Source {
     const uint16_t *k, *v;
   };
-  auto locate = [&](int i) __attribute__((always_inline)) {  // tile i of the part
-    const int pos = w.span.tile(begin + i) * kTileKeys;
+  // Position pos, the first of a tile: its slot, and the first element of its block's head.
+  auto find = [&](int pos, int* slot) __attribute__((always_inline)) {
     const int lb = (int)((__umulhi((uint32_t)pos, p.seqs.block_magic) + (uint32_t)pos) >> p.seqs.block_shift);
-    const int slot = pos - lb * bs;
-    const int64_t base = ((int64_t)table[lb] * p.h_kv + kv_head) * head_stride;
+    *slot = pos - lb * bs;
+    return ((int64_t)table[lb] * p.h_kv + kv_head) * head_stride;
+  };
+  auto locate = [&](int i) __attribute__((always_inline)) {  // tile i of the part
+    int slot;
+    const int64_t base = find(w.span.tile(begin + i) * kTileKeys, &slot);
     return Source{p.k_pool + base + (int64_t)slot * D + k_lane, p.v_pool + base + slot + v_lane};
   };
+  auto visible = [&](int key) { return key < w.span.len && (key < w.span.sink_end || key >= w.span.low); };
   bf16x8 k[4][KS], v[2][MD];  // of a tile: K by product, V by 32-key half
   auto fetch_k = [&](const uint16_t* src) __attribute__((always_inline)) {
 #pragma unroll
@@ -174,9 +184,7 @@ __global__ __launch_bounds__(kDecodeThreads) void decode_attn_kernel(const Decod
     if (key0 + kTileKeys > w.span.len || (key0 < w.span.low && key0 + kTileKeys > w.span.sink_end)) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const int key = key0 + (e >> 3) * 32 + g4 * 8 + (e & 7);
-        const bool seen = key < w.span.len && (key < w.span.sink_end || key >= w.span.low);
-        hidden |= seen ? 0u : 1u << e;
+        hidden |= visible(key0 + (e >> 3) * 32 + g4 * 8 + (e & 7)) ? 0u : 1u << e;
       }
       // What a hidden position holds may be NaN; its probability is 0.
 #pragma unroll
@@ -238,6 +246,7 @@ __global__ __launch_bounds__(kDecodeThreads) void decode_attn_kernel(const Decod
 
   // The wavefronts' partials meet in LDS.  Lane l holds head l % 16 and dims
   // 16 md + 4 (l / 16) .. + 3.
+  float probe = 0.f;  // NaN if some accumulator is not finite
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const float l = quad_rows_sum(l_run[t]);
@@ -246,10 +255,41 @@ __global__ __launch_bounds__(kDecodeThreads) void decode_attn_kernel(const Decod
       part_l[wave][t * 16 + l16] = l;
     }
 #pragma unroll
-    for (int md = 0; md < MD; ++md)
+    for (int md = 0; md < MD; ++md) {
       *reinterpret_cast<f32x4*>(&part_o[wave][t * 16 + l16][md * 16 + g4 * 4]) = oacc[t][md];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) probe = fmaf(oacc[t][md][e], 0.f, probe);
+    }
   }
+  const bool wave_apart = __builtin_amdgcn_ballot_w64(probe != probe) != 0;
+  if (lane == 0) part_apart[wave] = wave_apart;
+  if (tid < D) marks[tid] = 0;
   __syncthreads();
+  uint32_t apart = 0;
+#pragma unroll
+  for (int x = 0; x < kDecodeWaves; ++x) apart |= part_apart[x];
+  if (apart != 0) {  // the same for the whole workgroup
+    constexpr int SIDE = kDecodeThreads / D;  // tiles searched side by side
+    const int dim = tid % D;
+    uint32_t mark = 0;
+#pragma unroll 1
+    for (int i = tid / D; i < tiles; i += SIDE) {
+      const int key0 = w.span.tile(begin + i) * kTileKeys;
+      int slot;
+      const uint16_t* src = p.v_pool + find(key0, &slot) + (int64_t)dim * bs;
+#pragma unroll 1
+      for (int c = 0; c < kTileKeys; c += 8) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(src + slot + c);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t v = x[e / 2] >> (16 * (e & 1)) & 0xFFFFu;
+          if ((v & 0x7F80u) == 0x7F80u && visible(key0 + c + e)) mark |= (v & 0x7Fu) ? 3u : v >> 15 ? 2u : 1u;
+        }
+      }
+    }
+    if (mark != 0) atomicOr(&marks[dim], mark);
+    __syncthreads();
+  }
   constexpr int QUADS = D / 4;
   for (int i = tid; i < min(NT * 16, p.group - head0) * QUADS; i += kDecodeThreads) {
     const int row = i / QUADS, quad = i % QUADS;
@@ -272,6 +312,13 @@ __global__ __launch_bounds__(kDecodeThreads) void decode_attn_kernel(const Decod
     const float row_lse = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
     const int head = kv_head * p.group + head0 + row;
     acc *= inv;
+    if (apart != 0 && l > 0.f) {  // (a NaN score's row is NaN)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t mark = marks[quad * 4 + e];
+        if (mark != 0) acc[e] = mark == 1 ? INFINITY : mark == 2 ? -INFINITY : NAN;
+      }
+    }
     if (w.parts == 1) {
       const int64_t at = (int64_t)w.seq * p.h_q + head;
       bf16x4 v;
@@ -295,6 +342,15 @@ __global__ __launch_bounds__(kDecodeThreads) void decode_attn_kernel(const Decod
 // forms 64 weights together, and requests the partials of 8 (head_dim 128: 16)
 // parts at once, the first before any weight is known.  6 us for 4 sequences of 64
 // heads in 164 parts in all (14 with one wavefront for a row), and for 32 of 32 heads.
+
+// The weight of a part with keys is never 0, so that infinities and NaN in its O count
+// however far it lies below the others; the least fp32 value times a finite O adds
+// less than 5e-7.
+__device__ __forceinline__ float part_weight(float lse, float m) {
+  const float w = expf(lse - m);
+  return w == 0.f ? 1.4e-45f : w;
+}
+
 template <int D>
 __global__ __launch_bounds__(kDecodeThreads) void decode_join_kernel(const DecodeAttnLaunch p) {
   constexpr int QUADS = D / 4, SIDE = 64 / QUADS;  // parts read side by side
@@ -327,7 +383,7 @@ __global__ __launch_bounds__(kDecodeThreads) void decode_join_kernel(const Decod
   f32x4 acc = f32x4{};
   for (int r0 = begin; r0 < end; r0 += 64) {
     if (r0 > begin) lr = load_lse(r0 + lane);
-    const float weight = lr != -INFINITY ? expf(lr - m) : 0.f;  // NaN reaches the result
+    const float weight = lr != -INFINITY ? part_weight(lr, m) : 0.f;  // NaN reaches the result
     z += weight;
     const int n = min(64, end - r0);
     for (int i0 = 0; i0 < n; i0 += kAhead * SIDE) {
@@ -365,10 +421,10 @@ __global__ __launch_bounds__(kDecodeThreads) void decode_join_kernel(const Decod
 #pragma unroll
   for (int x = 0; x < kDecodeWaves; ++x) {
     // A wavefront without parts, or whose parts have no keys, has a sum of 0 and is left
-    // out.  A NaN part's maximum is not above the others', so its factor may be 0: it is
-    // the sum that tells whether the wavefront counts, and 0 times NaN reaches the result.
+    // out: not its factor tells, which is next to 0 where a NaN part has left the
+    // maximum to the other wavefronts.
     const bool counts = wave_z[x] != 0.f;
-    const float f = counts ? expf(wave_m[x] - m) : 0.f;
+    const float f = counts ? part_weight(wave_m[x], m) : 0.f;
     z += counts ? f * wave_z[x] : 0.f;
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[e] += counts ? f * wave_o[x][quad][e] : 0.f;

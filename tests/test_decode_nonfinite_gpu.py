@@ -80,3 +80,65 @@ def test_a_nonfinite_key_in_every_tile(gpu, kind, h_q, h_kv, d, window, sinks):
         assert torch.equal(torch.isnan(o).all(-1), want) and torch.equal(torch.isnan(o).any(-1), want), f"tile {tile}"
         assert torch.isfinite(lse[~want]).all() and torch.isfinite(o[~want].float()).all()
         assert torch.equal(bits(o[~near]), bits(o0[~near])) and torch.equal(bits(lse[~near]), bits(lse0[~near]))
+
+
+# Dim -> what two neighbouring keys hold there.
+VALUES = {DIM: (math.inf, None), 10: (None, -math.inf), 11: (math.inf, -math.inf), 12: (math.nan, None), 13: (math.inf, math.inf),
+          63: (-math.inf, None)}
+
+
+@pytest.mark.parametrize("window,sinks", WINDOWS)
+@pytest.mark.parametrize("h_q,h_kv,d", HEADS)
+def test_infinite_values_in_every_tile(gpu, h_q, h_kv, d, window, sinks):
+    """O is infinite where one infinity is seen, NaN where both or a NaN are, and the same bits as ever elsewhere."""
+    say(f"[case] decode infinite values {h_q}/{h_kv}/{d} window={window} sinks={sinks}")
+    store, tables, lens, q = cases(h_q, h_kv, d, 410)
+    group = h_q // h_kv
+    o0, lse0 = attend(store, tables, lens, q, d ** -0.5, window, sinks)
+    before = store.v_pool.clone()
+    for tile in range(MAX_LEN // 64):
+        first = tile * 64 + 30
+        for b, n in enumerate(LENS):
+            for i in range(2):
+                if first + i < n:
+                    for dim, values in VALUES.items():
+                        if values[i] is not None:
+                            store.v_pool[tables[b, tile].long(), h_kv - 1, dim, 30 + i] = values[i]
+        o, lse = attend(store, tables, lens, q, d ** -0.5, window, sinks)
+        assert torch.equal(bits(lse), bits(lse0)), f"tile {tile}"
+        want, heads = o0.clone().float(), slice(h_q - group, h_q)
+        for b, n in enumerate(LENS):
+            for dim, values in VALUES.items():
+                seen = [v for i, v in enumerate(values) if v is not None and sees(n, first + i, window, sinks)]
+                if seen:
+                    want[b, heads, dim] = sum(seen)
+        same = (o.float() == want) | (torch.isnan(o) & torch.isnan(want))
+        assert same.all(), f"tile {tile}: {same.logical_not().nonzero()[:4].tolist()}"
+        store.v_pool.copy_(before)
+
+
+@pytest.mark.parametrize("h_q,h_kv,d", HEADS)
+def test_values_of_the_smallest_weights(gpu, h_q, h_kv, d):
+    """Infinite and NaN values of keys whose probability is nothing in fp32 reach O all the same."""
+    say(f"[case] decode values of the smallest weights {h_q}/{h_kv}/{d}")
+    store, tables, ks, vs = make_store(420, [2048], 64, h_kv, d)
+    q = torch.zeros(1, h_q, d, dtype=torch.bfloat16)
+    q[:, 0::2, 0], q[:, 1::2, 0] = 1.0, -1.0
+    # Scores of -150 to 150 and back: exp(-300) is 0 in fp32.
+    ramp = torch.linspace(-150, 150, 2048).to(torch.bfloat16).view(32, 64).cuda()
+    for tile in range(32):
+        store.k_pool[tables[0, tile].long(), :, :, 0] = ramp[tile]
+    lens = torch.tensor([2048], dtype=torch.int32).cuda()
+    o0, lse0 = attend(store, tables, lens, q.cuda(), 1.0, 0, 0)
+    assert torch.isfinite(o0.float()).all()
+    for tile in (0, 15, 31):
+        pool = store.v_pool[tables[0, tile].long()]
+        before = pool.clone()
+        pool[:, DIM, 40], pool[:, 10, 41], pool[:, 11, 42] = math.inf, -math.inf, math.nan
+        store.v_pool[tables[0, tile].long()] = pool
+        o, lse = attend(store, tables, lens, q.cuda(), 1.0, 0, 0)
+        store.v_pool[tables[0, tile].long()] = before
+        assert torch.equal(bits(lse), bits(lse0))
+        assert (o[:, :, DIM] == math.inf).all() and (o[:, :, 10] == -math.inf).all() and torch.isnan(o[:, :, 11]).all()
+        o[:, :, DIM:12] = o0[:, :, DIM:12]
+        assert torch.equal(bits(o), bits(o0))
