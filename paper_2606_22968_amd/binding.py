@@ -577,8 +577,9 @@ def _store_on(store: KvStore, device: int) -> mocap_kv_store:
 
 
 def _batch(store: KvStore, block_tables: torch.Tensor, seq_lens: torch.Tensor, max_len: Optional[int], device: int,
-           window: int = 0, sinks: int = 0):
-    """Checks a batch's tables and lengths; returns their addresses, batch, table_stride and max_len."""
+           window: int = 0, sinks: int = 0, skip_longer: bool = False):
+    """Checks a batch's tables and lengths; returns their addresses, batch, table_stride and max_len.  A sequence longer
+    than max_len ends there, or with skip_longer is none."""
     tables_ptr = _need(block_tables, torch.int32, "block_tables", 2, device)
     lens_ptr = _need(seq_lens, torch.int32, "seq_lens", 1, device)
     batch, stride = block_tables.shape
@@ -587,7 +588,7 @@ def _batch(store: KvStore, block_tables: torch.Tensor, seq_lens: torch.Tensor, m
     max_len = min(stride * store.block_size, (1 << 31) - 128) if max_len is None else int(max_len)
     if _check_tables:
         for table, n in zip(block_tables.cpu(), seq_lens.tolist()):
-            n = min(n, max_len)
+            n = 0 if skip_longer and n > max_len else min(n, max_len)
             low = max(0, n - window) if window > 0 else 0
             mocap_check_block_table(table, 0, max(0, min(sinks, low)), store.block_size, store.num_blocks)
             mocap_check_block_table(table, low, max(low, n), store.block_size, store.num_blocks)
@@ -598,8 +599,8 @@ def mocap_decode_append(store: KvStore, block_tables: torch.Tensor, seq_lens: to
                         v: torch.Tensor, stream=None) -> None:
     """Stores row b of k and v (bf16 [batch][h_kv][head_dim]) at position seq_lens[b] - 1 of sequence b."""
     device = _raw_device()
-    # Only the entry of the last position is used.
-    tables_ptr, lens_ptr, batch, stride, _ = _batch(store, block_tables, seq_lens, None, device, window=1)
+    # Only the entry of the last position is used, and none of a sequence that the tables do not hold.
+    tables_ptr, lens_ptr, batch, stride, _ = _batch(store, block_tables, seq_lens, None, device, window=1, skip_longer=True)
     k_ptr = _need(k, torch.bfloat16, "k", 3, device)
     v_ptr = _need(v, torch.bfloat16, "v", 3, device)
     if k.shape != v.shape or k.shape != (batch, store.h_kv, store.head_dim):

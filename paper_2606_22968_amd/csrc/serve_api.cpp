@@ -124,10 +124,12 @@ void set_tables(const mocap_kv_store* kv, const int32_t* block_tables, int32_t t
 }
 
 #ifdef MOCAP_DEBUG_TABLES
-// Every entry that the visible positions of a sequence use names a block.
-// Sequences may share blocks.
+// Every entry that the visible positions of a sequence use names a block; a sequence
+// longer than max_len ends there, or with skip_longer uses none.  Sequences may share
+// blocks.
 mocap_status debug_check_batch(const mocap_kv_store* kv, const int32_t* block_tables, int32_t table_stride,
-                               const int32_t* seq_lens, int32_t batch, int64_t max_len, int64_t window, int64_t sinks) {
+                               const int32_t* seq_lens, int32_t batch, int64_t max_len, int64_t window, int64_t sinks,
+                               bool skip_longer = false) {
   const int64_t entries = (int64_t)batch * table_stride;
   std::unique_ptr<int32_t[]> host(new (std::nothrow) int32_t[entries + batch]);
   if (!host) return MOCAP_ERR_UNSUPPORTED;
@@ -135,6 +137,7 @@ mocap_status debug_check_batch(const mocap_kv_store* kv, const int32_t* block_ta
       hipMemcpy(host.get() + entries, seq_lens, batch * sizeof(int32_t), hipMemcpyDeviceToHost) != hipSuccess)
     return MOCAP_ERR_HIP;
   for (int32_t b = 0; b < batch; ++b) {
+    if (skip_longer && host[entries + b] > max_len) continue;
     const int64_t n = std::min<int64_t>(host[entries + b], max_len);
     const int64_t low = window > 0 ? std::max<int64_t>(0, n - window) : 0;
     for (int64_t lb = 0; lb * kv->block_size < n; ++lb) {
@@ -348,7 +351,8 @@ mocap_status mocap_decode_append(const mocap_kv_store* kv, const int32_t* block_
   if (st != MOCAP_OK || batch == 0) return st;
   if (!k || !v || !aligned16(k) || !aligned16(v)) return MOCAP_ERR_INVALID_ARG;
   if (batch > kMaxGroups || (int64_t)kv->h_kv * (kv->head_dim / 8) > 65535 * 64) return MOCAP_ERR_UNSUPPORTED;
-  MOCAP_DEBUG_CHECK_BATCH(kv, block_tables, table_stride, seq_lens, batch, (int64_t)table_stride * kv->block_size, 1, 0);
+  MOCAP_DEBUG_CHECK_BATCH(kv, block_tables, table_stride, seq_lens, batch, (int64_t)table_stride * kv->block_size, 1, 0,
+                          true);
   mocap::DecodeAppendLaunch p;
   p.k = static_cast<const uint16_t*>(k);
   p.v = static_cast<const uint16_t*>(v);

@@ -346,3 +346,19 @@ def test_table_checks_of_an_append(gpu):
     assert torch.equal(store.k_pool[tables[0, 3].long(), 0, 0], k[0, 0])
     before[tables[0, 3].long(), 0, 0] = k[0, 0]
     assert torch.equal(store.k_pool, before)
+
+
+def test_table_checks_of_an_append_beyond_the_tables(gpu):
+    """Nothing is written for a sequence that the tables do not hold: no entry of its is looked at."""
+    store, tables, _, _ = make_store(34, [192, 192], 64, 1, 64, fill=0.0)
+    tables[0] = -1
+    k, v = randn(35, 2, 1, 64).cuda(), randn(36, 2, 1, 64).cuda()
+    before = store.k_pool.clone()
+    binding.set_table_checks(True)
+    try:
+        binding.mocap_decode_append(store, tables, torch.tensor([193, 192], dtype=torch.int32).cuda(), k, v)
+    finally:
+        binding.set_table_checks(False)
+    torch.cuda.synchronize()
+    before[tables[1, 2].long(), 0, 63] = k[1, 0]
+    assert torch.equal(store.k_pool, before)

@@ -387,3 +387,12 @@ def test_debug_build_checks_the_tables(mocap_lib, tmp_path):
         assert evict(lib, src=kv, src_table=ints(*table), n_src=3, n=700, keep=300, dst_table=ints(0, 1)) == status
     assert window(lib, kv=kv, table=ints(0, 9, 2), n_table=3, P=650, L=50, window=100) == 0
     assert evict(lib, src=kv, src_table=ints(0, 1, 2), n_src=3, n=700, keep=300, dst=kv, dst_table=ints(0, 4)) == INVALID
+
+
+def test_debug_build_skips_appends_beyond_the_tables(mocap_lib, tmp_path):
+    """Nothing is written for a sequence that the tables do not hold, so no entry of its is looked at."""
+    lib = recording_build(mocap_lib, tmp_path, "-DMOCAP_DEBUG_TABLES")
+    table, args = (ctypes.c_int32 * 6)(0, 1, -1, 0, 1, 2), dict(kv=store(num_blocks=4), stride=3, batch=2)
+    for lens, status in (((769, 700), 0), ((1 << 30, 1), 0), ((768, 700), INVALID), ((512, 769), 0)):
+        lens = (ctypes.c_int32 * 2)(*lens)
+        assert append(lib, tables=ctypes.addressof(table), lens=ctypes.addressof(lens), **args) == status
