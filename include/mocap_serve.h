@@ -107,7 +107,9 @@ mocap_status mocap_decode_attn(const mocap_kv_store* kv, const int32_t* block_ta
  * mocap_window_attn_workspace_size -- the range count and workspace bytes of
  * mocap_window_attn.  num_splits as a request: 1 = one range, n >= 2 = the tiles
  * that any row of a workgroup sees cut into n ranges, 0 = chosen from the shape.
- * A request is clamped to the number of tiles.  splits_out may be NULL.
+ * A request is clamped to the tiles that a workgroup's windows and sinks can touch
+ * wherever in a tile they begin: at most two more than they do touch, and the ranges
+ * that are then empty cost their workspace only.  splits_out may be NULL.
  * Errors: as mocap_chunk_attn_workspace_size; INVALID_ARG for window < 1 or
  * sinks < 0.
  */

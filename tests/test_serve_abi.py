@@ -396,3 +396,30 @@ def test_debug_build_skips_appends_beyond_the_tables(mocap_lib, tmp_path):
     for lens, status in (((769, 700), 0), ((1 << 30, 1), 0), ((768, 700), INVALID), ((512, 769), 0)):
         lens = (ctypes.c_int32 * 2)(*lens)
         assert append(lib, tables=ctypes.addressof(table), lens=ctypes.addressof(lens), **args) == status
+
+
+def window_tiles(P, L, group, win, sinks):
+    """Tiles that some row of a workgroup of 256 rows sees, for the workgroup with the most."""
+    most = 0
+    for row in range(0, L * group, 256):
+        first, last = P + row // group, P + min(row + 255, L * group - 1) // group
+        low = max(0, first - win + 1)
+        most = max(most, len({j // 64 for j in range(last + 1) if j >= low or j < sinks}))
+    return most
+
+
+def test_window_range_requests(host):
+    """A request is met up to the number of tiles, and exceeds it by two at most."""
+    rng = random.Random(8)
+    for _ in range(300):
+        P, L = rng.choice((0, 1, 63, 64, 700, 2001)), rng.choice((1, 2, 31, 100, 300))
+        group, win = rng.choice((1, 3, 4, 64)), rng.choice((1, 2, 64, 65, 100, 1100, 5000))
+        sinks = rng.choice((0, 1, 64, 70, 300, 9999))
+        tiles = window_tiles(P, L, group, win, sinks)
+        for splits in (1, 2, 3, tiles - 1, tiles, tiles + 1, tiles + 2, tiles + 3, 1 << 30):
+            if splits < 1:
+                continue
+            n, size = ctypes.c_int32(0), ctypes.c_size_t(0)
+            assert host.mocap_window_attn_workspace_size(P, L, 2 * group, 2, 128, win, sinks, splits, ctypes.byref(n),
+                                                         ctypes.byref(size)) == 0
+            assert min(splits, tiles) <= n.value <= min(splits, tiles + 2)
