@@ -278,3 +278,32 @@ def test_kept_on_the_weights_is_refused(gpu):
     torch.cuda.synchronize()
     for h in range(2):
         assert kept[h].tolist() == expected(weights[h].cpu(), 500, 100, 4, 10)
+
+
+@pytest.mark.parametrize("kind", ["heavy", "ties", "special"])
+@pytest.mark.parametrize("sinks,recent", [(0, 0), (4, 33)])
+@pytest.mark.parametrize("candidates", [1, 1024, 4095, 4096, 4097, 16383, 16384, 16385])
+def test_candidates_at_the_dispatch_borders(gpu, candidates, sinks, recent, kind):
+    """Four or sixteen candidates a thread of one workgroup, or chunks."""
+    say(f"[case] evict candidates={candidates} sinks={sinks} recent={recent} {kind}")
+    n = candidates + sinks + recent
+    src, tables, ks, vs = make_store(360, [n], 256, 2, 64)
+    weights = weights_of(kind, 2, n, 361)
+    keep = sinks + recent + max(1, candidates // 5)
+    out = evict(src, tables[0], weights, n, keep, sinks, recent)
+    check(src, ks[0], vs[0], weights, n, keep, sinks, recent, *out)
+
+
+@pytest.mark.parametrize("n,sinks,recent,chosen", [
+    (20000, 4, 16000, 100),   # few candidates of many positions: a workspace that is not used
+    (20000, 10000, 9000, 1), (20000, 4, 18000, 0), (40000, 3, 64, 0), (40000, 20000, 3616, 0), (40000, 20000, 3616, 16384),
+    (40000, 20000, 3615, 16384), (40000, 64, 0, 39936)])
+@pytest.mark.parametrize("kind", ["heavy", "special", "equal"])
+def test_many_positions_kept_whatever_they_weigh(gpu, n, sinks, recent, chosen, kind):
+    """Many sinks and recent positions, and few, no or all candidates chosen."""
+    say(f"[case] evict n={n} sinks={sinks} recent={recent} chosen={chosen} {kind}")
+    src, tables, ks, vs = make_store(362, [n], 256, 1, 64)
+    weights = weights_of(kind, 1, n, 363)
+    keep = sinks + recent + chosen
+    out = evict(src, tables[0], weights, n, keep, sinks, recent)
+    check(src, ks[0], vs[0], weights, n, keep, sinks, recent, *out)
