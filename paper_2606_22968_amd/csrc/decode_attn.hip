@@ -249,7 +249,9 @@ __global__ __launch_bounds__(kDecodeThreads) void decode_attn_kernel(const Decod
   float probe = 0.f;  // NaN if some accumulator is not finite
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    const float l = quad_rows_sum(l_run[t]);
+    // A score whose product with the scale is beyond fp32 makes every other exponential
+    // 0 and its own too; the row is NaN, as with an infinite score.
+    const float l = m_run[t] == INFINITY ? NAN : quad_rows_sum(l_run[t]);
     if (g4 == 0) {
       part_m[wave][t * 16 + l16] = m_run[t];
       part_l[wave][t * 16 + l16] = l;

@@ -451,9 +451,12 @@ __global__ __launch_bounds__(kAttnThreads, 2) void window_attn_kernel(const Wind
     if (pending) pv(i1 - 1);
   }
 
-  const float l_tot = lane_pair_sum(l_run), f_tot = lane_pair_sum(f_run);
+  // A score whose product with the scale is beyond fp32 makes every exponential 0, its
+  // own too; the row is NaN, as with an infinite score.
+  const bool beyond = m_run == INFINITY;
+  const float l_tot = lane_pair_sum(l_run), f_tot = beyond ? NAN : lane_pair_sum(f_run);
   if (row0 + l32 >= rows_end) return;
-  const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+  const float inv = beyond ? NAN : l_tot > 0.f ? 1.f / l_tot : 0.f;
   const float row_lse = f_tot == 0.f ? -INFINITY : (m_run + log2f(f_tot)) * kLn2;
   const int64_t out_row = (int64_t)token * p.h_q + head;
   const int64_t part_row = (int64_t)range * L * p.h_q + out_row;

@@ -142,3 +142,21 @@ def test_values_of_the_smallest_weights(gpu, h_q, h_kv, d):
         assert (o[:, :, DIM] == math.inf).all() and (o[:, :, 10] == -math.inf).all() and torch.isnan(o[:, :, 11]).all()
         o[:, :, DIM:12] = o0[:, :, DIM:12]
         assert torch.equal(bits(o), bits(o0))
+
+
+@pytest.mark.parametrize("h_q,h_kv,d", HEADS)
+def test_scores_beyond_fp32(gpu, h_q, h_kv, d):
+    """Products within fp32 whose multiple by the scale is not: NaN, as with an infinite score, and not an empty row."""
+    say(f"[case] decode scores beyond fp32 {h_q}/{h_kv}/{d}")
+    store, tables, lens, q = cases(h_q, h_kv, d, 430)
+    q[:, :, 0] = torch.where(q[:, :, 0] > 0, 1e19, q[:, :, 0])
+    for tile in (0, 3, 17, 31):
+        rows = [b for b, n in enumerate(LENS) if tile * 64 + 5 < n]
+        blocks = tables[rows, tile].long()
+        store.k_pool[:, :, :, 0] = 0.0
+        store.k_pool[blocks, :, 5, 0] = 1e19  # 1e38, and 4e38 with the scale
+        o, lse = attend(store, tables, lens, q, 4.0, 0, 0)
+        want = torch.zeros(len(LENS), h_q, dtype=torch.bool)
+        want[rows, 0::2] = True
+        assert torch.equal(torch.isnan(lse), want) and torch.isfinite(lse[~want]).all(), f"tile {tile}"
+        assert torch.equal(torch.isnan(o).all(-1), want) and torch.isfinite(o[~want].float()).all(), f"tile {tile}"

@@ -240,3 +240,22 @@ def test_empty_chunk(gpu):
     q = torch.zeros((0, 4, 64), dtype=torch.bfloat16, device="cuda")
     binding.mocap_window_attn(store, torch.zeros(2, dtype=torch.int32, device="cuda"), q, 100, 0.1, 5, 1, q.clone(),
                               torch.zeros((4, 0), device="cuda"))
+
+
+@pytest.mark.parametrize("splits", [1, 3])
+@pytest.mark.parametrize("d", [64, 128])
+def test_scores_beyond_fp32(gpu, splits, d):
+    """Products within fp32 whose multiple by the scale is not: NaN, as with an infinite score, and not an empty row."""
+    prefix, rows, window, sinks, h_q, h_kv = 600, 300, 150, 5, 4, 2
+    store, tables, _, _ = make_store(121, [prefix + rows], 64, h_kv, d)
+    store.k_pool[:, :, :, 0] = 0.0
+    want = torch.zeros(rows, h_q, dtype=torch.bool)
+    t = prefix + torch.arange(rows)
+    for j in (500, 640, 831):
+        store.k_pool[tables[0, j // 64].long(), :, j % 64, 0] = 1e19  # 1e38, and 4e38 with the scale
+        want[(j <= t) & (j > t - window), 0::2] = True
+    q = randn(122, rows, h_q, d)
+    q[:, 0::2, 0], q[:, 1::2, 0] = 1e19, -1.0
+    o, lse, _ = attend(store, tables[0], q.cuda(), prefix, 4.0, window, sinks, splits)
+    assert torch.equal(torch.isnan(lse.cpu()).t(), want) and torch.isfinite(lse.cpu().t()[~want]).all()
+    assert torch.equal(torch.isnan(o.cpu()).all(-1), want) and torch.isfinite(o.cpu()[~want].float()).all()
