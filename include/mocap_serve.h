@@ -159,7 +159,8 @@ mocap_status mocap_key_weights_workspace_size(int64_t prefix_len, int32_t chunk_
  *   kv, block_table, n_table, q, prefix_len P, chunk_len L, h_q, h_kv, head_dim,
  *   scale         as in mocap_chunk_attn; only keys are read
  *   lse           device fp32 [h_q][L], natural log: that of mocap_chunk_attn for
- *                 these rows.  A row whose LSE is -infinity adds nothing.
+ *                 these rows.  A row whose LSE is -infinity (every score of it is) adds
+ *                 nothing; a NaN score or LSE makes the weight of the keys it meets NaN
  *   prev          device fp32 [h_kv][weight_stride], or NULL: 0 everywhere; may be
  *                 `weights` itself, and must not overlap it otherwise
  *   weights       device fp32 [h_kv][weight_stride], weight_stride >= P + L (output;

@@ -18,7 +18,10 @@
 //   * Products, softmax bookkeeping and outputs are those of chunk_attn.hip:
 //     S^T = K Q^T and O^T += V^T P^T with v_mfma_f32_32x32x16_bf16, the
 //     probabilities rounded to bf16 (their bf16 sum normalises O, the fp32 sum of
-//     the exponentials gives the LSE).
+//     the exponentials gives the LSE).  A layer's windowed and full rows then have
+//     one precision (O 0.0023 of its norm from 64 bits; 0.0017, its own rounding, with
+//     exact probabilities), and a low part beside them, as in decode_attn.hip, would
+//     double the P*V products of a kernel that is bound by issue.
 //   * A wavefront makes tile k's scores, then tile k - 1's P*V with tile k's
 //     exponentials, packing and row sums woven in between the MFMAs.
 //   * Tiles that some row of the workgroup does not see in full are masked.  A
