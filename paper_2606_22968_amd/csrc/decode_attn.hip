@@ -23,7 +23,8 @@
 //   * MFMAs are busy 6% of the time, so precision is cheap: the probabilities go
 //     in as two bf16 values, p = hi + lo.  lo is 0 or negative as often as not, which
 //     an infinite value turns into NaN or the other infinity; where an accumulator is
-//     not finite, the part's values are searched for what its dim gets by definition.
+//     not finite, the part's values are searched for what its dim gets by definition
+//     (an infinity in every block of the four long sequences below: 483 us for 299).
 // Measured: four sequences of 65537 to 131072 positions, 64/8/128 heads, 1.70 GB
 // in 293 us, 5.8 TB/s (a large copy runs at 5.1); 32 of 1 to 8192, 32/8/128, 340 MB
 // in 68 us and the join's 6; one of 572 positions, 9 us: lengths, table, keys and
@@ -279,14 +280,13 @@ __global__ __launch_bounds__(kDecodeThreads) void decode_attn_kernel(const Decod
       const int key0 = w.span.tile(begin + i) * kTileKeys;
       int slot;
       const uint16_t* src = p.v_pool + find(key0, &slot) + (int64_t)dim * bs;
-#pragma unroll 1
-      for (int c = 0; c < kTileKeys; c += 8) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(src + slot + c);
+      u32x4 x[kTileKeys / 8];  // all loads in flight
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const uint32_t v = x[e / 2] >> (16 * (e & 1)) & 0xFFFFu;
-          if ((v & 0x7F80u) == 0x7F80u && visible(key0 + c + e)) mark |= (v & 0x7Fu) ? 3u : v >> 15 ? 2u : 1u;
-        }
+      for (int c = 0; c < kTileKeys / 8; ++c) x[c] = *reinterpret_cast<const u32x4*>(src + slot + c * 8);
+#pragma unroll
+      for (int e = 0; e < kTileKeys; ++e) {
+        const uint32_t v = x[e / 8][e / 2 % 4] >> (16 * (e & 1)) & 0xFFFFu;
+        if ((v & 0x7F80u) == 0x7F80u && visible(key0 + e)) mark |= (v & 0x7Fu) ? 3u : v >> 15 ? 2u : 1u;
       }
     }
     if (mark != 0) atomicOr(&marks[dim], mark);
