@@ -58,6 +58,19 @@ SERVE_EXPORTED = (
     "mocap_kv_evict",
 )
 
+# Every entry point mocap_cache.h declares.
+CACHE_EXPORTED = (
+    "mocap_rope_append",
+    "mocap_decode_rope_append",
+    "mocap_kv4_append",
+    "mocap_kv4_decode_append",
+    "mocap_kv4_load",
+    "mocap_kv4_decode_attn_workspace_size",
+    "mocap_kv4_decode_attn",
+    "mocap_kv4_chunk_attn_workspace_size",
+    "mocap_kv4_chunk_attn",
+)
+
 
 class mocap_lbcp_serving(ctypes.Structure):
     _fields_ = [
@@ -84,6 +97,27 @@ class mocap_kv_store(ctypes.Structure):
         ("block_size", ctypes.c_int32),
         ("h_kv", ctypes.c_int32),
         ("head_dim", ctypes.c_int32),
+    ]
+
+
+class mocap_kv4_store(ctypes.Structure):
+    _fields_ = [
+        ("k_pool", ctypes.c_void_p),
+        ("v_pool", ctypes.c_void_p),
+        ("k_scale", ctypes.c_void_p),
+        ("v_scale", ctypes.c_void_p),
+        ("num_blocks", ctypes.c_int32),
+        ("block_size", ctypes.c_int32),
+        ("h_kv", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+    ]
+
+
+class mocap_rope(ctypes.Structure):
+    _fields_ = [
+        ("inv_freq", ctypes.c_void_p),
+        ("rot_dim", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
     ]
 
 
@@ -202,6 +236,20 @@ def load_library():
                                   ptr],
         mocap_kv_evict_workspace_size=[i64, i32, i32, size_out],
         mocap_kv_evict=[store, ptr, i32, store, ptr, i32, i64, i32, i32, i32, ptr, i64, ptr, ptr, ptr, size, ptr],
+    )
+    store4, rope = ctypes.POINTER(mocap_kv4_store), ctypes.POINTER(mocap_rope)
+    rows = [ptr, i64, i32, ptr, i64, ptr, i64, ptr, ptr]
+    attn = [ctypes.c_float, i64, i64, ptr, ptr, ptr, size]
+    serve.update(
+        mocap_rope_append=[store, ptr, i32, i64, i32, rope, i64, *rows],
+        mocap_decode_rope_append=[store, ptr, i32, ptr, i32, rope, ptr, *rows],
+        mocap_kv4_append=[store4, ptr, i32, i64, i32, rope, i64, *rows],
+        mocap_kv4_decode_append=[store4, ptr, i32, ptr, i32, rope, ptr, *rows],
+        mocap_kv4_load=[store4, ptr, i32, ptr, i32, i32, ptr, ptr, ptr],
+        mocap_kv4_decode_attn_workspace_size=[i32, i64, i32, i32, i32, i64, i64, size_out],
+        mocap_kv4_decode_attn=[store4, ptr, i32, ptr, i32, i64, ptr, i32, i32, i32, *attn, ptr],
+        mocap_kv4_chunk_attn_workspace_size=[i64, i32, i32, i32, i32, i64, i64, i32, ctypes.POINTER(i32), size_out],
+        mocap_kv4_chunk_attn=[store4, ptr, i32, ptr, i64, i32, i32, i32, i32, *attn, i32, ptr],
     )
     for name, argtypes in serve.items():
         f = getattr(lib, name)
@@ -785,3 +833,245 @@ def mocap_kv_evict(src: KvStore, src_table: torch.Tensor, dst: KvStore, dst_tabl
         ctypes.byref(from_desc), src_ptr, src_table.shape[0], ctypes.byref(to_desc), dst_ptr, dst_table.shape[0], int(n),
         int(keep), int(sinks), int(recent), w_ptr, weights.shape[1], kept_ptr, kw_ptr, ws_ptr, ws_bytes,
         _stream_on(stream, device)), "mocap_kv_evict")
+
+
+# ---- Rotating appends and the 4-bit store (mocap_cache.h) ----
+
+class Rope:
+    """A rotation: inv_freq fp32 [rot_dim / 2] on the GPU, radians a position; pairs are dims (i, i + rot_dim / 2), or
+    (2 i, 2 i + 1) if interleaved."""
+
+    def __init__(self, inv_freq: torch.Tensor, interleaved: bool = False):
+        _require(inv_freq, torch.float32, "inv_freq", 1)
+        self.inv_freq, self.interleaved = inv_freq, bool(interleaved)
+
+    @property
+    def rot_dim(self) -> int:
+        return 2 * self.inv_freq.shape[0]
+
+    def descriptor(self) -> mocap_rope:
+        return mocap_rope(self.inv_freq.data_ptr(), self.rot_dim, int(self.interleaved))
+
+
+class Kv4Store:
+    """Caller-owned pools of a 4-bit store (uint8, torch device memory) plus the C descriptor.
+
+    k_pool: [num_blocks][h_kv][block_size][head_dim / 2]
+    v_pool: [num_blocks][h_kv][block_size / 64][head_dim / 2][64]
+    k_scale, v_scale: [num_blocks][h_kv][block_size / 64][head_dim / 32][64]
+    """
+
+    def __init__(self, num_blocks: int, block_size: int, h_kv: int, head_dim: int,
+                 device="cuda", fill: Optional[int] = None):
+        self.num_blocks, self.block_size, self.h_kv, self.head_dim = num_blocks, block_size, h_kv, head_dim
+        tiles = (num_blocks, h_kv, block_size // 64)
+        self.k_pool = torch.empty((num_blocks, h_kv, block_size, head_dim // 2), dtype=torch.uint8, device=device)
+        self.v_pool = torch.empty((*tiles, head_dim // 2, 64), dtype=torch.uint8, device=device)
+        self.k_scale = torch.empty((*tiles, head_dim // 32, 64), dtype=torch.uint8, device=device)
+        self.v_scale = torch.empty((*tiles, head_dim // 32, 64), dtype=torch.uint8, device=device)
+        if fill is not None:
+            for pool in (self.k_pool, self.v_pool, self.k_scale, self.v_scale):
+                pool.fill_(fill)
+
+    def descriptor(self) -> mocap_kv4_store:
+        return mocap_kv4_store(self.k_pool.data_ptr(), self.v_pool.data_ptr(), self.k_scale.data_ptr(),
+                               self.v_scale.data_ptr(), self.num_blocks, self.block_size, self.h_kv, self.head_dim)
+
+
+def _store4_on(store: Kv4Store, device: int) -> mocap_kv4_store:
+    """The store's descriptor, of pools on the current device."""
+    _need(store.k_pool, torch.uint8, "k_pool", 4, device)
+    _need(store.v_pool, torch.uint8, "v_pool", 5, device)
+    _need(store.k_scale, torch.uint8, "k_scale", 5, device)
+    _need(store.v_scale, torch.uint8, "v_scale", 5, device)
+    return store.descriptor()
+
+
+def _rows(t: torch.Tensor, name: str, device: int):
+    """The address and token stride of a bf16 [tokens][heads][head_dim] tensor on the current device whose tokens' values
+    are contiguous."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype is not torch.bfloat16:
+        raise TypeError(f"{name} must be {torch.bfloat16}, got {t.dtype}")
+    if t.dim() != 3:
+        raise ValueError(f"{name} must have 3 dimensions, got {tuple(t.shape)}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}, but the current device is cuda:{device}")
+    tokens, heads, d = t.shape
+    stride = t.stride()
+    if stride[2] != 1 or (stride[1] != d and heads > 1):
+        raise ValueError(f"the values of a token of {name} must be contiguous")
+    return t.data_ptr(), stride[0] if tokens > 1 else heads * d
+
+
+def _rope_rows(store, k: torch.Tensor, v: torch.Tensor, rope: Optional[Rope], q: Optional[torch.Tensor],
+               q_out: Optional[torch.Tensor], device: int):
+    """Checks a rotating append's rows; returns the rotation's descriptor (or None) and the arguments q .. q_out."""
+    k_ptr, k_stride = _rows(k, "k", device)
+    v_ptr, v_stride = _rows(v, "v", device)
+    tokens, h_kv, head_dim = k.shape
+    if v.shape != k.shape or h_kv != store.h_kv or head_dim != store.head_dim:
+        raise ValueError("k/v must be [tokens][h_kv][head_dim] of the store")
+    q_ptr, q_stride, h_q, out_ptr = None, 0, 0, None
+    if q is not None:
+        q_ptr, q_stride = _rows(q, "q", device)
+        h_q = q.shape[1]
+        if q.shape[0] != tokens or q.shape[2] != head_dim:
+            raise ValueError("q must be [tokens][h_q][head_dim]")
+        out_ptr = _need(q_out, torch.bfloat16, "q_out", 3, device)
+        if q_out.shape != q.shape:
+            raise ValueError("q_out must have the shape of q")
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    desc = None
+    if rope is not None:
+        _need(rope.inv_freq, torch.float32, "inv_freq", 1, device)
+        desc = ctypes.byref(rope.descriptor())
+    return desc, (q_ptr, q_stride, h_q, k_ptr, k_stride, v_ptr, v_stride, out_ptr)
+
+
+def _append_chunk(call: str, desc, store, block_table: torch.Tensor, start_pos: int, k: torch.Tensor, v: torch.Tensor,
+                  rope: Optional[Rope], position: Optional[int], q: Optional[torch.Tensor],
+                  q_out: Optional[torch.Tensor], stream, device: int) -> None:
+    table_ptr = _need(block_table, torch.int32, "block_table", 1, device)
+    rope_desc, rows = _rope_rows(store, k, v, rope, q, q_out, device)
+    start_pos, n = int(start_pos), k.shape[0]
+    _maybe_check(store, block_table, start_pos, start_pos + n)
+    _check(getattr(load_library(), call)(
+        ctypes.byref(desc), table_ptr, block_table.shape[0], start_pos, n, rope_desc,
+        start_pos if position is None else int(position), *rows, _stream_on(stream, device)), call)
+
+
+def _append_batch(call: str, desc, store, block_tables: torch.Tensor, seq_lens: torch.Tensor, k: torch.Tensor,
+                  v: torch.Tensor, rope: Optional[Rope], positions: Optional[torch.Tensor],
+                  q: Optional[torch.Tensor], q_out: Optional[torch.Tensor], stream, device: int) -> None:
+    # Only the entry of the last position is used, and none of a sequence that the tables do not hold.
+    tables_ptr, lens_ptr, batch, stride, _ = _batch(store, block_tables, seq_lens, None, device, window=1, skip_longer=True)
+    rope_desc, rows = _rope_rows(store, k, v, rope, q, q_out, device)
+    pos_ptr = None if positions is None else _need(positions, torch.int32, "positions", 1, device)
+    if k.shape[0] != batch or (positions is not None and positions.shape[0] != batch):
+        raise ValueError("k, v, q and positions must have one row for each sequence")
+    _check(getattr(load_library(), call)(
+        ctypes.byref(desc), tables_ptr, stride, lens_ptr, batch, rope_desc, pos_ptr, *rows, _stream_on(stream, device)),
+        call)
+
+
+def mocap_rope_append(store: KvStore, block_table: torch.Tensor, start_pos: int, k: torch.Tensor, v: torch.Tensor,
+                      rope: Optional[Rope], position: Optional[int] = None, q: Optional[torch.Tensor] = None,
+                      q_out: Optional[torch.Tensor] = None, stream=None) -> None:
+    """k, v: bf16 [chunk_len][h_kv][head_dim], q: bf16 [chunk_len][h_q][head_dim] or None, tokens at any stride (parts of a
+    projection's rows); q_out: bf16 [chunk_len][h_q][head_dim].  position: the rotation's, of the first token (None:
+    start_pos)."""
+    device = _raw_device()
+    _append_chunk("mocap_rope_append", _store_on(store, device), store, block_table, start_pos, k, v, rope, position, q,
+                  q_out, stream, device)
+
+
+def mocap_decode_rope_append(store: KvStore, block_tables: torch.Tensor, seq_lens: torch.Tensor, k: torch.Tensor,
+                             v: torch.Tensor, rope: Optional[Rope], positions: Optional[torch.Tensor] = None,
+                             q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                             stream=None) -> None:
+    """Row b of k, v and q is the new token of sequence b; positions: int32 [batch], the rotation's (None: seq_lens - 1)."""
+    device = _raw_device()
+    _append_batch("mocap_decode_rope_append", _store_on(store, device), store, block_tables, seq_lens, k, v, rope,
+                  positions, q, q_out, stream, device)
+
+
+def mocap_kv4_append(store: Kv4Store, block_table: torch.Tensor, start_pos: int, k: torch.Tensor, v: torch.Tensor,
+                     rope: Optional[Rope] = None, position: Optional[int] = None, q: Optional[torch.Tensor] = None,
+                     q_out: Optional[torch.Tensor] = None, stream=None) -> None:
+    """As mocap_rope_append, into a 4-bit store."""
+    device = _raw_device()
+    _append_chunk("mocap_kv4_append", _store4_on(store, device), store, block_table, start_pos, k, v, rope, position, q,
+                  q_out, stream, device)
+
+
+def mocap_kv4_decode_append(store: Kv4Store, block_tables: torch.Tensor, seq_lens: torch.Tensor, k: torch.Tensor,
+                            v: torch.Tensor, rope: Optional[Rope] = None, positions: Optional[torch.Tensor] = None,
+                            q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                            stream=None) -> None:
+    """As mocap_decode_rope_append, into a 4-bit store."""
+    device = _raw_device()
+    _append_batch("mocap_kv4_decode_append", _store4_on(store, device), store, block_tables, seq_lens, k, v, rope,
+                  positions, q, q_out, stream, device)
+
+
+def mocap_kv4_load(store: Kv4Store, block_tables: torch.Tensor, ends: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                   stream=None) -> None:
+    """k, v: bf16 [batch][n][h_kv][head_dim], the values of the last n of the positions [0, ends[b]) of sequence b."""
+    device = _raw_device()
+    k_ptr = _need(k, torch.bfloat16, "k", 4, device)
+    v_ptr = _need(v, torch.bfloat16, "v", 4, device)
+    tables_ptr, ends_ptr, batch, stride, _ = _batch(store, block_tables, ends, None, device, window=k.shape[1],
+                                                    skip_longer=True)
+    if k.shape != v.shape or k.shape[0] != batch or k.shape[2:] != (store.h_kv, store.head_dim):
+        raise ValueError("k/v must be [batch][n][h_kv][head_dim] of the store")
+    desc = _store4_on(store, device)
+    _check(load_library().mocap_kv4_load(ctypes.byref(desc), tables_ptr, stride, ends_ptr, batch, k.shape[1], k_ptr, v_ptr,
+                                         _stream_on(stream, device)), "mocap_kv4_load")
+
+
+def mocap_kv4_decode_attn_workspace_size(batch: int, h_q: int, h_kv: int, head_dim: int, max_len: int, window: int = 0,
+                                         sinks: int = 0) -> int:
+    nbytes = ctypes.c_size_t(0)
+    _check(load_library().mocap_kv4_decode_attn_workspace_size(
+        int(batch), int(max_len), int(h_q), int(h_kv), int(head_dim), int(window), int(sinks), ctypes.byref(nbytes)),
+        "mocap_kv4_decode_attn_workspace_size")
+    return nbytes.value
+
+
+def mocap_kv4_decode_attn(store: Kv4Store, block_tables: torch.Tensor, seq_lens: torch.Tensor, q: torch.Tensor,
+                          max_len: Optional[int], scale: float, o: torch.Tensor, lse: torch.Tensor,
+                          workspace: Optional[torch.Tensor] = None, window: int = 0, sinks: int = 0, stream=None) -> None:
+    """As mocap_decode_attn, over a 4-bit store."""
+    device = _raw_device()
+    window, sinks = int(window), int(sinks)
+    tables_ptr, lens_ptr, batch, stride, max_len = _batch(store, block_tables, seq_lens, max_len, device, window, sinks)
+    q_ptr = _need(q, torch.bfloat16, "q", 3, device)
+    o_ptr = _need(o, torch.bfloat16, "o", 3, device)
+    lse_ptr = _need(lse, torch.float32, "lse", 2, device)
+    rows, h_q, head_dim = q.shape
+    if rows != batch or o.shape != q.shape or lse.shape != (batch, h_q):
+        raise ValueError("q and o must be [batch][h_q][head_dim] and lse [batch][h_q]")
+    ws_ptr, ws_bytes = _workspace(workspace, device)
+    desc = _store4_on(store, device)
+    _check(load_library().mocap_kv4_decode_attn(
+        ctypes.byref(desc), tables_ptr, stride, lens_ptr, batch, max_len, q_ptr, h_q, store.h_kv, head_dim, scale, window,
+        sinks, o_ptr, lse_ptr, ws_ptr, ws_bytes, _stream_on(stream, device)), "mocap_kv4_decode_attn")
+
+
+def mocap_kv4_chunk_attn_workspace_size(prefix_len: int, chunk_len: int, h_q: int, h_kv: int, head_dim: int,
+                                        window: int = 0, sinks: int = 0, num_splits: int = 0) -> Tuple[int, int]:
+    """Returns (number of KV ranges, workspace bytes)."""
+    splits = ctypes.c_int32(0)
+    nbytes = ctypes.c_size_t(0)
+    _check(load_library().mocap_kv4_chunk_attn_workspace_size(
+        int(prefix_len), int(chunk_len), int(h_q), int(h_kv), int(head_dim), int(window), int(sinks), int(num_splits),
+        ctypes.byref(splits), ctypes.byref(nbytes)), "mocap_kv4_chunk_attn_workspace_size")
+    return splits.value, nbytes.value
+
+
+def mocap_kv4_chunk_attn(store: Kv4Store, block_table: torch.Tensor, q: torch.Tensor, prefix_len: int, scale: float,
+                         o: torch.Tensor, lse: torch.Tensor, workspace: Optional[torch.Tensor] = None, window: int = 0,
+                         sinks: int = 0, num_splits: int = 0, stream=None) -> None:
+    """As mocap_chunk_attn (window 0) or mocap_window_attn, over a 4-bit store."""
+    device = _raw_device()
+    table_ptr = _need(block_table, torch.int32, "block_table", 1, device)
+    q_ptr = _need(q, torch.bfloat16, "q", 3, device)
+    o_ptr = _need(o, torch.bfloat16, "o", 3, device)
+    lse_ptr = _need(lse, torch.float32, "lse", 2, device)
+    chunk_len, h_q, head_dim = q.shape
+    if o.shape != q.shape or lse.shape != (h_q, chunk_len):
+        raise ValueError("o must match q and lse must be [h_q][chunk_len]")
+    ws_ptr, ws_bytes = _workspace(workspace, device)
+    prefix_len, window, sinks = int(prefix_len), int(window), int(sinks)
+    end = prefix_len + chunk_len
+    if window > 0:
+        _maybe_check(store, block_table, 0, min(sinks, end))
+    _maybe_check(store, block_table, max(0, prefix_len - window + 1) if window > 0 else 0, end)
+    desc = _store4_on(store, device)
+    _check(load_library().mocap_kv4_chunk_attn(
+        ctypes.byref(desc), table_ptr, block_table.shape[0], q_ptr, prefix_len, chunk_len, h_q, store.h_kv, head_dim,
+        scale, window, sinks, o_ptr, lse_ptr, ws_ptr, ws_bytes, int(num_splits), _stream_on(stream, device)),
+        "mocap_kv4_chunk_attn")

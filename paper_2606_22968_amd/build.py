@@ -15,7 +15,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libmocap_attn.so")
 SOURCES = ["api.cpp", "plan.cpp", "chunk_attn.hip", "chunk_attn_short.hip", "kv_append.hip", "lse_merge.hip",
-           "serve_api.cpp", "decode_attn.hip", "window_attn.hip", "key_weights.hip", "kv_evict.hip"]
+           "serve_api.cpp", "decode_attn.hip", "window_attn.hip", "key_weights.hip", "kv_evict.hip",
+           "cache_api.cpp", "rope_append.hip", "kv4_decode.hip", "kv4_chunk.hip"]
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -1,0 +1,310 @@
+// Host side of the rotating appends and of the 4-bit store (mocap_cache.h):
+// argument validation, how the work is cut, and kernel dispatch.  Every check runs
+// before anything is enqueued.
+#include "mocap_cache.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "cache.h"
+#include "serve_host.h"
+
+namespace {
+
+using namespace mocap;
+
+// A 4-bit store as the checks of sizes, tables and pool pointers see it.
+mocap_kv_store view_of(const mocap_kv4_store* kv) {
+  return mocap_kv_store{kv->k_pool, kv->v_pool, kv->num_blocks, kv->block_size, kv->h_kv, kv->head_dim};
+}
+
+bool scales_missing(const mocap_kv4_store* kv) {
+  return !kv->k_scale || !kv->v_scale || !aligned16(kv->k_scale) || !aligned16(kv->v_scale);
+}
+
+StorePools pools_of(const mocap_kv_store* kv) { return StorePools{kv->k_pool, kv->v_pool, nullptr, nullptr}; }
+StorePools pools_of(const mocap_kv4_store* kv) {
+  return StorePools{kv->k_pool, kv->v_pool, static_cast<uint8_t*>(kv->k_scale), static_cast<uint8_t*>(kv->v_scale)};
+}
+
+mocap_status done(hipError_t e) { return e == hipSuccess ? MOCAP_OK : MOCAP_ERR_HIP; }
+
+// 2-byte values of `tokens` rows of `heads` heads.
+bool overlap_bf16(const void* a, int64_t a_stride, const void* b, int64_t b_stride, int64_t tokens, int64_t a_row,
+                  int64_t b_row) {
+  const wide x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + 2 * extent(tokens, b_stride, b_row) && y < x + 2 * extent(tokens, a_stride, a_row);
+}
+
+// Checks the rotation and the rows of Q, K and V of `tokens` tokens, and fills in
+// their part of the launch.
+mocap_status set_rows(const mocap_kv_store& kv, const mocap_rope* rope, const void* q, int64_t q_stride, int32_t h_q,
+                      const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* q_out, int64_t tokens,
+                      RopeAppendLaunch* p) {
+  p->inv_freq = nullptr;
+  p->rot = 0;
+  p->interleaved = false;
+  if (rope != nullptr) {
+    if (!rope->inv_freq || !aligned4(rope->inv_freq) || rope->rot_dim <= 0 || rope->rot_dim > kv.head_dim)
+      return MOCAP_ERR_INVALID_ARG;
+    if (rope->rot_dim % 16 != 0) return MOCAP_ERR_UNSUPPORTED;
+    p->inv_freq = rope->inv_freq;
+    p->rot = rope->rot_dim;
+    p->interleaved = rope->interleaved != 0;
+  }
+  const int64_t kv_row = (int64_t)kv.h_kv * kv.head_dim, q_row = (int64_t)h_q * kv.head_dim;
+  if (h_q < 0 || h_q % kv.h_kv != 0) return MOCAP_ERR_INVALID_ARG;
+  if (k_stride < kv_row || v_stride < kv_row || k_stride % 8 != 0 || v_stride % 8 != 0) return MOCAP_ERR_INVALID_ARG;
+  if (!k || !v || !aligned16(k) || !aligned16(v)) return MOCAP_ERR_INVALID_ARG;
+  if (h_q > 0) {
+    if (!q || !q_out || !aligned16(q) || !aligned16(q_out) || q_stride < q_row || q_stride % 8 != 0)
+      return MOCAP_ERR_INVALID_ARG;
+    const bool in_place = q_out == q && q_stride == q_row;
+    if ((!in_place && overlap_bf16(q_out, q_row, q, q_stride, tokens, q_row, q_row)) ||
+        overlap_bf16(q_out, q_row, k, k_stride, tokens, q_row, kv_row) ||
+        overlap_bf16(q_out, q_row, v, v_stride, tokens, q_row, kv_row))
+      return MOCAP_ERR_INVALID_ARG;
+  }
+  p->q = static_cast<const uint16_t*>(q);
+  p->k = static_cast<const uint16_t*>(k);
+  p->v = static_cast<const uint16_t*>(v);
+  p->q_out = static_cast<uint16_t*>(q_out);
+  p->q_stride = q_stride;
+  p->k_stride = k_stride;
+  p->v_stride = v_stride;
+  p->h_q = h_q;
+  p->h_kv = kv.h_kv;
+  p->block_size = kv.block_size;
+  return MOCAP_OK;
+}
+
+mocap_status append_chunk(const mocap_kv_store& kv, const StorePools& pools, bool scales_bad,
+                          const int32_t* block_table, int32_t n_table, int64_t start_pos, int32_t chunk_len,
+                          const mocap_rope* rope, int64_t first_pos, const void* q, int64_t q_stride, int32_t h_q,
+                          const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* q_out, void* stream) {
+  mocap_status st = check_store(&kv);
+  if (st == MOCAP_OK) st = check_positions(&kv, n_table, start_pos, chunk_len);
+  if (st != MOCAP_OK) return st;
+  if (first_pos < 0 || first_pos > kMaxPositions - chunk_len)
+    return MOCAP_ERR_INVALID_ARG;
+  if (chunk_len == 0) return MOCAP_OK;
+  if (!kv.k_pool || !kv.v_pool || !block_table || !aligned16(kv.k_pool) || !aligned16(kv.v_pool) || scales_bad ||
+      !aligned4(block_table))
+    return MOCAP_ERR_INVALID_ARG;
+  RopeAppendLaunch p{};
+  st = set_rows(kv, rope, q, q_stride, h_q, k, k_stride, v, v_stride, q_out, chunk_len, &p);
+  if (st != MOCAP_OK) return st;
+  if (ceil_div(start_pos % kTileKeys + chunk_len, kTileKeys) > kMaxGroups ||
+      kv.h_kv + ceil_div(h_q, kRopeHeads) > 65535)
+    return MOCAP_ERR_UNSUPPORTED;
+  MOCAP_DEBUG_CHECK(block_table, start_pos, start_pos + chunk_len, &kv);
+  p.pools = pools;
+  p.tables = block_table;
+  p.start_pos = start_pos;
+  p.first_pos = first_pos;
+  p.chunk_len = chunk_len;
+  return done(launch_rope_append(p, kv.head_dim, static_cast<hipStream_t>(stream)));
+}
+
+mocap_status append_batch(const mocap_kv_store& kv, const StorePools& pools, bool scales_bad,
+                          const int32_t* block_tables, int32_t table_stride, const int32_t* seq_lens, int32_t batch,
+                          const mocap_rope* rope, const int32_t* positions, const void* q, int64_t q_stride,
+                          int32_t h_q, const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* q_out,
+                          void* stream) {
+  mocap_status st = check_batch(&kv, block_tables, table_stride, seq_lens, batch, 0);
+  if (st != MOCAP_OK || batch == 0) return st;
+  if (scales_bad || !aligned4(positions)) return MOCAP_ERR_INVALID_ARG;
+  RopeAppendLaunch p{};
+  st = set_rows(kv, rope, q, q_stride, h_q, k, k_stride, v, v_stride, q_out, batch, &p);
+  if (st != MOCAP_OK) return st;
+  if (batch > kMaxGroups || ((int64_t)kv.h_kv + h_q) * (kv.head_dim / 16) > 65535 * 64) return MOCAP_ERR_UNSUPPORTED;
+  MOCAP_DEBUG_CHECK_BATCH(&kv, block_tables, table_stride, seq_lens, batch, (int64_t)table_stride * kv.block_size, 1, 0,
+                          true);
+  p.pools = pools;
+  p.tables = block_tables;
+  p.seq_lens = seq_lens;
+  p.positions = positions;
+  p.table_stride = table_stride;
+  p.batch = batch;
+  return done(launch_decode_rope_append(p, kv.head_dim, static_cast<hipStream_t>(stream)));
+}
+
+}  // namespace
+
+extern "C" {
+
+mocap_status mocap_rope_append(const mocap_kv_store* kv, const int32_t* block_table, int32_t n_table,
+                               int64_t start_pos, int32_t chunk_len, const mocap_rope* rope, int64_t first_pos,
+                               const void* q, int64_t q_stride, int32_t h_q, const void* k, int64_t k_stride,
+                               const void* v, int64_t v_stride, void* q_out, void* stream) {
+  if (kv == nullptr) return MOCAP_ERR_INVALID_ARG;
+  return append_chunk(*kv, pools_of(kv), false, block_table, n_table, start_pos, chunk_len, rope, first_pos, q,
+                      q_stride, h_q, k, k_stride, v, v_stride, q_out, stream);
+}
+
+mocap_status mocap_kv4_append(const mocap_kv4_store* kv, const int32_t* block_table, int32_t n_table,
+                              int64_t start_pos, int32_t chunk_len, const mocap_rope* rope, int64_t first_pos,
+                              const void* q, int64_t q_stride, int32_t h_q, const void* k, int64_t k_stride,
+                              const void* v, int64_t v_stride, void* q_out, void* stream) {
+  if (kv == nullptr) return MOCAP_ERR_INVALID_ARG;
+  return append_chunk(view_of(kv), pools_of(kv), scales_missing(kv), block_table, n_table, start_pos, chunk_len, rope,
+                      first_pos, q, q_stride, h_q, k, k_stride, v, v_stride, q_out, stream);
+}
+
+mocap_status mocap_decode_rope_append(const mocap_kv_store* kv, const int32_t* block_tables, int32_t table_stride,
+                                      const int32_t* seq_lens, int32_t batch, const mocap_rope* rope,
+                                      const int32_t* positions, const void* q, int64_t q_stride, int32_t h_q,
+                                      const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* q_out,
+                                      void* stream) {
+  if (kv == nullptr) return MOCAP_ERR_INVALID_ARG;
+  return append_batch(*kv, pools_of(kv), false, block_tables, table_stride, seq_lens, batch, rope, positions, q,
+                      q_stride, h_q, k, k_stride, v, v_stride, q_out, stream);
+}
+
+mocap_status mocap_kv4_decode_append(const mocap_kv4_store* kv, const int32_t* block_tables, int32_t table_stride,
+                                     const int32_t* seq_lens, int32_t batch, const mocap_rope* rope,
+                                     const int32_t* positions, const void* q, int64_t q_stride, int32_t h_q,
+                                     const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* q_out,
+                                     void* stream) {
+  if (kv == nullptr) return MOCAP_ERR_INVALID_ARG;
+  return append_batch(view_of(kv), pools_of(kv), scales_missing(kv), block_tables, table_stride, seq_lens, batch, rope,
+                      positions, q, q_stride, h_q, k, k_stride, v, v_stride, q_out, stream);
+}
+
+mocap_status mocap_kv4_load(const mocap_kv4_store* kv, const int32_t* block_tables, int32_t table_stride,
+                            const int32_t* ends, int32_t batch, int32_t n, void* k, void* v, void* stream) {
+  if (kv == nullptr || n < 0 || n > kMaxPositions) return MOCAP_ERR_INVALID_ARG;
+  const mocap_kv_store view = view_of(kv);
+  const mocap_status st = check_batch(&view, block_tables, table_stride, ends, batch, 0);
+  if (st != MOCAP_OK || batch == 0) return st;
+  if (scales_missing(kv)) return MOCAP_ERR_INVALID_ARG;
+  if (n == 0) return MOCAP_OK;
+  if (!k || !v || !aligned16(k) || !aligned16(v)) return MOCAP_ERR_INVALID_ARG;
+  if (batch > 65535 || kv->h_kv > 65535 || ceil_div(n, kTileKeys) + 1 > kMaxGroups) return MOCAP_ERR_UNSUPPORTED;
+  MOCAP_DEBUG_CHECK_BATCH(&view, block_tables, table_stride, ends, batch, (int64_t)table_stride * kv->block_size, n, 0,
+                          true);
+  const Kv4LoadLaunch p{pools_of(kv), block_tables, ends, table_stride, static_cast<uint16_t*>(k),
+                        static_cast<uint16_t*>(v), batch, n, kv->h_kv, kv->block_size};
+  return done(launch_kv4_load(p, kv->head_dim, static_cast<hipStream_t>(stream)));
+}
+
+mocap_status mocap_kv4_decode_attn_workspace_size(int32_t batch, int64_t max_len, int32_t h_q, int32_t h_kv,
+                                                  int32_t head_dim, int64_t window, int64_t sinks, size_t* bytes_out) {
+  if (bytes_out == nullptr || batch < 0 || max_len < 0 || max_len > kMaxPositions || window < 0 || sinks < 0)
+    return MOCAP_ERR_INVALID_ARG;
+  mocap_status st = check_heads(h_q, h_kv, head_dim);
+  if (st != MOCAP_OK) return st;
+  *bytes_out = 0;
+  if (batch == 0) return MOCAP_OK;
+  DecodeAttnLaunch p;
+  st = plan_decode(batch, max_len, h_q, h_kv, window, sinks, &p);
+  if (st == MOCAP_OK) *bytes_out = decode_workspace(p, head_dim);
+  return st;
+}
+
+mocap_status mocap_kv4_decode_attn(const mocap_kv4_store* kv, const int32_t* block_tables, int32_t table_stride,
+                                   const int32_t* seq_lens, int32_t batch, int64_t max_len, const void* q, int32_t h_q,
+                                   int32_t h_kv, int32_t head_dim, float scale, int64_t window, int64_t sinks, void* o,
+                                   float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  if (kv == nullptr) return MOCAP_ERR_INVALID_ARG;
+  const mocap_kv_store view = view_of(kv);
+  mocap_status st = check_batch(&view, block_tables, table_stride, seq_lens, batch, max_len);
+  if (st != MOCAP_OK) return st;
+  if (h_q <= 0 || h_kv <= 0 || h_q % h_kv != 0 || h_kv != kv->h_kv || head_dim != kv->head_dim || !valid_scale(scale) ||
+      window < 0 || sinks < 0)
+    return MOCAP_ERR_INVALID_ARG;
+  if (batch == 0) return MOCAP_OK;
+  if (scales_missing(kv) || !q || !o || !lse || !aligned16(q) || !aligned16(o) || !aligned4(lse))
+    return MOCAP_ERR_INVALID_ARG;
+  Kv4DecodeLaunch p;
+  st = plan_decode(batch, max_len, h_q, h_kv, window, sinks, &p.a);
+  if (st != MOCAP_OK) return st;
+  if (p.a.may_split && (!workspace || !aligned16(workspace) || workspace_bytes < decode_workspace(p.a, head_dim)))
+    return MOCAP_ERR_WORKSPACE;
+  MOCAP_DEBUG_CHECK_BATCH(&view, block_tables, table_stride, seq_lens, batch, max_len, window, sinks);
+  set_tables(&view, block_tables, table_stride, seq_lens, &p.a.seqs);
+  p.a.q = static_cast<const uint16_t*>(q);
+  p.a.k_pool = static_cast<const uint16_t*>(kv->k_pool);
+  p.a.v_pool = static_cast<const uint16_t*>(kv->v_pool);
+  p.k_scale = static_cast<const uint8_t*>(kv->k_scale);
+  p.v_scale = static_cast<const uint8_t*>(kv->v_scale);
+  p.a.o = static_cast<uint16_t*>(o);
+  p.a.lse = lse;
+  p.a.ws_o = nullptr;
+  p.a.ws_lse = nullptr;
+  if (p.a.may_split) {
+    p.a.ws_o = static_cast<float*>(workspace);
+    p.a.ws_lse = reinterpret_cast<float*>(static_cast<char*>(workspace) +
+                                          round_up((size_t)p.a.seqs.items * h_q * head_dim * sizeof(float), 256));
+  }
+  p.a.scale_log2 = (float)((double)scale * 1.4426950408889634);
+  return done(launch_kv4_decode(p, head_dim, static_cast<hipStream_t>(stream)));
+}
+
+mocap_status mocap_kv4_chunk_attn_workspace_size(int64_t prefix_len, int32_t chunk_len, int32_t h_q, int32_t h_kv,
+                                                 int32_t head_dim, int64_t window, int64_t sinks, int32_t num_splits,
+                                                 int32_t* splits_out, size_t* bytes_out) {
+  if (bytes_out == nullptr || window < 0 || sinks < 0 || num_splits < 0) return MOCAP_ERR_INVALID_ARG;
+  mocap_status st = check_chunk(prefix_len, chunk_len);
+  if (st == MOCAP_OK) st = check_heads(h_q, h_kv, head_dim);
+  if (st != MOCAP_OK) return st;
+  WindowLaunch p;
+  p.n_ranges = 1;
+  if (window == 0) window = kMaxPositions, sinks = 0;
+  if (chunk_len > 0) st = plan_window(prefix_len, chunk_len, h_q, h_kv, head_dim, window, sinks, num_splits, &p);
+  if (st != MOCAP_OK) return st;
+  if (splits_out) *splits_out = p.n_ranges;
+  *bytes_out = chunk_len > 0 ? window_workspace(p, head_dim) : 0;
+  return MOCAP_OK;
+}
+
+mocap_status mocap_kv4_chunk_attn(const mocap_kv4_store* kv, const int32_t* block_table, int32_t n_table, const void* q,
+                                  int64_t prefix_len, int32_t chunk_len, int32_t h_q, int32_t h_kv, int32_t head_dim,
+                                  float scale, int64_t window, int64_t sinks, void* o, float* lse, void* workspace,
+                                  size_t workspace_bytes, int32_t num_splits, void* stream) {
+  if (kv == nullptr) return MOCAP_ERR_INVALID_ARG;
+  const mocap_kv_store view = view_of(kv);
+  mocap_status st = check_chunk_args(&view, block_table, n_table, q, prefix_len, chunk_len, h_q, h_kv, head_dim, scale);
+  if (st != MOCAP_OK) return st;
+  if (window < 0 || sinks < 0 || num_splits < 0) return MOCAP_ERR_INVALID_ARG;
+  if (chunk_len == 0) return MOCAP_OK;
+  if (scales_missing(kv) || !o || !lse || !aligned16(o) || !aligned4(lse)) return MOCAP_ERR_INVALID_ARG;
+  if (window == 0) window = kMaxPositions, sinks = 0;
+  Kv4ChunkLaunch p;
+  st = plan_window(prefix_len, chunk_len, h_q, h_kv, head_dim, window, sinks, num_splits, &p.a);
+  if (st != MOCAP_OK) return st;
+  if (p.a.n_ranges > 1 && (!workspace || !aligned16(workspace) || workspace_bytes < window_workspace(p.a, head_dim)))
+    return MOCAP_ERR_WORKSPACE;
+  MOCAP_DEBUG_CHECK(block_table, 0, std::min<int64_t>(sinks, prefix_len + chunk_len), &view);
+  MOCAP_DEBUG_CHECK(block_table, std::max<int64_t>(0, prefix_len - window + 1), prefix_len + chunk_len, &view);
+  p.a.q = static_cast<const uint16_t*>(q);
+  p.a.k_pool = static_cast<const uint16_t*>(kv->k_pool);
+  p.a.v_pool = static_cast<const uint16_t*>(kv->v_pool);
+  p.k_scale = static_cast<const uint8_t*>(kv->k_scale);
+  p.v_scale = static_cast<const uint8_t*>(kv->v_scale);
+  p.a.table = block_table;
+  p.a.o = static_cast<uint16_t*>(o);
+  p.a.lse = lse;
+  p.a.block_size = kv->block_size;
+  block_divider((uint32_t)kv->block_size, &p.a.block_magic, &p.a.block_shift);
+  p.a.scale_log2 = (float)((double)scale * 1.4426950408889634);
+  p.a.ws_o = nullptr;
+  p.a.ws_lse = nullptr;
+  if (p.a.n_ranges > 1) {
+    p.a.ws_o = static_cast<float*>(workspace);
+    p.a.ws_lse = reinterpret_cast<float*>(
+        static_cast<char*>(workspace) + round_up((size_t)p.a.n_ranges * h_q * chunk_len * head_dim * sizeof(float), 256));
+  }
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (launch_kv4_chunk(p, head_dim, s) != hipSuccess) return MOCAP_ERR_HIP;
+  if (p.a.n_ranges > 1) {
+    const MergeLaunch m{p.a.ws_o, p.a.ws_lse, p.a.o, lse, chunk_len, h_q, p.a.n_ranges};
+    if (launch_lse_merge(m, head_dim, s) != hipSuccess) return MOCAP_ERR_HIP;
+  }
+  return MOCAP_OK;
+}
+
+}  // extern "C"

@@ -29,6 +29,7 @@
 // in 293 us, 5.8 TB/s (a large copy runs at 5.1); 32 of 1 to 8192, 32/8/128, 340 MB
 // in 68 us and the join's 6; one of 572 positions, 9 us: lengths, table, keys and
 // values, one after the other.
+#include "cache.h"
 #include "serve_device.h"
 
 namespace mocap {
@@ -448,8 +449,6 @@ void launch(const DecodeAttnLaunch& p, hipStream_t stream) {
   } else {
     hipLaunchKernelGGL((decode_attn_kernel<D, 2>), grid, block, 0, stream, p);
   }
-  if (!p.may_split) return;
-  hipLaunchKernelGGL((decode_join_kernel<D>), dim3((unsigned)(p.seqs.batch * p.h_q)), block, 0, stream, p);
 }
 
 }  // namespace
@@ -459,6 +458,17 @@ hipError_t launch_decode_attn(const DecodeAttnLaunch& p, int head_dim, hipStream
     launch<128>(p, stream);
   } else {
     launch<64>(p, stream);
+  }
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess || !p.may_split ? e : launch_decode_join(p, head_dim, stream);
+}
+
+hipError_t launch_decode_join(const DecodeAttnLaunch& p, int head_dim, hipStream_t stream) {
+  const dim3 grid((unsigned)(p.seqs.batch * p.h_q)), block(kDecodeThreads);
+  if (head_dim == 128) {
+    hipLaunchKernelGGL(decode_join_kernel<128>, grid, block, 0, stream, p);
+  } else {
+    hipLaunchKernelGGL(decode_join_kernel<64>, grid, block, 0, stream, p);
   }
   return hipGetLastError();
 }

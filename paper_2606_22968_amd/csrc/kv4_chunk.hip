@@ -1,0 +1,460 @@
+// Causal attention of a chunk over the 4-bit store, in full or in a sliding window
+// with sinks, for gfx950 (CDNA4).
+//
+// As window_attn.hip, which see for the walk, the products and the softmax; what is
+// different is how a tile comes into LDS:
+//   * A 64-key tile is 4 KiB of K and 4 KiB of V codes (d 128) and 512 bytes of
+//     scales.  Each of wavefronts 0-3 loads K, 4-7 V, a 16-byte piece per lane, a tile
+//     ahead in registers; during the next tile's step it turns them into bf16 (exact)
+//     and stores them in LDS in the layout that the products read.  Every row of the
+//     workgroup then uses them, so 256 rows pay for one conversion.
+//   * K has two stages, V three (a tile's P*V follows the next tile's scores); one
+//     barrier per tile.
+//   * A value block that reads as NaN enters the product with a scale next to 0; the
+//     rows that see it get NaN in its dims at the end.
+#include "kv4_device.h"
+
+namespace mocap {
+namespace {
+
+template <int D>
+__device__ __forceinline__ int k_swizzle(int r) {
+  return D == 128 ? (r & 15) : ((r >> 1) & 7);
+}
+__device__ __forceinline__ int v_swizzle(int e) { return (e >> 1) & 7; }
+
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+  __builtin_amdgcn_s_barrier();
+}
+
+__device__ __forceinline__ uint32_t div_by(uint32_t n, uint32_t magic, int shift) {
+  return (__umulhi(n, magic) + n) >> shift;
+}
+
+// Whether some byte of a word of scales is kScaleNan (bits 7, 15, 23 or 31).
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t x) { return ((x & 0x7F7F7F7Fu) + 0x01010101u) & x & 0x80808080u; }
+
+// The tiles of a run of rows at positions [first, last]: the sinks' [0, sinks),
+// then [begin, end).
+struct Tiles {
+  int sinks, begin, end;
+  __device__ __forceinline__ int count() const { return sinks + end - begin; }
+  __device__ __forceinline__ int at(int i) const { return i < sinks ? i : i - sinks + begin; }
+};
+__device__ __forceinline__ Tiles tiles_of(const WindowLaunch& p, int first, int last) {
+  const int low = max(0, first - p.window + 1);
+  Tiles t;
+  t.begin = low / kTileKeys;
+  t.end = last / kTileKeys + 1;
+  t.sinks = min((min(p.sinks, low) + kTileKeys - 1) / kTileKeys, t.begin);
+  return t;
+}
+
+template <int D>
+__global__ __launch_bounds__(kAttnThreads, 2) void kv4_chunk_kernel(const Kv4ChunkLaunch launch) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const WindowLaunch& p = launch.a;
+  constexpr int KS = D / 16;
+  constexpr int MD = D / 32;                 // 32-dim blocks
+  constexpr int TILE_ELEMS = kTileKeys * D;
+  constexpr int K_STAGES = 2, V_STAGES = 3;
+  constexpr int PIECES = 2 * D;              // 16-byte pieces of a tile's K or V codes
+  // One array: with several, the compiler takes reads of one to depend on writes of another.
+  __shared__ __attribute__((aligned(1024))) uint16_t lds[(K_STAGES + V_STAGES) * TILE_ELEMS + 2 * 4];
+  int* const found = reinterpret_cast<int*>(lds + (K_STAGES + V_STAGES) * TILE_ELEMS);  // [4]: tile i holds NaN value blocks
+  auto k_tile = [&](int i) __attribute__((always_inline)) { return lds + (i % K_STAGES) * TILE_ELEMS; };
+  auto v_tile = [&](int i) __attribute__((always_inline)) { return lds + (K_STAGES + i % V_STAGES) * TILE_ELEMS; };
+
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int half = lane >> 5;
+  const int l32 = lane & 31;
+  const int P = p.prefix_len, L = p.chunk_len;
+
+  // Within a KV head: row block (the last ones first), then range; a row block's
+  // ranges share no tile, neighbouring row blocks most of them.
+  const int logical = xcd_contiguous(blockIdx.x, p.total_wgs);
+  const int per_kv = p.row_blocks * p.n_ranges;
+  const int kv_head = logical / per_kv;
+  const int in_kv = logical - kv_head * per_kv;
+  const int range = in_kv / p.row_blocks;
+  const int block = p.row_blocks - 1 - (in_kv - range * p.row_blocks);
+
+  // Row r of the KV head is token r / G, head r % G.  The workgroup's and the
+  // wavefront's positions.
+  const int64_t rows_end = (int64_t)L * p.group;
+  const int wg_row0 = block * kWindowRows, row0 = wg_row0 + wave * kAttnWaveRows;
+  auto token_of = [&](int64_t r) { return (int)div_by((uint32_t)min(r, rows_end - 1), p.group_magic, p.group_shift); };
+  const int wg_first = P + token_of(wg_row0), wg_last = P + token_of((int64_t)wg_row0 + kWindowRows - 1);
+  const int first = P + token_of(row0), last = P + token_of((int64_t)row0 + kAttnWaveRows - 1);
+  const bool wave_on = row0 < rows_end;
+  const Tiles tiles = tiles_of(p, wg_first, wg_last), own = tiles_of(p, first, last);
+  const int i0 = (int)((int64_t)tiles.count() * range / p.n_ranges);
+  const int i1 = (int)((int64_t)tiles.count() * (range + 1) / p.n_ranges);
+  // A tile that all rows of [a, b] see in full; one that some row of this wavefront sees.
+  auto full_for = [&](int t, int a, int b) __attribute__((always_inline)) -> bool {
+    const int k0 = t * kTileKeys, k1 = k0 + kTileKeys;
+    return k1 <= a + 1 && (k0 > b - p.window || k1 <= p.sinks);
+  };
+  auto seen = [&](int t) __attribute__((always_inline)) -> bool {
+    return wave_on && (t < own.sinks || (t >= own.begin && t < own.end));
+  };
+
+  // This lane's row: its token, and its head of the group.  Lanes past the last
+  // row take the last; nothing of theirs is stored.
+  const int lane_r = (int)min((int64_t)row0 + l32, rows_end - 1);
+  const int token = token_of(lane_r);
+  const int head = kv_head * p.group + lane_r - token * p.group;
+  const int pos = P + token;
+
+  bf16x8 qf[KS];
+  {
+    const uint16_t* qrow = p.q + ((int64_t)token * p.h_q + head) * D + half * 8;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(qrow + ks * 16);
+  }
+
+  // A lane's piece of a tile: 32 dims of a key, or 16 keys of V row (block, dim), that is of
+  // dims 32 block + dim and 16 on.
+  const int block_tiles = p.block_size / kTileKeys;
+  const uint8_t* const k_pool = reinterpret_cast<const uint8_t*>(p.k_pool);
+  const uint8_t* const v_pool = reinterpret_cast<const uint8_t*>(p.v_pool);
+  const bool takes_v = wave >= 4;
+  const int piece = tid & 255;
+  const bool takes = piece < PIECES;
+  const const_i32_ptr table = (const_i32_ptr)p.table;
+  u32x4 codes, scales;
+  auto tile_number = [&](int i) __attribute__((always_inline)) {
+    const int pos0 = tiles.at(i) * kTileKeys;
+    const int lb = (int)div_by((uint32_t)pos0, p.block_magic, p.block_shift);
+    return ((int64_t)table[lb] * p.h_kv + kv_head) * block_tiles + (pos0 - lb * p.block_size) / kTileKeys;
+  };
+  auto fetch = [&](int i) __attribute__((always_inline)) {
+    const int64_t t = tile_number(i);
+    if (!takes) return;
+    if (takes_v) {
+      codes = *reinterpret_cast<const u32x4*>(v_pool + t * (PIECES * 16) + piece * 16);
+      scales = *reinterpret_cast<const u32x4*>(launch.v_scale + t * (MD * kTileKeys) + piece / 64 * kTileKeys + piece % 4 * 16);
+    } else {
+      codes = *reinterpret_cast<const u32x4*>(k_pool + t * (PIECES * 16) + piece * 16);
+      scales[0] = launch.k_scale[t * (MD * kTileKeys) + piece % MD * kTileKeys + piece / MD];
+    }
+  };
+  auto convert = [&](int i) __attribute__((always_inline)) {
+    if (!takes) return;
+    if (takes_v) {
+      uint32_t bad = 0;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) bad |= nan_bytes(scales[w]);
+      if (bad != 0) {
+        found[i % 4] = 1;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) scales[w] &= ~((nan_bytes(scales[w]) >> 7) * 0xFFu);
+      }
+      const int e = piece / 64 * 32 + piece / 4 % 16, c = piece % 4 * 2;
+      uint16_t* vl = v_tile(i);
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        u32x4 low, high;
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          const uint32_t v = codes[2 * x + w], s = scales[2 * x + w];
+          const uint32_t v0 = two_values<0>(v, scale_of(s, 0)), v1 = two_values<1>(v, scale_of(s, 1));
+          const uint32_t v2 = two_values<2>(v, scale_of(s, 2)), v3 = two_values<3>(v, scale_of(s, 3));
+          low[2 * w] = low_halves(v0, v1);
+          low[2 * w + 1] = low_halves(v2, v3);
+          high[2 * w] = high_halves(v0, v1);
+          high[2 * w + 1] = high_halves(v2, v3);
+        }
+        *reinterpret_cast<u32x4*>(vl + e * kTileKeys + (((c + x) ^ v_swizzle(e)) << 3)) = low;
+        *reinterpret_cast<u32x4*>(vl + (e + 16) * kTileKeys + (((c + x) ^ v_swizzle(e + 16)) << 3)) = high;
+      }
+    } else {
+      const int r = piece / MD, c = piece % MD * 4;
+      uint16_t* kl = k_tile(i) + r * D;
+      const float s = scale_of(scales[0], 0);
+#pragma unroll
+      for (int w = 0; w < 4; ++w)
+        *reinterpret_cast<u32x4*>(kl + (((c + w) ^ k_swizzle<D>(r)) << 3)) =
+            u32x4{two_values<0>(codes[w], s), two_values<1>(codes[w], s), two_values<2>(codes[w], s),
+                  two_values<3>(codes[w], s)};
+    }
+  };
+
+  f32x16 oacc[MD];
+#pragma unroll
+  for (int md = 0; md < MD; ++md) oacc[md] = f32x16{};
+  float m_run = -INFINITY, l_run = 0.f, f_run = 0.f;
+  const float sl2 = p.scale_log2;
+  const int k_row_lo = key_row_order(l32);
+  const int v_row_sw = v_swizzle(l32);
+
+  // Tile i holds NaN value blocks: the 32-dim blocks in which this lane's row sees one, as bits.
+  uint32_t nan_dims = 0;
+  auto note_nan = [&](int i) __attribute__((always_inline)) {
+    const uint8_t* s = launch.v_scale + tile_number(i) * (MD * kTileKeys);
+    const int k0 = tiles.at(i) * kTileKeys;
+#pragma unroll 1
+    for (int x = 0; x < MD * kTileKeys; ++x) {
+      const int at = k0 + x % kTileKeys;
+      if (s[x] == kScaleNan && at <= pos && (at > pos - p.window || at < p.sinks)) nan_dims |= 1u << x / kTileKeys;
+    }
+  };
+
+  // Visible keys of this lane's 16 of a 32-key half: keys base + {0..7, 16..23}, as bits.
+  auto visible_bits = [&](int base) __attribute__((always_inline)) -> uint32_t {
+    auto below = [&](int x) {  // keys below x
+      x -= base;
+      const int n = x <= 0 ? 0 : x <= 8 ? x : x <= 16 ? 8 : x <= 24 ? x - 8 : 16;
+      return (1u << n) - 1u;
+    };
+    return below(pos + 1) & (~below(max(pos - p.window + 1, 0)) | below(p.sinks));
+  };
+
+  // Scores of tile i, all MFMAs, K fragments read two k-steps ahead.
+  f32x16 s[2];
+  uint32_t pk[16];          // probabilities in pairs: pair 8 sb + j holds scores 2 j, 2 j + 1 of half sb
+  float rs[2], fs[2];       // per 32-key half: sums of the rounded probabilities, of the exponentials
+  auto scores = [&](int i) __attribute__((always_inline)) {
+    const int t = tiles.at(i);
+    const uint16_t* kl = k_tile(i);
+    const int kr0 = k_row_lo, kr1 = 32 + k_row_lo;
+    const int ksw0 = k_swizzle<D>(kr0), ksw1 = k_swizzle<D>(kr1);
+    auto kfrag = [&](int kr, int ksw, int ks) __attribute__((always_inline)) {
+      return *reinterpret_cast<const bf16x8*>(kl + kr * D + (((ks * 2 + half) ^ ksw) << 3));
+    };
+    bf16x8 a0[KS], a1[KS];
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      a0[ks] = kfrag(kr0, ksw0, ks);
+      a1[ks] = kfrag(kr1, ksw1, ks);
+    }
+    s[0] = s[1] = f32x16{};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      if (ks + 2 < KS) {
+        a0[ks + 2] = kfrag(kr0, ksw0, ks + 2);
+        a1[ks + 2] = kfrag(kr1, ksw1, ks + 2);
+      }
+      s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a0[ks], qf[ks], s[0], 0, 0, 0);
+      s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a1[ks], qf[ks], s[1], 0, 0, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x100, 4, 1);  // LDS reads
+#pragma unroll
+    for (int k = 0; k < 2 * KS; ++k) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);  // MFMA
+      if (k + 4 < 2 * KS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
+    }
+    if (!full_for(t, first, last)) {
+#pragma unroll
+      for (int sb = 0; sb < 2; ++sb) {
+        const uint32_t vm = visible_bits(t * kTileKeys + sb * 32 + half * 8);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const int keep = __builtin_amdgcn_sbfe((int)vm, j, 1);
+          s[sb][j] = __int_as_float((__float_as_int(s[sb][j]) & keep) | (~keep & (int)0xFF800000u));
+        }
+      }
+    }
+  };
+  auto probs = [&](float neg_m) __attribute__((always_inline)) {
+#pragma unroll
+    for (int sb = 0; sb < 2; ++sb) {
+      float fa = 0.f, acc = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float e0 = __builtin_amdgcn_exp2f(fmaf(s[sb][2 * j], sl2, neg_m));
+        const float e1 = __builtin_amdgcn_exp2f(fmaf(s[sb][2 * j + 1], sl2, neg_m));
+        pk[sb * 8 + j] = pack_bf16x2(e0, e1);
+        fa += e0 + e1;
+        acc = dot2_bf16(pk[sb * 8 + j], 0x3F803F80u, acc);
+      }
+      fs[sb] = fa;
+      rs[sb] = acc;
+    }
+  };
+  // Raises the reference exponents of rows that need it (see attn_device.h).
+  auto settle = [&]() __attribute__((always_inline)) {
+    const bool over = !(rs[0] <= kSumLimit) || !(rs[1] <= kSumLimit);
+    if (__builtin_amdgcn_ballot_w64(over) != 0) {
+      const bool row_over = lane_pair_max(over ? 1.f : 0.f) > 0.f;
+      float mx = -INFINITY;
+#pragma unroll
+      for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) mx = fmaxf(mx, s[sb][j]);
+      mx = lane_pair_max(mx) * sl2;
+      if (row_over) {
+        if (lane_pair_sum(l_run) != 0.f) {
+          const float f = __builtin_amdgcn_exp2f(m_run - mx);
+#pragma unroll
+          for (int md = 0; md < MD; ++md) oacc[md] *= f;
+          l_run *= f;
+          f_run *= f;
+        }
+        m_run = mx;
+        probs(m_run == -INFINITY ? 0.f : -m_run);
+      }
+    }
+    l_run += rs[0] + rs[1];
+    f_run += fs[0] + fs[1];
+  };
+  // P*V takes the keys 16 at a time (quad q = pairs 4 q .. 4 q + 3) for each
+  // 32-dim block: MFMA k is quad k / MD, block k % MD.
+  constexpr int NF = 4 * MD;
+  auto vfrag = [&](const uint16_t* vl, int k) __attribute__((always_inline)) {
+    const int q = k / MD, md = k % MD;
+    return *reinterpret_cast<const bf16x8*>(vl + (md * 32 + l32) * kTileKeys + (((q * 2 + half) ^ v_row_sw) << 3));
+  };
+  auto pfrag = [&](int k) __attribute__((always_inline)) {
+    const int q = k / MD * 4;
+    return __builtin_bit_cast(bf16x8, u32x4{pk[q], pk[q + 1], pk[q + 2], pk[q + 3]});
+  };
+  // Tile i's P*V alone.
+  auto pv = [&](int i) __attribute__((always_inline)) {
+    constexpr int AHEAD = 3;
+    const uint16_t* vl = v_tile(i);
+    bf16x8 vf[AHEAD + 1];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) vf[k] = vfrag(vl, k);
+#pragma unroll
+    for (int k = 0; k < NF; ++k) {
+      if (k + AHEAD < NF) vf[(k + AHEAD) % (AHEAD + 1)] = vfrag(vl, k + AHEAD);
+      oacc[k % MD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[k % (AHEAD + 1)], pfrag(k), oacc[k % MD], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // Tile i's P*V with the next tile's probabilities (from s) woven in after the
+  // MFMAs, in place: a pair is packed four pairs after its exponentials, when the
+  // MFMAs of the quad it replaces are issued, and summed two pairs later.
+  auto pv_probs = [&](int i, float neg_m) __attribute__((always_inline)) {
+    constexpr int AHEAD = 2, NPAIRS = 16, PAIRS = NPAIRS / NF, LAG_PACK = 4, LAG_SUM = 6;
+    static_assert(PAIRS * NF == NPAIRS, "whole pairs per MFMA");
+    const uint16_t* vl = v_tile(i);
+    bf16x8 vf[AHEAD + 1];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) vf[k] = vfrag(vl, k);
+    float acc[2] = {0.f, 0.f}, facc[2] = {0.f, 0.f};
+    float ex[NPAIRS][2];
+    auto trail = [&](int pr) __attribute__((always_inline)) {
+      if (pr >= LAG_PACK && pr - LAG_PACK < NPAIRS) {
+        const int x = pr - LAG_PACK;
+        pk[x] = pack_bf16x2(ex[x][0], ex[x][1]);
+      }
+      if (pr >= LAG_SUM) {
+        const int x = pr - LAG_SUM;
+        acc[x / 8] = dot2_bf16(pk[x], 0x3F803F80u, acc[x / 8]);
+        facc[x / 8] += ex[x][0] + ex[x][1];
+      }
+    };
+#pragma unroll
+    for (int k = 0; k < NF; ++k) {
+      if (k + AHEAD < NF) vf[(k + AHEAD) % (AHEAD + 1)] = vfrag(vl, k + AHEAD);
+      oacc[k % MD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[k % (AHEAD + 1)], pfrag(k), oacc[k % MD], 0, 0, 0);
+#pragma unroll
+      for (int x = 0; x < PAIRS; ++x) {
+        const int pr = k * PAIRS + x;
+        ex[pr][0] = __builtin_amdgcn_exp2f(fmaf(s[pr / 8][pr % 8 * 2], sl2, neg_m));
+        ex[pr][1] = __builtin_amdgcn_exp2f(fmaf(s[pr / 8][pr % 8 * 2 + 1], sl2, neg_m));
+        trail(pr);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int pr = NPAIRS; pr < NPAIRS + LAG_SUM; ++pr) trail(pr);
+#pragma unroll
+    for (int sb = 0; sb < 2; ++sb) {
+      rs[sb] = acc[sb];
+      fs[sb] = facc[sb];
+    }
+  };
+  // Tile by tile: its scores, then the tile before's P*V with its probabilities
+  // woven in.  A tile that this wavefront does not see ends the chain: the tile
+  // before's P*V is made alone (its stage is refilled after the next barrier),
+  // and the next tile begins a new one.
+  if (tid < 4) found[tid] = 0;
+  __syncthreads();
+  if (i0 < i1) {
+    fetch(i0);
+    convert(i0);
+    if (i0 + 1 < i1) fetch(i0 + 1);
+    bool pending = false;  // tile i - 1's P*V is still to be made
+    for (int i = i0; i < i1; ++i) {
+      lds_barrier();
+      if (__builtin_amdgcn_readfirstlane(found[i % 4]) != 0) note_nan(i);
+      if (tid == 0) found[(i + 2) % 4] = 0;
+      if (i + 1 < i1) convert(i + 1);
+      if (i + 2 < i1) fetch(i + 2);
+      const bool on = seen(tiles.at(i));
+      if (pending && !on) {
+        pv(i - 1);
+        pending = false;
+      }
+      if (!on) continue;
+      scores(i);
+      if (pending) {
+        pv_probs(i - 1, -m_run);
+      } else {
+        probs(-m_run);
+      }
+      settle();
+      pending = true;
+    }
+    if (pending) pv(i1 - 1);
+  }
+
+  // A score whose product with the scale is beyond fp32 makes every exponential 0, its
+  // own too; the row is NaN, as with an infinite score.
+  const bool beyond = m_run == INFINITY;
+  const float l_tot = lane_pair_sum(l_run), f_tot = beyond ? NAN : lane_pair_sum(f_run);
+  if (row0 + l32 >= rows_end) return;
+  const float inv = beyond ? NAN : l_tot > 0.f ? 1.f / l_tot : 0.f;
+  const float row_lse = f_tot == 0.f ? -INFINITY : (m_run + log2f(f_tot)) * kLn2;
+  const int64_t out_row = (int64_t)token * p.h_q + head;
+  const int64_t part_row = (int64_t)range * L * p.h_q + out_row;
+#pragma unroll
+  for (int md = 0; md < MD; ++md) {
+    const float scale = nan_dims >> md & 1 ? NAN : inv;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int dim = md * 32 + j * 8 + half * 4;
+      f32x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[e] = oacc[md][j * 4 + e] * scale;
+      }
+      if (p.n_ranges == 1) {
+        bf16x4 x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = (__bf16)v[e];
+        *reinterpret_cast<bf16x4*>(p.o + out_row * D + dim) = x;
+      } else {
+        *reinterpret_cast<f32x4*>(p.ws_o + part_row * D + dim) = v;
+      }
+    }
+  }
+  if (half == 0) {
+    if (p.n_ranges == 1) {
+      p.lse[(int64_t)head * L + token] = row_lse;
+    } else {
+      p.ws_lse[part_row] = row_lse;
+    }
+  }
+#endif  // __HIP_DEVICE_COMPILE__
+}
+
+}  // namespace
+
+hipError_t launch_kv4_chunk(const Kv4ChunkLaunch& p, int head_dim, hipStream_t stream) {
+  const dim3 grid(p.a.total_wgs), block(kAttnThreads);
+  if (head_dim == 128) {
+    hipLaunchKernelGGL(kv4_chunk_kernel<128>, grid, block, 0, stream, p);
+  } else {
+    hipLaunchKernelGGL(kv4_chunk_kernel<64>, grid, block, 0, stream, p);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace mocap

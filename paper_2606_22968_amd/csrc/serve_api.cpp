@@ -103,23 +103,6 @@ int32_t evict_chunks(int64_t candidates) {
   return (int32_t)std::min<int64_t>(mocap::kEvictMaxChunks, ceil_div(candidates, 4096));
 }
 
-// Checks shared by the calls on one chunk of one sequence.
-mocap_status check_chunk_args(const mocap_kv_store* kv, const int32_t* block_table, int32_t n_table, const void* q,
-                              int64_t prefix_len, int32_t chunk_len, int32_t h_q, int32_t h_kv, int32_t head_dim,
-                              float scale) {
-  mocap_status st = check_store(kv);
-  if (st != MOCAP_OK) return st;
-  if (h_q <= 0 || h_kv <= 0 || h_q % h_kv != 0 || h_kv != kv->h_kv || head_dim != kv->head_dim || !valid_scale(scale))
-    return MOCAP_ERR_INVALID_ARG;
-  st = check_positions(kv, n_table, prefix_len, chunk_len);
-  if (st != MOCAP_OK) return st;
-  if (chunk_len == 0) return MOCAP_OK;
-  if (!kv->k_pool || !kv->v_pool || !block_table || !q) return MOCAP_ERR_INVALID_ARG;
-  if (!aligned16(kv->k_pool) || !aligned16(kv->v_pool) || !aligned4(block_table) || !aligned16(q))
-    return MOCAP_ERR_INVALID_ARG;
-  return MOCAP_OK;
-}
-
 }  // namespace
 
 extern "C" {
