@@ -51,7 +51,7 @@ __global__ __launch_bounds__(kThreads) void kv4_decode_kernel(const Kv4DecodeLau
   const SeqPart w = locate_item(p.seqs, lane, item);
   if (w.seq == p.seqs.batch) return;
   int begin, end;
-  part_range(w, &begin, &end);
+  part_range_longer_first(w, &begin, &end);
 
   // Q as the B operand: lane l holds head l % 16, dims D / 4 (l / 16) + 8 ks .. + 7.
   // Lanes past the group's last head take that head; nothing of theirs is stored.
@@ -142,28 +142,25 @@ __global__ __launch_bounds__(kThreads) void kv4_decode_kernel(const Kv4DecodeLau
       }
     }
     if (more) fetch_k(next);
-    // Score e of a lane (product e / 4) belongs to key key0 + 16 g4 + e; hidden ones as bits.
+    // Score e of a lane (product e / 4) belongs to key key0 + 16 g4 + e.
     const int key0 = w.span.tile(begin + i) * kTileKeys;
-    uint32_t hidden = 0;
     if (key0 + kTileKeys > w.span.len || (key0 < w.span.low && key0 + kTileKeys > w.span.sink_end)) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) hidden |= visible(key0 + g4 * 16 + e) ? 0u : 1u << e;
-      // A hidden position's scale may be NaN; its probability is 0.
+      for (int e = 0; e < 16; ++e) {
+        const bool gone = !visible(key0 + g4 * 16 + e);
 #pragma unroll
-      for (int b = 0; b < B; ++b)
+        for (int t = 0; t < NT; ++t) s[t][e >> 2][e & 3] = gone ? -INFINITY : s[t][e >> 2][e & 3];
+        // A hidden position's scale may be NaN; its probability is 0.
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          raw.v_scale[b][e >> 2] &= hidden >> e & 1 ? ~(0xFFu << (8 * (e & 3))) : ~0u;
+        for (int b = 0; b < B; ++b) raw.v_scale[b][e >> 2] &= gone ? ~(0xFFu << (8 * (e & 3))) : ~0u;
+      }
     }
     bf16x8 hi[NT][2], lo[NT][2];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      float x[16];
+      float mx = s[t][0][0];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) x[e] = hidden >> e & 1 ? -INFINITY : s[t][e >> 2][e & 3];
-      float mx = x[0];
-#pragma unroll
-      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, x[e]);
+      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[t][e >> 2][e & 3]);
       const float m_new = fmaxf(m_run[t], quad_rows_max(mx) * sl2);
       const float ref = m_new == -INFINITY ? 0.f : m_new;
       // The accumulators are scaled only when some row's maximum has grown.
@@ -179,8 +176,8 @@ __global__ __launch_bounds__(kThreads) void kv4_decode_kernel(const Kv4DecodeLau
         u32x4 ph, pl;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float a = __builtin_amdgcn_exp2f(fmaf(x[8 * h + 2 * e], sl2, -ref));
-          const float b = __builtin_amdgcn_exp2f(fmaf(x[8 * h + 2 * e + 1], sl2, -ref));
+          const float a = __builtin_amdgcn_exp2f(fmaf(s[t][2 * h + e / 2][2 * e & 3], sl2, -ref));
+          const float b = __builtin_amdgcn_exp2f(fmaf(s[t][2 * h + e / 2][(2 * e & 3) + 1], sl2, -ref));
           l_run[t] += a + b;
           ph[e] = pack_bf16x2(a, b);
           pl[e] = pack_bf16x2(a - __uint_as_float(ph[e] << 16), b - __uint_as_float(ph[e] & 0xFFFF0000u));

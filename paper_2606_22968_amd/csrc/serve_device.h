@@ -73,8 +73,15 @@ __device__ __forceinline__ float wave_largest(float x) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
 
-// Tiles of a part, from the lengths of all sequences; every wavefront makes it
-// for itself (4 bytes per sequence, from the L2).
+// Tiles of a part, from those of all sequences.
+__device__ __forceinline__ int tiles_per_part(const SeqBatch& s, float t) {
+  // (Floating point: no 64-bit division; a tile more or less in a part is no matter,
+  // but a part must not have fewer than total / target.)
+  const int few = min(s.min_tiles, max(s.least_tiles, (int)(t / (float)s.fill) + 1));
+  return max(few, (int)(t * 1.000001f / (float)s.target) + 1);
+}
+// The same from the lengths; every wavefront makes it for itself (4 bytes per
+// sequence, from the L2).
 __device__ __forceinline__ int part_tiles(const SeqBatch& s, int lane) {
   float t = 0.f;
   for (int b0 = 0; b0 < s.batch; b0 += 64) {
@@ -83,10 +90,7 @@ __device__ __forceinline__ int part_tiles(const SeqBatch& s, int lane) {
     const int sums = wave_sums(b < s.batch ? seq_span(s, s.seq_lens[b]).tiles : 0);
     t += (float)(uint32_t)__builtin_amdgcn_readlane(sums, 63);
   }
-  // (Floating point: no 64-bit division; a tile more or less in a part is no matter,
-  // but a part must not have fewer than total / target.)
-  const int few = min(s.min_tiles, max(s.least_tiles, (int)(t / (float)s.fill) + 1));
-  return max(few, (int)(t * 1.000001f / (float)s.target) + 1);
+  return tiles_per_part(s, t);
 }
 
 __device__ __forceinline__ int parts_for(int tiles, int per) { return max(1, (tiles + per - 1) / per); }
@@ -96,25 +100,39 @@ struct SeqPart {
   int seq, part, parts;
   SeqSpan span;
 };
+// Looks for the item among the sequences of 64 lanes, the first of which is b0 and has
+// the item `base`.
+__device__ __forceinline__ bool find_item(const SeqBatch& s, int item, int b0, int base, int len, int parts, int upto,
+                                          SeqPart* r) {
+  const uint64_t past = __builtin_amdgcn_ballot_w64(item < base + upto);
+  if (past == 0) return false;
+  const int at = __builtin_ctzll(past);
+  r->seq = b0 + at;
+  r->parts = __builtin_amdgcn_readlane(parts, at);
+  r->part = item - base - (__builtin_amdgcn_readlane(upto, at) - r->parts);
+  r->span = seq_span(s, __builtin_amdgcn_readlane(len, at));
+  return true;
+}
 __device__ __forceinline__ SeqPart locate_item(const SeqBatch& s, int lane, int item) {
-  const int per = part_tiles(s, lane);
   SeqPart r;
   r.seq = s.batch;
+  if (s.batch <= 64) {  // one load of the lengths, at the head of a chain of loads
+    const bool there = lane < s.batch;
+    const int len = there ? s.seq_lens[lane] : 0;
+    const int tiles = there ? seq_span(s, len).tiles : 0;
+    const int per = tiles_per_part(s, (float)(uint32_t)__builtin_amdgcn_readlane(wave_sums(tiles), 63));
+    const int parts = there ? parts_for(tiles, per) : 0;
+    find_item(s, item, 0, 0, len, parts, wave_sums(parts), &r);
+    return r;
+  }
+  const int per = part_tiles(s, lane);
   int base = 0;
   for (int b0 = 0; b0 < s.batch; b0 += 64) {
     const int b = b0 + lane;
     const int len = b < s.batch ? s.seq_lens[b] : 0;
     const int parts = b < s.batch ? parts_for(seq_span(s, len).tiles, per) : 0;
     const int upto = wave_sums(parts);
-    const uint64_t past = __builtin_amdgcn_ballot_w64(item < base + upto);
-    if (past != 0) {
-      const int at = __builtin_ctzll(past);
-      r.seq = b0 + at;
-      r.parts = __builtin_amdgcn_readlane(parts, at);
-      r.part = item - base - (__builtin_amdgcn_readlane(upto, at) - r.parts);
-      r.span = seq_span(s, __builtin_amdgcn_readlane(len, at));
-      return r;
-    }
+    if (find_item(s, item, b0, base, len, parts, upto, &r)) return r;
     base += __builtin_amdgcn_readlane(upto, 63);
   }
   return r;
@@ -143,6 +161,13 @@ __device__ __forceinline__ SeqPart parts_of(const SeqBatch& s, int lane, int seq
 __device__ __forceinline__ void part_range(const SeqPart& w, int* begin, int* end) {
   *begin = (int)((int64_t)w.span.tiles * w.part / w.parts);
   *end = (int)((int64_t)w.span.tiles * (w.part + 1) / w.parts);
+}
+// The same with the longer parts first: one 32-bit division instead of two of 64 bits (250
+// scalar instructions on the way to a workgroup's first load).
+__device__ __forceinline__ void part_range_longer_first(const SeqPart& w, int* begin, int* end) {
+  const int each = (int)((uint32_t)w.span.tiles / (uint32_t)w.parts), more = w.span.tiles - each * w.parts;
+  *begin = each * w.part + min(w.part, more);
+  *end = *begin + each + (w.part < more ? 1 : 0);
 }
 
 }  // namespace
