@@ -589,11 +589,28 @@ def mocap_lbcp_refine_e2e(seq_len: int, num_chunks: int, num_stages: int, align:
 
 # ---- After the prefill (mocap_serve.h) ----
 
+try:  # the same checks in C++ (csrc/tensors.cpp), 0.1 us a tensor for 0.3 to 0.5
+    from ._tensors import address as _address, rows as _row_address
+except ImportError:
+    def _address(t, dtype, ndim: int, device: int) -> Optional[int]:
+        if type(t) is torch.Tensor and t.dtype is dtype and t.get_device() == device and t.is_contiguous() and \
+                (ndim < 0 or t.dim() == ndim):
+            return t.data_ptr()
+        return None
+
+    def _row_address(t, device: int):
+        if type(t) is torch.Tensor and t.dtype is torch.bfloat16 and t.dim() == 3 and t.get_device() == device:
+            (tokens, heads, d), stride = t.shape, t.stride()
+            if stride[2] == 1 and (heads <= 1 or stride[1] == d):
+                return t.data_ptr(), stride[0] if tokens > 1 else heads * d, tokens, heads, d
+        return None
+
+
 def _need(t: torch.Tensor, dtype, name: str, ndim: Optional[int], device: int) -> int:
     """The address of a contiguous tensor of this type on the current device, where the call enqueues its work."""
-    if type(t) is torch.Tensor and t.dtype is dtype and t.get_device() == device and t.is_contiguous() and \
-            (ndim is None or t.dim() == ndim):
-        return t.data_ptr()
+    at = _address(t, dtype, -1 if ndim is None else ndim, device)
+    if at is not None:
+        return at
     _require(t, dtype, name, ndim)
     if t.get_device() != device:
         raise ValueError(f"{name} is on {t.device}, but the current device is cuda:{device}")
@@ -849,8 +866,9 @@ class Rope:
     def rot_dim(self) -> int:
         return 2 * self.inv_freq.shape[0]
 
-    def descriptor(self) -> mocap_rope:
-        return mocap_rope(self.inv_freq.data_ptr(), self.rot_dim, int(self.interleaved))
+    def descriptor(self, device: Optional[int] = None) -> mocap_rope:
+        at = _need(self.inv_freq, torch.float32, "inv_freq", 1, _raw_device() if device is None else device)
+        return mocap_rope(at, self.rot_dim, self.interleaved)
 
 
 class Kv4Store:
@@ -880,16 +898,18 @@ class Kv4Store:
 
 def _store4_on(store: Kv4Store, device: int) -> mocap_kv4_store:
     """The store's descriptor, of pools on the current device."""
-    _need(store.k_pool, torch.uint8, "k_pool", 4, device)
-    _need(store.v_pool, torch.uint8, "v_pool", 5, device)
-    _need(store.k_scale, torch.uint8, "k_scale", 5, device)
-    _need(store.v_scale, torch.uint8, "v_scale", 5, device)
-    return store.descriptor()
+    return mocap_kv4_store(
+        _need(store.k_pool, torch.uint8, "k_pool", 4, device), _need(store.v_pool, torch.uint8, "v_pool", 5, device),
+        _need(store.k_scale, torch.uint8, "k_scale", 5, device), _need(store.v_scale, torch.uint8, "v_scale", 5, device),
+        store.num_blocks, store.block_size, store.h_kv, store.head_dim)
 
 
 def _rows(t: torch.Tensor, name: str, device: int):
-    """The address and token stride of a bf16 [tokens][heads][head_dim] tensor on the current device whose tokens' values
-    are contiguous."""
+    """(address, token stride, tokens, heads, head_dim) of a bf16 [tokens][heads][head_dim] tensor on the current device
+    whose tokens' values are contiguous."""
+    at = _row_address(t, device)
+    if at is not None:
+        return at
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.dtype is not torch.bfloat16:
@@ -898,47 +918,42 @@ def _rows(t: torch.Tensor, name: str, device: int):
         raise ValueError(f"{name} must have 3 dimensions, got {tuple(t.shape)}")
     if t.get_device() != device:
         raise ValueError(f"{name} is on {t.device}, but the current device is cuda:{device}")
-    tokens, heads, d = t.shape
-    stride = t.stride()
-    if stride[2] != 1 or (stride[1] != d and heads > 1):
-        raise ValueError(f"the values of a token of {name} must be contiguous")
-    return t.data_ptr(), stride[0] if tokens > 1 else heads * d
+    if type(t) is not torch.Tensor:
+        return _rows(t.detach().as_subclass(torch.Tensor), name, device)
+    raise ValueError(f"the values of a token of {name} must be contiguous")
 
 
 def _rope_rows(store, k: torch.Tensor, v: torch.Tensor, rope: Optional[Rope], q: Optional[torch.Tensor],
                q_out: Optional[torch.Tensor], device: int):
-    """Checks a rotating append's rows; returns the rotation's descriptor (or None) and the arguments q .. q_out."""
-    k_ptr, k_stride = _rows(k, "k", device)
-    v_ptr, v_stride = _rows(v, "v", device)
-    tokens, h_kv, head_dim = k.shape
-    if v.shape != k.shape or h_kv != store.h_kv or head_dim != store.head_dim:
+    """Checks a rotating append's rows; returns their number, the rotation's descriptor (or None) and the arguments
+    q .. q_out."""
+    k_ptr, k_stride, *shape = _rows(k, "k", device)
+    v_ptr, v_stride, *v_shape = _rows(v, "v", device)
+    tokens, h_kv, head_dim = shape
+    if shape != v_shape or h_kv != store.h_kv or head_dim != store.head_dim:
         raise ValueError("k/v must be [tokens][h_kv][head_dim] of the store")
     q_ptr, q_stride, h_q, out_ptr = None, 0, 0, None
     if q is not None:
-        q_ptr, q_stride = _rows(q, "q", device)
-        h_q = q.shape[1]
-        if q.shape[0] != tokens or q.shape[2] != head_dim:
+        q_ptr, q_stride, q_tokens, h_q, q_dim = _rows(q, "q", device)
+        if q_tokens != tokens or q_dim != head_dim:
             raise ValueError("q must be [tokens][h_q][head_dim]")
         out_ptr = _need(q_out, torch.bfloat16, "q_out", 3, device)
-        if q_out.shape != q.shape:
+        if q_out.shape != (tokens, h_q, head_dim):
             raise ValueError("q_out must have the shape of q")
     elif q_out is not None:
         raise ValueError("q_out without q")
-    desc = None
-    if rope is not None:
-        _need(rope.inv_freq, torch.float32, "inv_freq", 1, device)
-        desc = ctypes.byref(rope.descriptor())
-    return desc, (q_ptr, q_stride, h_q, k_ptr, k_stride, v_ptr, v_stride, out_ptr)
+    desc = None if rope is None else ctypes.byref(rope.descriptor(device))
+    return tokens, desc, (q_ptr, q_stride, h_q, k_ptr, k_stride, v_ptr, v_stride, out_ptr)
 
 
 def _append_chunk(call: str, desc, store, block_table: torch.Tensor, start_pos: int, k: torch.Tensor, v: torch.Tensor,
                   rope: Optional[Rope], position: Optional[int], q: Optional[torch.Tensor],
                   q_out: Optional[torch.Tensor], stream, device: int) -> None:
     table_ptr = _need(block_table, torch.int32, "block_table", 1, device)
-    rope_desc, rows = _rope_rows(store, k, v, rope, q, q_out, device)
-    start_pos, n = int(start_pos), k.shape[0]
+    n, rope_desc, rows = _rope_rows(store, k, v, rope, q, q_out, device)
+    start_pos = int(start_pos)
     _maybe_check(store, block_table, start_pos, start_pos + n)
-    _check(getattr(load_library(), call)(
+    _check(getattr(_lib or load_library(), call)(
         ctypes.byref(desc), table_ptr, block_table.shape[0], start_pos, n, rope_desc,
         start_pos if position is None else int(position), *rows, _stream_on(stream, device)), call)
 
@@ -948,11 +963,11 @@ def _append_batch(call: str, desc, store, block_tables: torch.Tensor, seq_lens: 
                   q: Optional[torch.Tensor], q_out: Optional[torch.Tensor], stream, device: int) -> None:
     # Only the entry of the last position is used, and none of a sequence that the tables do not hold.
     tables_ptr, lens_ptr, batch, stride, _ = _batch(store, block_tables, seq_lens, None, device, window=1, skip_longer=True)
-    rope_desc, rows = _rope_rows(store, k, v, rope, q, q_out, device)
+    n, rope_desc, rows = _rope_rows(store, k, v, rope, q, q_out, device)
     pos_ptr = None if positions is None else _need(positions, torch.int32, "positions", 1, device)
-    if k.shape[0] != batch or (positions is not None and positions.shape[0] != batch):
+    if n != batch or (positions is not None and positions.shape[0] != batch):
         raise ValueError("k, v, q and positions must have one row for each sequence")
-    _check(getattr(load_library(), call)(
+    _check(getattr(_lib or load_library(), call)(
         ctypes.byref(desc), tables_ptr, stride, lens_ptr, batch, rope_desc, pos_ptr, *rows, _stream_on(stream, device)),
         call)
 
