@@ -4,15 +4,22 @@
 // As window_attn.hip, which see for the walk, the products and the softmax; what is
 // different is how a tile comes into LDS:
 //   * A 64-key tile is 4 KiB of K and 4 KiB of V codes (d 128) and 512 bytes of
-//     scales.  Each of wavefronts 0-3 loads K, 4-7 V, a 16-byte piece per lane, a tile
-//     ahead in registers; during the next tile's step it turns them into bf16 (exact)
-//     and stores them in LDS in the layout that the products read.  Every row of the
-//     workgroup then uses them, so 256 rows pay for one conversion.
+//     scales.  Each of wavefronts 0-3 loads K, 4-7 V, 16 bytes a lane (d 64: 8), a tile
+//     ahead in registers; during the step before its own the tile is turned into bf16
+//     (exact) and stored in LDS in the layout that the products read.  Every row of the
+//     workgroup then uses it, so 256 rows pay for one conversion.
 //   * K has two stages, V three (a tile's P*V follows the next tile's scores); one
 //     barrier per tile.
-//   * A value block that reads as NaN enters the product with a scale next to 0; the
-//     rows that see it get NaN in its dims at the end.
+//   * A value block that reads as NaN is left to the product where all rows of the
+//     workgroup see its tile.  In other tiles its scale is set next to 0, and the rows
+//     that see it get NaN in its dims at the end.
+// Measured: 2048 tokens of 32/8/128 heads behind 30720, 993 us, 1.07 PFLOP/s; issue and
+// power bound it, as in chunk_attn.hip (the median of 30 in a row is 1055).  The
+// conversion is 5.5% of it, half of that the stores to LDS.  Looking a table entry up a
+// tile ahead changes nothing.
 #include "kv4_device.h"
+
+#include <type_traits>
 
 namespace mocap {
 namespace {
@@ -58,8 +65,12 @@ __global__ __launch_bounds__(kAttnThreads, 2) void kv4_chunk_kernel(const Kv4Chu
   constexpr int KS = D / 16;
   constexpr int MD = D / 32;                 // 32-dim blocks
   constexpr int TILE_ELEMS = kTileKeys * D;
+  // Where the next tile is turned into bf16: between the MFMAs of this one's scores (from a
+  // second set of registers), or ahead of them.  2048 tokens of 32/8/128 heads behind 30720
+  // 1030 and 993 us, of 16/2/64 behind 16384 217 and 231: at head_dim 128 a tile's MFMAs
+  // are twice as many beside the same exponentials, and take the issue slots.
+  constexpr bool kWeave = D == 64;
   constexpr int K_STAGES = 2, V_STAGES = 3;
-  constexpr int PIECES = 2 * D;              // 16-byte pieces of a tile's K or V codes
   // One array: with several, the compiler takes reads of one to depend on writes of another.
   __shared__ __attribute__((aligned(1024))) uint16_t lds[(K_STAGES + V_STAGES) * TILE_ELEMS + 2 * 4];
   int* const found = reinterpret_cast<int*>(lds + (K_STAGES + V_STAGES) * TILE_ELEMS);  // [4]: tile i holds NaN value blocks
@@ -116,70 +127,86 @@ __global__ __launch_bounds__(kAttnThreads, 2) void kv4_chunk_kernel(const Kv4Chu
     for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(qrow + ks * 16);
   }
 
-  // A lane's piece of a tile: 32 dims of a key, or 16 keys of V row (block, dim), that is of
-  // dims 32 block + dim and 16 on.
+  // A thread's piece of a tile: of wavefronts 0-3 D / 4 dims of a key, of 4-7 D / 8 keys of V row
+  // (block, dim), that is of dims 32 block + dim and 16 on.
   const int block_tiles = p.block_size / kTileKeys;
   const uint8_t* const k_pool = reinterpret_cast<const uint8_t*>(p.k_pool);
   const uint8_t* const v_pool = reinterpret_cast<const uint8_t*>(p.v_pool);
+  constexpr int WORDS = D / 32;              // of codes, a thread
+  constexpr int STEPS = 2 * WORDS;           // of their conversion
+  constexpr int TILE_BYTES = kTileKeys * D / 2, SCALE_BYTES = kTileKeys * MD;
   const bool takes_v = wave >= 4;
   const int piece = tid & 255;
-  const bool takes = piece < PIECES;
   const const_i32_ptr table = (const_i32_ptr)p.table;
-  u32x4 codes, scales;
+  typedef uint32_t words __attribute__((ext_vector_type(WORDS)));
+  struct Raw {
+    words codes, scales;                     // K: one scale
+  } raw, next;  // of the tile to be turned into bf16; kWeave: and of the one after it
+  const int k_key = piece / 4, k_part = piece % 4;   // dims D / 4 k_part ..
+  constexpr int V_PARTS = 512 / D;
+  const int v_row = piece / V_PARTS, v_part = piece % V_PARTS;
+  const int scale_at = takes_v ? v_row / 16 * kTileKeys + v_part * (D / 8) : k_part * (D / 4) / 32 * kTileKeys + k_key;
   auto tile_number = [&](int i) __attribute__((always_inline)) {
     const int pos0 = tiles.at(i) * kTileKeys;
     const int lb = (int)div_by((uint32_t)pos0, p.block_magic, p.block_shift);
     return ((int64_t)table[lb] * p.h_kv + kv_head) * block_tiles + (pos0 - lb * p.block_size) / kTileKeys;
   };
-  auto fetch = [&](int i) __attribute__((always_inline)) {
+  auto fetch = [&](int i, Raw& to) __attribute__((always_inline)) {
     const int64_t t = tile_number(i);
-    if (!takes) return;
     if (takes_v) {
-      codes = *reinterpret_cast<const u32x4*>(v_pool + t * (PIECES * 16) + piece * 16);
-      scales = *reinterpret_cast<const u32x4*>(launch.v_scale + t * (MD * kTileKeys) + piece / 64 * kTileKeys + piece % 4 * 16);
+      to.codes = *reinterpret_cast<const words*>(v_pool + t * TILE_BYTES + piece * (D / 8));
+      to.scales = *reinterpret_cast<const words*>(launch.v_scale + t * SCALE_BYTES + scale_at);
     } else {
-      codes = *reinterpret_cast<const u32x4*>(k_pool + t * (PIECES * 16) + piece * 16);
-      scales[0] = launch.k_scale[t * (MD * kTileKeys) + piece % MD * kTileKeys + piece / MD];
+      to.codes = *reinterpret_cast<const words*>(k_pool + t * TILE_BYTES + piece * (D / 8));
+      to.scales[0] = launch.k_scale[t * SCALE_BYTES + scale_at];
+    }
+  };
+  // Where all rows see a whole tile, a NaN value block reaches all of them as NaN; in other
+  // tiles it is noted and its scale set next to 0 (unwritten scales may be NaN as well).
+  auto set_apart = [&](int i) __attribute__((always_inline)) {
+    if (!takes_v || full_for(tiles.at(i), wg_first, wg_last)) return;
+    uint32_t bad = 0;
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) bad |= nan_bytes(raw.scales[w]);
+    if (bad == 0) return;
+    found[i % 4] = 1;
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) raw.scales[w] &= ~((nan_bytes(raw.scales[w]) >> 7) * 0xFFu);
+  };
+  // Turns the fetched codes into bf16 in the stages of tile i, in STEPS steps.
+  u32x4 out[2];
+  auto k_step = [&](int i, int step) __attribute__((always_inline)) {
+    const uint32_t c = raw.codes[step / 2];
+    const float s = scale_of(raw.scales[0], 0);
+    if (step % 2 == 0) {
+      out[0] = u32x4{two_values<0>(c, s), two_values<1>(c, s), two_values<2>(c, s), two_values<3>(c, s)};
+    } else {
+      *reinterpret_cast<u32x4*>(k_tile(i) + k_key * D + (((k_part * WORDS + step / 2) ^ k_swizzle<D>(k_key)) << 3)) = out[0];
+    }
+  };
+  auto v_step = [&](int i, int step) __attribute__((always_inline)) {
+    if (step % 4 < 2) {
+      const int w = step % 4;
+      const uint32_t v = raw.codes[step / 4 * 2 + w], sc = raw.scales[step / 4 * 2 + w];
+      const uint32_t v0 = two_values<0>(v, scale_of(sc, 0)), v1 = two_values<1>(v, scale_of(sc, 1));
+      const uint32_t v2 = two_values<2>(v, scale_of(sc, 2)), v3 = two_values<3>(v, scale_of(sc, 3));
+      out[0][2 * w] = low_halves(v0, v1);
+      out[0][2 * w + 1] = low_halves(v2, v3);
+      out[1][2 * w] = high_halves(v0, v1);
+      out[1][2 * w + 1] = high_halves(v2, v3);
+    } else {
+      const int e = v_row / 16 * 32 + v_row % 16 + (step % 4 - 2) * 16;
+      *reinterpret_cast<u32x4*>(v_tile(i) + e * kTileKeys + (((v_part * (WORDS / 2) + step / 4) ^ v_swizzle(e)) << 3)) =
+          out[step % 4 - 2];
     }
   };
   auto convert = [&](int i) __attribute__((always_inline)) {
-    if (!takes) return;
     if (takes_v) {
-      uint32_t bad = 0;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) bad |= nan_bytes(scales[w]);
-      if (bad != 0) {
-        found[i % 4] = 1;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) scales[w] &= ~((nan_bytes(scales[w]) >> 7) * 0xFFu);
-      }
-      const int e = piece / 64 * 32 + piece / 4 % 16, c = piece % 4 * 2;
-      uint16_t* vl = v_tile(i);
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        u32x4 low, high;
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          const uint32_t v = codes[2 * x + w], s = scales[2 * x + w];
-          const uint32_t v0 = two_values<0>(v, scale_of(s, 0)), v1 = two_values<1>(v, scale_of(s, 1));
-          const uint32_t v2 = two_values<2>(v, scale_of(s, 2)), v3 = two_values<3>(v, scale_of(s, 3));
-          low[2 * w] = low_halves(v0, v1);
-          low[2 * w + 1] = low_halves(v2, v3);
-          high[2 * w] = high_halves(v0, v1);
-          high[2 * w + 1] = high_halves(v2, v3);
-        }
-        *reinterpret_cast<u32x4*>(vl + e * kTileKeys + (((c + x) ^ v_swizzle(e)) << 3)) = low;
-        *reinterpret_cast<u32x4*>(vl + (e + 16) * kTileKeys + (((c + x) ^ v_swizzle(e + 16)) << 3)) = high;
-      }
+      for (int step = 0; step < STEPS; ++step) v_step(i, step);
     } else {
-      const int r = piece / MD, c = piece % MD * 4;
-      uint16_t* kl = k_tile(i) + r * D;
-      const float s = scale_of(scales[0], 0);
 #pragma unroll
-      for (int w = 0; w < 4; ++w)
-        *reinterpret_cast<u32x4*>(kl + (((c + w) ^ k_swizzle<D>(r)) << 3)) =
-            u32x4{two_values<0>(codes[w], s), two_values<1>(codes[w], s), two_values<2>(codes[w], s),
-                  two_values<3>(codes[w], s)};
+      for (int step = 0; step < STEPS; ++step) k_step(i, step);
     }
   };
 
@@ -217,8 +244,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void kv4_chunk_kernel(const Kv4Chu
   f32x16 s[2];
   uint32_t pk[16];          // probabilities in pairs: pair 8 sb + j holds scores 2 j, 2 j + 1 of half sb
   float rs[2], fs[2];       // per 32-key half: sums of the rounded probabilities, of the exponentials
-  auto scores = [&](int i) __attribute__((always_inline)) {
-    const int t = tiles.at(i);
+  auto scores = [&](int i, auto with_next) __attribute__((always_inline)) {
+    constexpr int NEXT = decltype(with_next)::value;  // 1, 2: turns tile i + 1's K or V into bf16 between the MFMAs
     const uint16_t* kl = k_tile(i);
     const int kr0 = k_row_lo, kr1 = 32 + k_row_lo;
     const int ksw0 = k_swizzle<D>(kr0), ksw1 = k_swizzle<D>(kr1);
@@ -232,6 +259,11 @@ __global__ __launch_bounds__(kAttnThreads, 2) void kv4_chunk_kernel(const Kv4Chu
       a1[ks] = kfrag(kr1, ksw1, ks);
     }
     s[0] = s[1] = f32x16{};
+    auto between = [&](int mfma) __attribute__((always_inline)) {
+      constexpr int EVERY = 2 * KS / STEPS;
+      if (NEXT == 1 && mfma % EVERY == 0) k_step(i + 1, mfma / EVERY);
+      if (NEXT == 2 && mfma % EVERY == 0) v_step(i + 1, mfma / EVERY);
+    };
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       if (ks + 2 < KS) {
@@ -239,14 +271,15 @@ __global__ __launch_bounds__(kAttnThreads, 2) void kv4_chunk_kernel(const Kv4Chu
         a1[ks + 2] = kfrag(kr1, ksw1, ks + 2);
       }
       s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a0[ks], qf[ks], s[0], 0, 0, 0);
+      between(2 * ks);
+      __builtin_amdgcn_sched_barrier(0);
       s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a1[ks], qf[ks], s[1], 0, 0, 0);
+      between(2 * ks + 1);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    __builtin_amdgcn_sched_group_barrier(0x100, 4, 1);  // LDS reads
-#pragma unroll
-    for (int k = 0; k < 2 * KS; ++k) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);  // MFMA
-      if (k + 4 < 2 * KS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
-    }
+  };
+  auto mask = [&](int i) __attribute__((always_inline)) {
+    const int t = tiles.at(i);
     if (!full_for(t, first, last)) {
 #pragma unroll
       for (int sb = 0; sb < 2; ++sb) {
@@ -377,23 +410,40 @@ __global__ __launch_bounds__(kAttnThreads, 2) void kv4_chunk_kernel(const Kv4Chu
   if (tid < 4) found[tid] = 0;
   __syncthreads();
   if (i0 < i1) {
-    fetch(i0);
+    fetch(i0, raw);
+    set_apart(i0);
     convert(i0);
-    if (i0 + 1 < i1) fetch(i0 + 1);
+    if (i0 + 1 < i1) fetch(i0 + 1, kWeave ? next : raw);
     bool pending = false;  // tile i - 1's P*V is still to be made
     for (int i = i0; i < i1; ++i) {
       lds_barrier();
+      const bool more = i + 1 < i1;
       if (__builtin_amdgcn_readfirstlane(found[i % 4]) != 0) note_nan(i);
       if (tid == 0) found[(i + 2) % 4] = 0;
-      if (i + 1 < i1) convert(i + 1);
-      if (i + 2 < i1) fetch(i + 2);
+      if (kWeave) {
+        raw = next;
+        if (i + 2 < i1) fetch(i + 2, next);
+      }
+      if (more) set_apart(i + 1);
+      if (!kWeave) {
+        if (more) convert(i + 1);
+        if (i + 2 < i1) fetch(i + 2, raw);
+      }
       const bool on = seen(tiles.at(i));
       if (pending && !on) {
         pv(i - 1);
         pending = false;
       }
-      if (!on) continue;
-      scores(i);
+      if (!kWeave || !on || !more) {
+        if (kWeave && more) convert(i + 1);
+        if (!on) continue;
+        scores(i, std::integral_constant<int, 0>{});
+      } else if (takes_v) {
+        scores(i, std::integral_constant<int, 2>{});
+      } else {
+        scores(i, std::integral_constant<int, 1>{});
+      }
+      mask(i);
       if (pending) {
         pv_probs(i - 1, -m_run);
       } else {
