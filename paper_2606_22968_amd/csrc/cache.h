@@ -68,6 +68,7 @@ struct Kv4ChunkLaunch {
   WindowLaunch a;
   const uint8_t* k_scale;
   const uint8_t* v_scale;
+  bool mirrored;            // a workgroup's two row groups: the x-th from either end
 };
 
 hipError_t launch_rope_append(const RopeAppendLaunch& p, int head_dim, hipStream_t stream);

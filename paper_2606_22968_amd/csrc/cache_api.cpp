@@ -285,6 +285,14 @@ mocap_status mocap_kv4_chunk_attn(const mocap_kv4_store* kv, const int32_t* bloc
   p.a.v_pool = static_cast<const uint16_t*>(kv->v_pool);
   p.k_scale = static_cast<const uint8_t*>(kv->k_scale);
   p.v_scale = static_cast<const uint8_t*>(kv->v_scale);
+  int cus = 0;
+  st = device_cu_count(&cus);
+  if (st != MOCAP_OK) return st;
+  // Rows that see all keys before them: long and short row groups together where every
+  // workgroup starts at once (32/8/128 heads, 2048 tokens without a prefix 74 -> 60 us,
+  // behind 2048 140 -> 124), neighbours, longest first, where they follow one another (8192
+  // tokens 577 us, mirrored 645).
+  p.mirrored = window >= prefix_len + chunk_len && p.a.total_wgs <= cus;
   p.a.table = block_table;
   p.a.o = static_cast<uint16_t*>(o);
   p.a.lse = lse;

@@ -84,23 +84,30 @@ __global__ __launch_bounds__(kAttnThreads, 2) void kv4_chunk_kernel(const Kv4Chu
   const int l32 = lane & 31;
   const int P = p.prefix_len, L = p.chunk_len;
 
-  // Within a KV head: row block (the last ones first), then range; a row block's
-  // ranges share no tile, neighbouring row blocks most of them.
+  // Within a KV head: row block, then range; a row block's ranges share no tile, neighbouring
+  // row blocks most of them.
   const int logical = xcd_contiguous(blockIdx.x, p.total_wgs);
   const int per_kv = p.row_blocks * p.n_ranges;
   const int kv_head = logical / per_kv;
   const int in_kv = logical - kv_head * per_kv;
   const int range = in_kv / p.row_blocks;
-  const int block = p.row_blocks - 1 - (in_kv - range * p.row_blocks);
+  const int block = in_kv - range * p.row_blocks;
 
-  // Row r of the KV head is token r / G, head r % G.  The workgroup's and the
-  // wavefront's positions.
+  // Row r of the KV head is token r / G, head r % G.  Wavefronts 0-3 and 4-7 take 128 rows each:
+  // neighbouring row groups, the last ones first, or (mirrored) the x-th from either end,
+  // the later one for wavefronts 0-3 (its V is more work to convert than K: 60 us for 65),
+  // the middle one of an odd count alone.
   const int64_t rows_end = (int64_t)L * p.group;
-  const int wg_row0 = block * kWindowRows, row0 = wg_row0 + wave * kAttnWaveRows;
+  constexpr int kGroupRows = kWindowRows / 2;
+  const int groups = (int)((rows_end + kGroupRows - 1) / kGroupRows);
+  const int low = launch.mirrored ? block : 2 * (p.row_blocks - 1 - block);
+  const int high = launch.mirrored ? groups - 1 - block : min(low + 1, groups - 1);
+  const int row0 = ((wave < 4) == launch.mirrored ? high : low) * kGroupRows + (wave & 3) * kAttnWaveRows;
   auto token_of = [&](int64_t r) { return (int)div_by((uint32_t)min(r, rows_end - 1), p.group_magic, p.group_shift); };
-  const int wg_first = P + token_of(wg_row0), wg_last = P + token_of((int64_t)wg_row0 + kWindowRows - 1);
+  const int wg_first = P + token_of((int64_t)low * kGroupRows);
+  const int wg_last = P + token_of((int64_t)high * kGroupRows + kGroupRows - 1);
   const int first = P + token_of(row0), last = P + token_of((int64_t)row0 + kAttnWaveRows - 1);
-  const bool wave_on = row0 < rows_end;
+  const bool wave_on = row0 < rows_end && (wave < 4 || low < high);  // (equal: wavefronts 0-3 alone)
   const Tiles tiles = tiles_of(p, wg_first, wg_last), own = tiles_of(p, first, last);
   const int i0 = (int)((int64_t)tiles.count() * range / p.n_ranges);
   const int i1 = (int)((int64_t)tiles.count() * (range + 1) / p.n_ranges);
@@ -459,7 +466,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void kv4_chunk_kernel(const Kv4Chu
   // own too; the row is NaN, as with an infinite score.
   const bool beyond = m_run == INFINITY;
   const float l_tot = lane_pair_sum(l_run), f_tot = beyond ? NAN : lane_pair_sum(f_run);
-  if (row0 + l32 >= rows_end) return;
+  if (!wave_on || row0 + l32 >= rows_end) return;
   const float inv = beyond ? NAN : l_tot > 0.f ? 1.f / l_tot : 0.f;
   const float row_lse = f_tot == 0.f ? -INFINITY : (m_run + log2f(f_tot)) * kLn2;
   const int64_t out_row = (int64_t)token * p.h_q + head;
