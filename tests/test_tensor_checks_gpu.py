@@ -3,13 +3,20 @@ with the same addresses and strides."""
 import pytest
 import torch
 
-from paper_2606_22968_amd import _tensors, binding
+from paper_2606_22968_amd import binding
 
 pytestmark = pytest.mark.gpu
 
 
 class Sub(torch.Tensor):
     pass
+
+
+@pytest.fixture(scope="module")
+def ext(gpu):
+    from paper_2606_22968_amd import _tensors
+    assert binding._address is _tensors.address and binding._row_address is _tensors.rows
+    return _tensors
 
 
 def tensors():
@@ -24,25 +31,25 @@ def tensors():
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32, torch.int32, torch.uint8])
 @pytest.mark.parametrize("ndim", [-1, 0, 1, 3])
-def test_addresses(gpu, dtype, ndim):
+def test_addresses(ext, dtype, ndim):
     for t in tensors():
         for device in (0, 1):
             want = None
             if type(t) in (torch.Tensor, torch.nn.Parameter) and t.layout is torch.strided and t.dtype is dtype and t.is_contiguous() and \
                     t.device == torch.device("cuda", device) and (ndim < 0 or t.dim() == ndim):
                 want = t.data_ptr()
-            assert _tensors.address(t, dtype, ndim, device) == want
+            assert ext.address(t, dtype, ndim, device) == want
 
 
-def test_rows(gpu):
+def test_rows(ext):
     for t in tensors():
         want = None
         if type(t) in (torch.Tensor, torch.nn.Parameter) and t.layout is torch.strided and t.dtype is torch.bfloat16 and t.is_cuda and \
                 t.dim() == 3 and t.stride(2) == 1 and (t.stride(1) == t.shape[2] or t.shape[1] <= 1):
             n, h, d = t.shape
             want = (t.data_ptr(), t.stride(0) if n > 1 else h * d, n, h, d)
-        assert _tensors.rows(t, 0) == want
-        assert _tensors.rows(t, 1) is None
+        assert ext.rows(t, 0) == want
+        assert ext.rows(t, 1) is None
 
 
 def test_parameters_and_subclasses_pass_all_the_same(gpu):
@@ -54,9 +61,9 @@ def test_parameters_and_subclasses_pass_all_the_same(gpu):
         binding._need(x, torch.bfloat16, "x", 3, 1)
 
 
-def test_wrong_calls():
+def test_wrong_calls(ext):
     for args in ((), (None,), (None, 3, 1, 0), (None, torch.uint8, "a", 0)):
         with pytest.raises(TypeError):
-            _tensors.address(*args)
+            ext.address(*args)
     with pytest.raises(TypeError):
-        _tensors.rows(None)
+        ext.rows(None)
