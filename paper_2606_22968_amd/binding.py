@@ -1,4 +1,4 @@
-"""ctypes binding of libmocap_attn (argument marshalling only).
+"""Binding of libmocap_attn through ctypes (argument marshalling only).
 
 Each function carries the name of the C entry point it wraps and does no
 arithmetic of its own: it checks tensor dtypes, devices, shapes and
@@ -11,6 +11,25 @@ import os
 from typing import List, Optional, Sequence, Tuple
 
 import torch
+
+try:  # shortcuts in C++ (csrc/marshal.cpp): checks of a tensor in 0.1 us, and whole calls
+    from . import _marshal
+    _address, _row_address = _marshal.address, _marshal.rows
+except ImportError:
+    _marshal = None
+
+    def _address(t, dtype, ndim: int, device: int) -> Optional[int]:
+        if type(t) is torch.Tensor and t.dtype is dtype and t.get_device() == device and t.is_contiguous() and \
+                (ndim < 0 or t.dim() == ndim):
+            return t.data_ptr()
+        return None
+
+    def _row_address(t, device: int):
+        if type(t) is torch.Tensor and t.dtype is torch.bfloat16 and t.dim() == 3 and t.get_device() == device:
+            (tokens, heads, d), stride = t.shape, t.stride()
+            if stride[2] == 1 and (heads <= 1 or stride[1] == d):
+                return t.data_ptr(), stride[0] if tokens > 1 else heads * d, tokens, heads, d
+        return None
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmocap_attn.so")
@@ -254,6 +273,8 @@ def load_library():
     for name, argtypes in serve.items():
         f = getattr(lib, name)
         f.restype, f.argtypes = st, argtypes
+        if _marshal is not None and hasattr(_marshal, name):
+            _marshal.bind(name, ctypes.cast(f, ctypes.c_void_p).value)
     _lib = lib
     return lib
 
@@ -588,23 +609,6 @@ def mocap_lbcp_refine_e2e(seq_len: int, num_chunks: int, num_stages: int, align:
 
 
 # ---- After the prefill (mocap_serve.h) ----
-
-try:  # the same checks in C++ (csrc/tensors.cpp), 0.1 us a tensor for 0.3 to 0.5
-    from ._tensors import address as _address, rows as _row_address
-except ImportError:
-    def _address(t, dtype, ndim: int, device: int) -> Optional[int]:
-        if type(t) is torch.Tensor and t.dtype is dtype and t.get_device() == device and t.is_contiguous() and \
-                (ndim < 0 or t.dim() == ndim):
-            return t.data_ptr()
-        return None
-
-    def _row_address(t, device: int):
-        if type(t) is torch.Tensor and t.dtype is torch.bfloat16 and t.dim() == 3 and t.get_device() == device:
-            (tokens, heads, d), stride = t.shape, t.stride()
-            if stride[2] == 1 and (heads <= 1 or stride[1] == d):
-                return t.data_ptr(), stride[0] if tokens > 1 else heads * d, tokens, heads, d
-        return None
-
 
 def _need(t: torch.Tensor, dtype, name: str, ndim: Optional[int], device: int) -> int:
     """The address of a contiguous tensor of this type on the current device, where the call enqueues its work."""
@@ -946,6 +950,18 @@ def _rope_rows(store, k: torch.Tensor, v: torch.Tensor, rope: Optional[Rope], q:
     return tokens, desc, (q_ptr, q_stride, h_q, k_ptr, k_stride, v_ptr, v_stride, out_ptr)
 
 
+def _short(call: str, device: int, stream, *args) -> bool:
+    """Makes the call through the C++ shortcut; False where that leaves it to the long way."""
+    if _marshal is None or _check_tables:
+        return False
+    if _lib is None:
+        load_library()
+    status = getattr(_marshal, call)(*args, _stream_on(stream, device), device)
+    if status:
+        raise MocapError(status, call)
+    return status is not None
+
+
 def _append_chunk(call: str, desc, store, block_table: torch.Tensor, start_pos: int, k: torch.Tensor, v: torch.Tensor,
                   rope: Optional[Rope], position: Optional[int], q: Optional[torch.Tensor],
                   q_out: Optional[torch.Tensor], stream, device: int) -> None:
@@ -979,6 +995,8 @@ def mocap_rope_append(store: KvStore, block_table: torch.Tensor, start_pos: int,
     projection's rows); q_out: bf16 [chunk_len][h_q][head_dim].  position: the rotation's, of the first token (None:
     start_pos)."""
     device = _raw_device()
+    if _short("mocap_rope_append", device, stream, store, block_table, start_pos, k, v, rope, position, q, q_out):
+        return
     _append_chunk("mocap_rope_append", _store_on(store, device), store, block_table, start_pos, k, v, rope, position, q,
                   q_out, stream, device)
 
@@ -989,6 +1007,8 @@ def mocap_decode_rope_append(store: KvStore, block_tables: torch.Tensor, seq_len
                              stream=None) -> None:
     """Row b of k, v and q is the new token of sequence b; positions: int32 [batch], the rotation's (None: seq_lens - 1)."""
     device = _raw_device()
+    if _short("mocap_decode_rope_append", device, stream, store, block_tables, seq_lens, k, v, rope, positions, q, q_out):
+        return
     _append_batch("mocap_decode_rope_append", _store_on(store, device), store, block_tables, seq_lens, k, v, rope,
                   positions, q, q_out, stream, device)
 
@@ -998,6 +1018,8 @@ def mocap_kv4_append(store: Kv4Store, block_table: torch.Tensor, start_pos: int,
                      q_out: Optional[torch.Tensor] = None, stream=None) -> None:
     """As mocap_rope_append, into a 4-bit store."""
     device = _raw_device()
+    if _short("mocap_kv4_append", device, stream, store, block_table, start_pos, k, v, rope, position, q, q_out):
+        return
     _append_chunk("mocap_kv4_append", _store4_on(store, device), store, block_table, start_pos, k, v, rope, position, q,
                   q_out, stream, device)
 
@@ -1008,6 +1030,8 @@ def mocap_kv4_decode_append(store: Kv4Store, block_tables: torch.Tensor, seq_len
                             stream=None) -> None:
     """As mocap_decode_rope_append, into a 4-bit store."""
     device = _raw_device()
+    if _short("mocap_kv4_decode_append", device, stream, store, block_tables, seq_lens, k, v, rope, positions, q, q_out):
+        return
     _append_batch("mocap_kv4_decode_append", _store4_on(store, device), store, block_tables, seq_lens, k, v, rope,
                   positions, q, q_out, stream, device)
 
@@ -1016,6 +1040,8 @@ def mocap_kv4_load(store: Kv4Store, block_tables: torch.Tensor, ends: torch.Tens
                    stream=None) -> None:
     """k, v: bf16 [batch][n][h_kv][head_dim], the values of the last n of the positions [0, ends[b]) of sequence b."""
     device = _raw_device()
+    if _short("mocap_kv4_load", device, stream, store, block_tables, ends, k, v):
+        return
     k_ptr = _need(k, torch.bfloat16, "k", 4, device)
     v_ptr = _need(v, torch.bfloat16, "v", 4, device)
     tables_ptr, ends_ptr, batch, stride, _ = _batch(store, block_tables, ends, None, device, window=k.shape[1],
@@ -1041,6 +1067,8 @@ def mocap_kv4_decode_attn(store: Kv4Store, block_tables: torch.Tensor, seq_lens:
                           workspace: Optional[torch.Tensor] = None, window: int = 0, sinks: int = 0, stream=None) -> None:
     """As mocap_decode_attn, over a 4-bit store."""
     device = _raw_device()
+    if _short("mocap_kv4_decode_attn", device, stream, store, block_tables, seq_lens, q, max_len, scale, o, lse, workspace, window, sinks):
+        return
     window, sinks = int(window), int(sinks)
     tables_ptr, lens_ptr, batch, stride, max_len = _batch(store, block_tables, seq_lens, max_len, device, window, sinks)
     q_ptr = _need(q, torch.bfloat16, "q", 3, device)
@@ -1072,6 +1100,8 @@ def mocap_kv4_chunk_attn(store: Kv4Store, block_table: torch.Tensor, q: torch.Te
                          sinks: int = 0, num_splits: int = 0, stream=None) -> None:
     """As mocap_chunk_attn (window 0) or mocap_window_attn, over a 4-bit store."""
     device = _raw_device()
+    if _short("mocap_kv4_chunk_attn", device, stream, store, block_table, q, prefix_len, scale, o, lse, workspace, window, sinks, num_splits):
+        return
     table_ptr = _need(block_table, torch.int32, "block_table", 1, device)
     q_ptr = _need(q, torch.bfloat16, "q", 3, device)
     o_ptr = _need(o, torch.bfloat16, "o", 3, device)

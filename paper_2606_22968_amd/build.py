@@ -57,34 +57,34 @@ def build(verbose: bool = False, extra_flags=(), lib_path: str = LIB, build_dir:
     _check_stubs(tmp)
     os.replace(tmp, lib_path)
     if lib_path == LIB:
-        build_tensors(verbose)
+        build_marshal(verbose)
     return lib_path
 
 
-TENSORS = os.path.join(PKG, "_tensors.so")
+MARSHAL = os.path.join(PKG, "_marshal.so")
 
 
-def build_tensors(verbose: bool = False) -> str:
-    """The binding's tensor checks (csrc/tensors.cpp): a Python extension over torch's headers, host code only."""
+def build_marshal(verbose: bool = False) -> str:
+    """The binding's shortcuts (csrc/marshal.cpp): a Python extension over torch's headers, host code only."""
     import sysconfig
 
     import torch
     from torch.utils import cpp_extension
     includes = [*cpp_extension.include_paths(), sysconfig.get_path("include")]
     lib_dir = os.path.join(os.path.dirname(torch.__file__), "lib")
-    tmp = TENSORS + ".tmp"
+    tmp = MARSHAL + ".tmp"
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-w",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
-           *(f"-isystem{i}" for i in includes), os.path.join(CSRC, "tensors.cpp"), "-o", tmp,
+           *(f"-isystem{i}" for i in includes), f"-I{INCLUDE}", os.path.join(CSRC, "marshal.cpp"), "-o", tmp,
            f"-L{lib_dir}", "-lc10", "-ltorch_cpu", "-ltorch_python"]
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         sys.stderr.write(res.stdout + res.stderr)
-        raise RuntimeError("g++ failed on tensors.cpp")
-    os.replace(tmp, TENSORS)
-    return TENSORS
+        raise RuntimeError("g++ failed on marshal.cpp")
+    os.replace(tmp, MARSHAL)
+    return MARSHAL
 
 
 def _check_stubs(lib: str) -> None:
