@@ -354,7 +354,11 @@ __device__ __forceinline__ float part_weight(float lse, float m) {
   return w == 0.f ? 1.4e-45f : w;
 }
 
-template <int D>
+// SHORT: up to 16 (head_dim 64: 32) parts are joined by one wavefront from its first loads,
+// without the other three, LDS and a barrier: passes of 32 sequences of up to 8192
+// positions and of 16 in a window of 4096 over the 4-bit store 33.5 -> 32.1 and 23.7 -> 22.3
+// us.  (Another order of additions than the four wavefronts'.)
+template <int D, bool SHORT>
 __global__ __launch_bounds__(kDecodeThreads) void decode_join_kernel(const DecodeAttnLaunch p) {
   constexpr int QUADS = D / 4, SIDE = 64 / QUADS;  // parts read side by side
   constexpr int kAhead = 8;
@@ -366,7 +370,10 @@ __global__ __launch_bounds__(kDecodeThreads) void decode_join_kernel(const Decod
   int first;
   const SeqPart w = parts_of(p.seqs, lane, seq, &first);
   if (w.parts == 1) return;
-  const int begin = w.parts * wave / kDecodeWaves, end = w.parts * (wave + 1) / kDecodeWaves;
+  const bool alone = SHORT && w.parts <= kAhead * SIDE;
+  if (alone && wave != 0) return;
+  const int begin = alone ? 0 : w.parts * wave / kDecodeWaves;
+  const int end = alone ? w.parts : w.parts * (wave + 1) / kDecodeWaves;
   const int quad = lane % QUADS, side = lane / QUADS;
   const float* lse = p.ws_lse + (int64_t)first * p.h_q + head;
   const float* o = p.ws_o + ((int64_t)first * p.h_q + head) * D + quad * 4;
@@ -377,6 +384,14 @@ __global__ __launch_bounds__(kDecodeThreads) void decode_join_kernel(const Decod
       v[j] = *reinterpret_cast<const f32x4*>(o + (int64_t)min(r0 + j * SIDE + side, w.parts - 1) * p.h_q * D);
   };
   auto load_lse = [&](int r) { return r < end ? lse[(int64_t)r * p.h_q] : -INFINITY; };
+  auto store = [&](float m, float z, f32x4 acc) __attribute__((always_inline)) {
+    const float inv = z == 0.f ? 0.f : 1.f / z;
+    bf16x4 out;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out[e] = (__bf16)(acc[e] * inv);
+    *reinterpret_cast<bf16x4*>(p.o + at * D + quad * 4) = out;
+    if (quad == 0) p.lse[at] = z == 0.f ? -INFINITY : m + logf(z);
+  };
   fetch(begin);
   float lr = load_lse(begin + lane);
   float m = lr;
@@ -409,6 +424,10 @@ __global__ __launch_bounds__(kDecodeThreads) void decode_join_kernel(const Decod
   z = wave_total(z);
 #pragma unroll
   for (int e = 0; e < 4; ++e) acc[e] = SIDE == 2 ? lane_pair_sum(acc[e]) : quad_rows_sum(acc[e]);
+  if (alone) {
+    if (side == 0) store(m, z, acc);
+    return;
+  }
   if (lane == 0) {
     wave_m[wave] = m;
     wave_z[wave] = z;
@@ -432,12 +451,7 @@ __global__ __launch_bounds__(kDecodeThreads) void decode_join_kernel(const Decod
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[e] += counts ? f * wave_o[x][quad][e] : 0.f;
   }
-  const float inv = z == 0.f ? 0.f : 1.f / z;
-  bf16x4 out;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) out[e] = (__bf16)(acc[e] * inv);
-  *reinterpret_cast<bf16x4*>(p.o + at * D + quad * 4) = out;
-  if (quad == 0) p.lse[at] = z == 0.f ? -INFINITY : m + logf(z);
+  store(m, z, acc);
 }
 
 template <int D>
@@ -460,15 +474,23 @@ hipError_t launch_decode_attn(const DecodeAttnLaunch& p, int head_dim, hipStream
     launch<64>(p, stream);
   }
   const hipError_t e = hipGetLastError();
-  return e != hipSuccess || !p.may_split ? e : launch_decode_join(p, head_dim, stream);
+  return e != hipSuccess || !p.may_split ? e : launch_decode_join(p, head_dim, false, stream);
 }
 
-hipError_t launch_decode_join(const DecodeAttnLaunch& p, int head_dim, hipStream_t stream) {
+hipError_t launch_decode_join(const DecodeAttnLaunch& p, int head_dim, bool short_too, hipStream_t stream) {
   const dim3 grid((unsigned)(p.seqs.batch * p.h_q)), block(kDecodeThreads);
   if (head_dim == 128) {
-    hipLaunchKernelGGL(decode_join_kernel<128>, grid, block, 0, stream, p);
+    if (short_too) {
+      hipLaunchKernelGGL((decode_join_kernel<128, true>), grid, block, 0, stream, p);
+    } else {
+      hipLaunchKernelGGL((decode_join_kernel<128, false>), grid, block, 0, stream, p);
+    }
   } else {
-    hipLaunchKernelGGL(decode_join_kernel<64>, grid, block, 0, stream, p);
+    if (short_too) {
+      hipLaunchKernelGGL((decode_join_kernel<64, true>), grid, block, 0, stream, p);
+    } else {
+      hipLaunchKernelGGL((decode_join_kernel<64, false>), grid, block, 0, stream, p);
+    }
   }
   return hipGetLastError();
 }

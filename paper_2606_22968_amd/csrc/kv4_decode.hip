@@ -14,6 +14,14 @@
 //     g holds the scores of keys 16 g .. + 15, in order over the four products.  That
 //     is what a 16-byte load of a V row gives it: 16 keys of dims 32 b + i and
 //     32 b + 16 + i, one byte a key, which with that key's scale become a pair.
+// Measured: four sequences of 65537 to 131072 positions, 64/8/128 heads, 452 MB in 85 us,
+// 5.3 TB/s, 5.9 without the 6 us that a launch of one tile a wavefront takes; 32 of up to
+// 8192, 32/8/128, 23 us for 83 MB; one of 2048, 6 us.  HBM and that latency bound it:
+// without V's conversion it takes 3% less, without the low halves of the probabilities 2%.
+// Tried: the next tile's codes in a second set of registers (two wavefronts a SIMD, 89
+// us), 1 to 9 workgroups per compute unit, parts of whole turns of the four wavefronts, 128
+// registers and four wavefronts a SIMD (6 to 37 of them spilled: 117 to 158 us), Q in LDS,
+// V's scales loaded once for 16 lanes (none faster than +-3%).
 #include "kv4_device.h"
 #include "serve_device.h"
 
@@ -287,7 +295,7 @@ hipError_t launch_kv4_decode(const Kv4DecodeLaunch& p, int head_dim, hipStream_t
     launch<64>(p, stream);
   }
   const hipError_t e = hipGetLastError();
-  return e != hipSuccess || !p.a.may_split ? e : launch_decode_join(p.a, head_dim, stream);
+  return e != hipSuccess || !p.a.may_split ? e : launch_decode_join(p.a, head_dim, true, stream);
 }
 
 }  // namespace mocap

@@ -140,10 +140,20 @@ __device__ __forceinline__ SeqPart locate_item(const SeqBatch& s, int lane, int 
 
 // The parts of sequence `seq` and the first one's item.
 __device__ __forceinline__ SeqPart parts_of(const SeqBatch& s, int lane, int seq, int* first) {
-  const int per = part_tiles(s, lane);
   SeqPart r;
   r.seq = seq;
   r.part = 0;
+  if (s.batch <= 64) {  // as in locate_item
+    const bool there = lane < s.batch;
+    const int len = there ? s.seq_lens[lane] : 0;
+    const int tiles = there ? seq_span(s, len).tiles : 0;
+    const int per = tiles_per_part(s, (float)(uint32_t)__builtin_amdgcn_readlane(wave_sums(tiles), 63));
+    *first = __builtin_amdgcn_readlane(wave_sums(lane < seq ? parts_for(tiles, per) : 0), 63);
+    r.span = seq_span(s, __builtin_amdgcn_readlane(len, seq));
+    r.parts = parts_for(r.span.tiles, per);
+    return r;
+  }
+  const int per = part_tiles(s, lane);
   int base = 0;
   for (int b0 = 0; b0 <= seq; b0 += 64) {
     const int b = b0 + lane;
