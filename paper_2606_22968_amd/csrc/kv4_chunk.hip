@@ -39,8 +39,9 @@ __device__ __forceinline__ uint32_t div_by(uint32_t n, uint32_t magic, int shift
   return (__umulhi(n, magic) + n) >> shift;
 }
 
-// Whether some byte of a word of scales is kScaleNan (bits 7, 15, 23 or 31).
-__device__ __forceinline__ uint32_t nan_bytes(uint32_t x) { return ((x & 0x7F7F7F7Fu) + 0x01010101u) & x & 0x80808080u; }
+// Bytes of a word of scales that are kScaleNan, or more than any stored position's (253 and
+// 254 make infinities): bits 7, 15, 23 and 31.
+__device__ __forceinline__ uint32_t beyond_252(uint32_t x) { return ((x & 0x7F7F7F7Fu) + 0x03030303u) & x & 0x80808080u; }
 
 // The tiles of a run of rows at positions [first, last]: the sinks' [0, sinks),
 // then [begin, end).
@@ -169,16 +170,16 @@ __global__ __launch_bounds__(kAttnThreads, 2) void kv4_chunk_kernel(const Kv4Chu
     }
   };
   // Where all rows see a whole tile, a NaN value block reaches all of them as NaN; in other
-  // tiles it is noted and its scale set next to 0 (unwritten scales may be NaN as well).
+  // tiles it is noted and its scale set next to 0, as are scales of unwritten positions.
   auto set_apart = [&](int i) __attribute__((always_inline)) {
     if (!takes_v || full_for(tiles.at(i), wg_first, wg_last)) return;
     uint32_t bad = 0;
 #pragma unroll
-    for (int w = 0; w < WORDS; ++w) bad |= nan_bytes(raw.scales[w]);
+    for (int w = 0; w < WORDS; ++w) bad |= beyond_252(raw.scales[w]);
     if (bad == 0) return;
     found[i % 4] = 1;
 #pragma unroll
-    for (int w = 0; w < WORDS; ++w) raw.scales[w] &= ~((nan_bytes(raw.scales[w]) >> 7) * 0xFFu);
+    for (int w = 0; w < WORDS; ++w) raw.scales[w] &= ~((beyond_252(raw.scales[w]) >> 7) * 0xFFu);
   };
   // Turns the fetched codes into bf16 in the stages of tile i, in STEPS steps.
   u32x4 out[2];

@@ -242,6 +242,46 @@ def test_nan_blocks(gpu, d, window, sinks):
             assert ((got.double() - ref.o[0, g]).abs() <= bound[0, g])[~want].all()
 
 
+@pytest.mark.parametrize("fill", [0x00, 0x7F, 0xFC, 0xFD, 0xFE, 0xFF])
+@pytest.mark.parametrize("d", [64, 128])
+def test_whatever_unwritten_memory_holds(gpu, fill, d):
+    """Codes and scales of no position, and of positions behind a row, may be anything: scales beyond those that are
+    stored make infinities of their codes."""
+    lens = [1, 63, 65, 130]
+    _, store, tables, ks, vs = make_store4(190, lens, 192, 2, d, fill=fill)
+    q = randn(191, len(lens), 8, d).cuda()
+    o, lse = decode(store, tables, lens, q, 192, d ** -0.5)
+    check_decode(o, lse, q, ks, vs, lens, d ** -0.5)
+    for b, n in enumerate(lens):
+        for splits in (1, 2):
+            rows = randn(192 + b, n, 8, d)
+            o, lse, _ = chunk(store, tables[b].contiguous(), rows.cuda(), 0, d ** -0.5, splits=splits)
+            ref = Attention(rows, ks[b], vs[b], 0, d ** -0.5)
+            check_close(o, ref.o, ref.o_bound(CHUNK_ERROR), f"o n={n}")
+            check_close(lse, ref.lse, ref.lse_bound(), f"lse n={n}")
+
+
+def test_rows_of_larger_arrays(gpu):
+    """Tables, lengths and LSE need their type's alignment only."""
+    _, store, tables, ks, vs = make_store4(195, [300, 300], 64, 2, 64)
+    def apart(x):
+        return torch.cat((x.flatten()[:1], x.flatten()))[1:].view(x.shape)
+
+    q, lens = randn(196, 2, 4, 64).cuda(), torch.tensor([300, 77], dtype=torch.int32, device="cuda")
+    o, lse = torch.empty_like(q), apart(torch.zeros((2, 4), device="cuda"))
+    binding.mocap_kv4_decode_attn(store, apart(tables), apart(lens), q, 320, 0.125, o, lse,
+                                  torch.empty(1 << 20, dtype=torch.uint8, device="cuda"))
+    check_decode(o, lse, q, ks, vs, [300, 77], 0.125)
+    rows = randn(197, 40, 4, 64)
+    o, lse = torch.empty_like(rows, device="cuda"), apart(torch.zeros((4, 40), device="cuda"))
+    assert lse.data_ptr() % 16 == 4
+    binding.mocap_kv4_chunk_attn(store, apart(tables[1]), rows.cuda(), 260, 0.125, o, lse,
+                                 torch.empty(1 << 20, dtype=torch.uint8, device="cuda"))
+    ref = Attention(rows, ks[1], vs[1], 260, 0.125)
+    check_close(o, ref.o, ref.o_bound(CHUNK_ERROR), "o")
+    check_close(lse, ref.lse, ref.lse_bound(), "lse")
+
+
 def test_extreme_scales(gpu):
     """Scale bytes 2 and 252, and blocks of zeros, next to ordinary ones."""
     n, d = 130, 64
