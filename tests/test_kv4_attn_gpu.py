@@ -373,6 +373,35 @@ def test_chunk_on_another_stream_and_in_a_graph(gpu):
         assert torch.equal(o, o2) and torch.equal(lse, lse2)
 
 
+def test_two_calls_at_once(gpu):
+    """Chunks and batches of two streams over one store, with workspaces and outputs of their own."""
+    n, rows, d = 3000, 60, 64
+    _, store, tables, ks, vs = make_store4(165, [n, n - 100], 64, 2, d)
+    lens = torch.tensor([n, n - 100], dtype=torch.int32, device="cuda")
+    q, q1 = randn(166, 2, rows, 8, d).cuda(), randn(167, 2, 2, 8, d).cuda()
+    chunk_size = binding.mocap_kv4_chunk_attn_workspace_size(n - 100 - rows, rows, 8, 2, d)[1]
+    batch_size = binding.mocap_kv4_decode_attn_workspace_size(2, 8, 2, d, n)
+    assert chunk_size > 0 and batch_size > 0
+    streams, outs = [torch.cuda.Stream() for _ in range(2)], []
+    for i in range(2):
+        ws = [torch.empty(x, dtype=torch.uint8, device="cuda") for x in (chunk_size, batch_size)]
+        o, lse = torch.empty_like(q[i]), torch.empty((8, rows), device="cuda")
+        o1, lse1 = torch.empty_like(q1[i]), torch.empty((2, 8), device="cuda")
+        outs.append((ws, o, lse, o1, lse1))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i, (ws, o, lse, o1, lse1) in enumerate(outs):
+            binding.mocap_kv4_chunk_attn(store, tables[i], q[i], n - 100 - rows, 0.125, o, lse, ws[0], stream=streams[i])
+            binding.mocap_kv4_decode_attn(store, tables, lens, q1[i], n, 0.125, o1, lse1, ws[1], stream=streams[i])
+    torch.cuda.synchronize()
+    for i, (_, o, lse, o1, lse1) in enumerate(outs):
+        alone = chunk(store, tables[i], q[i], n - 100 - rows, 0.125)
+        assert torch.equal(o, alone[0]) and torch.equal(lse, alone[1])
+        alone = decode(store, tables, lens.tolist(), q1[i], n, 0.125)
+        assert torch.equal(o1, alone[0]) and torch.equal(lse1, alone[1])
+        check_decode(o1, lse1, q1[i], ks, vs, lens.tolist(), 0.125)
+
+
 def test_store_beyond_32_bits(gpu):
     """Pools of more than 2^32 bytes: the sequence lies in the last blocks."""
     bs, h_kv, d, n = 1600, 8, 128, 3300
@@ -392,8 +421,17 @@ def test_store_beyond_32_bits(gpu):
     k, v = randn(172, 70, h_kv, d), randn(173, 70, h_kv, d)
     binding.mocap_kv4_append(store, table, n - 40, k.cuda(), v.cuda())
     pools.put(tables[0], n - 40, k, v)
+    binding.mocap_kv4_decode_append(store, table[None], torch.tensor([2], dtype=torch.int32, device="cuda"), k[:1].cuda(),
+                                    v[:1].cuda())
+    pools.put(tables[0], 1, k[:1], v[:1])
     for name in Pools4.NAMES:
         assert torch.equal(getattr(store, name)[blocks - 3:].cpu(), getattr(pools, name)), name
+    far, near = ([torch.empty((1, n + 30, h_kv, d), dtype=torch.bfloat16, device="cuda") for _ in range(2)] for _ in range(2))
+    ends = torch.tensor([n + 30], dtype=torch.int32, device="cuda")
+    binding.mocap_kv4_load(store, table[None], ends, *far)
+    binding.mocap_kv4_load(pools.to_gpu(), tables, ends, *near)
+    for a, b in zip(far, near):
+        assert torch.equal(a, b)
 
 
 def test_refusals(gpu):

@@ -173,6 +173,56 @@ def test_batches(gpu, four, h_q, h_kv, d, rot, interleaved, given):
         assert same_bits(store.k_pool, k_pool) and same_bits(store.v_pool, v_pool)
 
 
+@pytest.mark.parametrize("four", [False, True])
+def test_positions_of_either_sign(gpu, four):
+    """A batch's rotation positions are any int32, apart from the slots."""
+    at = torch.tensor([-1, -(1 << 31), (1 << 31) - 1, -70000, 0], dtype=torch.int32)
+    batch, h_kv, d, bs = at.numel(), 2, 64, 64
+    lens = torch.arange(1, batch + 1, dtype=torch.int32)
+    tables = torch.arange(batch, dtype=torch.int32)[:, None].contiguous()
+    rope, freq = rope_of(d, False)
+    q, k, v = tokens(70, batch, 4, h_kv, d, True)
+    q_out = torch.empty((batch, 4, d), dtype=torch.bfloat16, device="cuda")
+    want_k, k_size = rotate(k.cpu(), at, freq, False)
+    want_q, q_size = rotate(q.cpu(), at, freq, False)
+    if four:
+        pools = Pools4(batch, bs, h_kv, d, fill=0)
+        store = pools.to_gpu()
+        binding.mocap_kv4_decode_append(store, tables.cuda(), lens.cuda(), k, v, rope, at.cuda(), q, q_out)
+        for b in range(batch):
+            pools.put(tables[b], int(lens[b]) - 1, want_k[b:b + 1], v[b:b + 1].cpu())
+        pools.same_as(store, "either sign")
+    else:
+        store = binding.KvStore(batch, bs, h_kv, d, fill=0.0)
+        binding.mocap_decode_rope_append(store, tables.cuda(), lens.cuda(), k, v, rope, at.cuda(), q, q_out)
+        got = store.k_pool.cpu()[torch.arange(batch), :, lens.long() - 1]
+        check_close(got, want_k, rotated_bound(want_k, k_size), "k")
+    check_close(q_out, want_q, rotated_bound(want_q, q_size), "q")
+
+
+def test_store_beyond_32_bits(gpu):
+    """A bf16 store of more than 2^32 values a pool: the positions lie in the last blocks."""
+    bs, h_kv, d, blocks = 1600, 8, 128, 2700
+    store = binding.KvStore(blocks, bs, h_kv, d)
+    assert store.k_pool.numel() > 1 << 32
+    store.k_pool[-2:], store.v_pool[-2:] = 0.0, 0.0
+    table = torch.tensor([blocks - 1, blocks - 2], dtype=torch.int32)
+    rope, freq = rope_of(d, False)
+    k, v = randn(80, 71, h_kv, d), randn(81, 71, h_kv, d)
+    binding.mocap_rope_append(store, table.cuda(), bs - 40, k[:70].cuda(), v[:70].cuda(), rope)
+    binding.mocap_decode_rope_append(store, table[None].cuda(), torch.tensor([bs + 31], dtype=torch.int32, device="cuda"),
+                                     k[70:].cuda(), v[70:].cuda(), rope)
+    at = bs - 40 + torch.arange(71)
+    want, size = rotate(k, at, freq, False)
+    small_k, small_v = store.k_pool[-2:].cpu(), store.v_pool[-2:].cpu()
+    near = table - (blocks - 2)
+    got = small_k[near.long()[at // bs], :, at % bs]
+    check_close(got, want, rotated_bound(want, size), "k")
+    k_pool, v_pool = torch.zeros_like(small_k), torch.zeros_like(small_v)
+    put(k_pool, v_pool, near, bs, bs - 40, got, v)
+    assert same_bits(small_k, k_pool) and same_bits(small_v, v_pool)
+
+
 def test_rounding_to_four_bits(gpu):
     """Every border between codes and scales, in blocks of their own: exact ties, their neighbours in bf16, powers of
     two, the least and the largest magnitudes, zeros of both signs, NaN and infinities."""
