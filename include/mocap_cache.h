@@ -144,8 +144,9 @@ mocap_status mocap_kv4_load(const mocap_kv4_store* kv, const int32_t* block_tabl
 /*
  * mocap_kv4_decode_attn_workspace_size, mocap_kv4_decode_attn --
  * mocap_decode_attn over a 4-bit store: the same arguments, results, precision
- * and errors, with the values that the store stands for.  A key block that reads
- * as NaN makes the rows that see it NaN, a value block its 32 dims of them.
+ * and errors (but blocks of any size are taken), with the values that the store
+ * stands for.  A key block that reads as NaN makes the rows that see it NaN, a
+ * value block its 32 dims of them.
  */
 mocap_status mocap_kv4_decode_attn_workspace_size(int32_t batch, int64_t max_len, int32_t h_q, int32_t h_kv,
                                                   int32_t head_dim, int64_t window, int64_t sinks, size_t* bytes_out);
@@ -162,7 +163,7 @@ mocap_status mocap_kv4_decode_attn(const mocap_kv4_store* kv, const int32_t* blo
  * values are read from the store as well.  num_splits as in
  * mocap_window_attn_workspace_size.  NaN blocks reach exactly the rows that see
  * them, as in mocap_kv4_decode_attn.
- * Errors: as mocap_window_attn, with window = 0 allowed.
+ * Errors: as mocap_window_attn, but window = 0 and blocks of any size are taken.
  */
 mocap_status mocap_kv4_chunk_attn_workspace_size(int64_t prefix_len, int32_t chunk_len, int32_t h_q, int32_t h_kv,
                                                  int32_t head_dim, int64_t window, int64_t sinks, int32_t num_splits,

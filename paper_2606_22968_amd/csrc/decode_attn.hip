@@ -94,7 +94,7 @@ __global__ __launch_bounds__(kDecodeThreads) void decode_attn_kernel(const Decod
   const int kv_head = work - item * p.h_kv;
   const int head0 = (in_stripe >> 3) * (NT * 16);  // of the group
   if (item >= p.seqs.items) return;
-  const SeqPart w = locate_item(p.seqs, lane, item);
+  const SeqPart w = locate_item<false>(p.seqs, lane, item);
   if (w.seq == p.seqs.batch) return;
   int begin, end;
   part_range(w, &begin, &end);

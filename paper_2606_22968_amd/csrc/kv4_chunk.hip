@@ -13,10 +13,13 @@
 //   * A value block that reads as NaN is left to the product where all rows of the
 //     workgroup see its tile.  In other tiles its scale is set next to 0, and the rows
 //     that see it get NaN in its dims at the end.
-// Measured: 2048 tokens of 32/8/128 heads behind 30720, 993 us, 1.07 PFLOP/s; issue and
-// power bound it, as in chunk_attn.hip (the median of 30 in a row is 1055).  The
-// conversion is 5.5% of it, half of that the stores to LDS.  Looking a table entry up a
-// tile ahead changes nothing.
+// Measured: 2048 tokens of 32/8/128 heads behind 30720, 960 to 1010 us by the card, 1.05 to
+// 1.11 PFLOP/s.  Issue bounds it: MFMAs hold 45% of the SIMDs' cycles, a third of those beside
+// vector instructions (2.3 GHz).  The conversion is 5.5% of it, half of that the stores to LDS.
+// Tried: a table entry looked up a tile ahead (no difference); pieces dealt to the lanes so
+// that those stores, 16 lanes over 32 banks, meet no bank twice, with loads 64 bytes apart
+// (1% more); the conversion of wavefronts 0-3 or 4-7 between the scores and the products or
+// after them (0 to 3% more), of all (10 to 14%).
 #include "kv4_device.h"
 
 #include <type_traits>

@@ -113,10 +113,14 @@ __device__ __forceinline__ bool find_item(const SeqBatch& s, int item, int b0, i
   r->span = seq_span(s, __builtin_amdgcn_readlane(len, at));
   return true;
 }
+// AT_ONCE: one load of the lengths where they fit in a wavefront, at the head of a chain of
+// loads.  Decoding over the bf16 store goes without: for 32 sequences of up to 8192 positions
+// 68 us, with it 70 (two registers more), one of 572 9.0 and 8.75.
+template <bool AT_ONCE = true>
 __device__ __forceinline__ SeqPart locate_item(const SeqBatch& s, int lane, int item) {
   SeqPart r;
   r.seq = s.batch;
-  if (s.batch <= 64) {  // one load of the lengths, at the head of a chain of loads
+  if (AT_ONCE && s.batch <= 64) {
     const bool there = lane < s.batch;
     const int len = there ? s.seq_lens[lane] : 0;
     const int tiles = there ? seq_span(s, len).tiles : 0;
