@@ -76,6 +76,7 @@ hipError_t launch_decode_rope_append(const RopeAppendLaunch& p, int head_dim, hi
 hipError_t launch_kv4_load(const Kv4LoadLaunch& p, int head_dim, hipStream_t stream);
 hipError_t launch_kv4_decode(const Kv4DecodeLaunch& p, int head_dim, hipStream_t stream);
 hipError_t launch_kv4_chunk(const Kv4ChunkLaunch& p, int head_dim, hipStream_t stream);
+hipError_t launch_kv4_few_rows(const Kv4ChunkLaunch& p, int head_dim, hipStream_t stream);
 // Joins the parts of a batch's sequences (decode_attn.hip); short_too: with the shorter way
 // for few parts.
 hipError_t launch_decode_join(const DecodeAttnLaunch& p, int head_dim, bool short_too, hipStream_t stream);

@@ -32,6 +32,83 @@ StorePools pools_of(const mocap_kv4_store* kv) {
 
 mocap_status done(hipError_t e) { return e == hipSuccess ? MOCAP_OK : MOCAP_ERR_HIP; }
 
+// ---- A chunk's attention ----
+
+// A chunk of few rows, or with few keys, takes decoding's way (kv4_decode.hip): tiles from the
+// store to registers, a wavefront each, without barriers, in blocks of up to 32 rows that each
+// read them.  Its 32 rows of a tile cost 0.44 us of a compute unit where 256 rows cost 1.9 in
+// kv4_chunk.hip, but a few rows there cost 1.5 as well, and a workgroup takes 2 us less to
+// start.  Measured, blocks of 32 against workgroups of 256, in us (d 128 with 8 KV heads, groups
+// of 4): 16 rows a KV head behind 30000 15 and 29, behind 120000 34 and 95; 64 rows 25 and 31;
+// 128 rows 38 and 34; chunks without a prefix of 300 tokens 11 and 16, of 1000 29 and 31, of 2000
+// 73 and 52; 137 tokens of 16/2/64 in a window of 1000 11.4 and 15.5.  The rule is a time of either
+// way in us: turns of the fullest compute unit, a fixed part, the merge's traffic.  Of 142 shapes
+// the way it chose took at most 1.19 of the better one's time, 1.00 on average.
+constexpr double kMergeUs = 3.5, kBigUs = 6.0, kSmallUs16 = 4.0, kSmallUs32 = 6.0;
+// Rows that see all keys before them: long and short row groups together where every
+// workgroup starts at once (32/8/128 heads, 2048 tokens without a prefix 74 -> 60 us,
+// behind 2048 140 -> 124), neighbours, longest first, where they follow one another (8192
+// tokens 577 us, mirrored 645).
+bool mirrored_rows(const WindowLaunch& p, int cus) {
+  return p.window >= p.prefix_len + p.chunk_len && p.total_wgs <= cus;
+}
+struct ChunkWork {
+  int64_t tiles;       // of the block with the most
+  double mean;         // of all blocks
+};
+ChunkWork work_of(const WindowLaunch& p, int64_t block) {
+  const int64_t end = (int64_t)p.prefix_len + p.chunk_len;
+  const int64_t span = std::min<int64_t>(p.chunk_len, ceil_div(block, p.group) + 1) + p.window;
+  ChunkWork w;
+  w.tiles = std::min(ceil_div(end, kTileKeys), ceil_div(span, kTileKeys) + 1 + ceil_div(p.sinks, kTileKeys));
+  w.mean = std::min((double)w.tiles, (p.prefix_len + 0.5 * p.chunk_len) / kTileKeys + 1.0);
+  return w;
+}
+double merge_us(const WindowLaunch& p, int32_t head_dim, int64_t n) {
+  return n > 1 ? kMergeUs + 8.0 * n * p.chunk_len * p.h_q * (head_dim + 1) / kWindowMergeBytesPerUs : 0.0;
+}
+
+mocap_status plan_chunk(int64_t prefix_len, int32_t chunk_len, int32_t h_q, int32_t h_kv, int32_t head_dim,
+                        int64_t window, int64_t sinks, int32_t num_splits, WindowLaunch* p, bool* few) {
+  if (window == 0) window = kMaxPositions, sinks = 0;
+  *few = false;
+  mocap_status st = plan_window(prefix_len, chunk_len, h_q, h_kv, head_dim, window, sinks, num_splits, p);
+  if (st != MOCAP_OK) return st;
+  int cus = 0;
+  st = device_cu_count(&cus);
+  if (st != MOCAP_OK) return st;
+  const int64_t rows = (int64_t)chunk_len * p->group, block = rows <= 16 ? 16 : 32, blocks = ceil_div(rows, block);
+  const ChunkWork big = work_of(*p, kWindowRows), small = work_of(*p, block);
+  const bool d64 = head_dim == 64;
+  const double big_tile = rows <= kWindowRows / 2 ? (d64 ? 1.1 : 1.5) : (d64 ? 1.4 : 1.9);
+  // (A workgroup with mirrored row groups walks the later one's tiles, half of them for both.)
+  const double big_tiles = mirrored_rows(*p, cus)
+                               ? 0.5 * (big.tiles + big.mean)
+                               : std::max((double)big.tiles, ceil_div(p->total_wgs, cus) * big.mean);
+  const double big_us = big_tiles / p->n_ranges * big_tile + kBigUs + merge_us(*p, head_dim, p->n_ranges);
+  const double turn = block == 16 ? (d64 ? 1.1 : 1.4) : (d64 ? 1.25 : 1.75);  // of a workgroup's four wavefronts
+  const double fixed = block == 16 ? kSmallUs16 : kSmallUs32;
+  int64_t best = 0;
+  double best_us = big_us;
+  const int64_t most = std::min<int64_t>(128, small.tiles);
+  for (int64_t n = num_splits > 0 ? std::min<int64_t>(num_splits, small.tiles) : 1; n <= std::max<int64_t>(most, num_splits);
+       n += n < 32 ? 1 : 8) {
+    const double turns = std::max((double)ceil_div(small.tiles, 4 * n),
+                                  ceil_div(blocks * h_kv * n, cus) * (small.mean / (4 * n) + 0.5));
+    const double us = turns * turn + fixed + merge_us(*p, head_dim, n);
+    if (us < best_us) best_us = us, best = n;
+    if (num_splits > 0) break;
+  }
+  if (best == 0 || best * h_kv * blocks > kMaxGroups) return MOCAP_OK;
+  *few = true;
+  p->row_blocks = (int32_t)blocks;
+  p->n_ranges = (int32_t)best;
+  p->total_wgs = (int32_t)(blocks * h_kv * best);
+  return MOCAP_OK;
+}
+
+// ---- Rows ----
+
 // 2-byte values of `tokens` rows of `heads` heads.
 bool overlap_bf16(const void* a, int64_t a_stride, const void* b, int64_t b_stride, int64_t tokens, int64_t a_row,
                   int64_t b_row) {
@@ -253,8 +330,8 @@ mocap_status mocap_kv4_chunk_attn_workspace_size(int64_t prefix_len, int32_t chu
   if (st != MOCAP_OK) return st;
   WindowLaunch p;
   p.n_ranges = 1;
-  if (window == 0) window = kMaxPositions, sinks = 0;
-  if (chunk_len > 0) st = plan_window(prefix_len, chunk_len, h_q, h_kv, head_dim, window, sinks, num_splits, &p);
+  bool few;
+  if (chunk_len > 0) st = plan_chunk(prefix_len, chunk_len, h_q, h_kv, head_dim, window, sinks, num_splits, &p, &few);
   if (st != MOCAP_OK) return st;
   if (splits_out) *splits_out = p.n_ranges;
   *bytes_out = chunk_len > 0 ? window_workspace(p, head_dim) : 0;
@@ -272,14 +349,14 @@ mocap_status mocap_kv4_chunk_attn(const mocap_kv4_store* kv, const int32_t* bloc
   if (window < 0 || sinks < 0 || num_splits < 0) return MOCAP_ERR_INVALID_ARG;
   if (chunk_len == 0) return MOCAP_OK;
   if (scales_missing(kv) || !o || !lse || !aligned16(o) || !aligned4(lse)) return MOCAP_ERR_INVALID_ARG;
-  if (window == 0) window = kMaxPositions, sinks = 0;
   Kv4ChunkLaunch p;
-  st = plan_window(prefix_len, chunk_len, h_q, h_kv, head_dim, window, sinks, num_splits, &p.a);
+  bool few;
+  st = plan_chunk(prefix_len, chunk_len, h_q, h_kv, head_dim, window, sinks, num_splits, &p.a, &few);
   if (st != MOCAP_OK) return st;
   if (p.a.n_ranges > 1 && (!workspace || !aligned16(workspace) || workspace_bytes < window_workspace(p.a, head_dim)))
     return MOCAP_ERR_WORKSPACE;
-  MOCAP_DEBUG_CHECK(block_table, 0, std::min<int64_t>(sinks, prefix_len + chunk_len), &view);
-  MOCAP_DEBUG_CHECK(block_table, std::max<int64_t>(0, prefix_len - window + 1), prefix_len + chunk_len, &view);
+  MOCAP_DEBUG_CHECK(block_table, 0, std::min<int64_t>(p.a.sinks, prefix_len + chunk_len), &view);
+  MOCAP_DEBUG_CHECK(block_table, std::max<int64_t>(0, prefix_len - p.a.window + 1), prefix_len + chunk_len, &view);
   p.a.q = static_cast<const uint16_t*>(q);
   p.a.k_pool = static_cast<const uint16_t*>(kv->k_pool);
   p.a.v_pool = static_cast<const uint16_t*>(kv->v_pool);
@@ -288,11 +365,7 @@ mocap_status mocap_kv4_chunk_attn(const mocap_kv4_store* kv, const int32_t* bloc
   int cus = 0;
   st = device_cu_count(&cus);
   if (st != MOCAP_OK) return st;
-  // Rows that see all keys before them: long and short row groups together where every
-  // workgroup starts at once (32/8/128 heads, 2048 tokens without a prefix 74 -> 60 us,
-  // behind 2048 140 -> 124), neighbours, longest first, where they follow one another (8192
-  // tokens 577 us, mirrored 645).
-  p.mirrored = window >= prefix_len + chunk_len && p.a.total_wgs <= cus;
+  p.mirrored = mirrored_rows(p.a, cus);
   p.a.table = block_table;
   p.a.o = static_cast<uint16_t*>(o);
   p.a.lse = lse;
@@ -307,7 +380,7 @@ mocap_status mocap_kv4_chunk_attn(const mocap_kv4_store* kv, const int32_t* bloc
         static_cast<char*>(workspace) + round_up((size_t)p.a.n_ranges * h_q * chunk_len * head_dim * sizeof(float), 256));
   }
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (launch_kv4_chunk(p, head_dim, s) != hipSuccess) return MOCAP_ERR_HIP;
+  if ((few ? launch_kv4_few_rows : launch_kv4_chunk)(p, head_dim, s) != hipSuccess) return MOCAP_ERR_HIP;
   if (p.a.n_ranges > 1) {
     const MergeLaunch m{p.a.ws_o, p.a.ws_lse, p.a.o, lse, chunk_len, h_q, p.a.n_ranges};
     if (launch_lse_merge(m, head_dim, s) != hipSuccess) return MOCAP_ERR_HIP;

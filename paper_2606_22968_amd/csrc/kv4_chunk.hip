@@ -38,30 +38,6 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_s_barrier();
 }
 
-__device__ __forceinline__ uint32_t div_by(uint32_t n, uint32_t magic, int shift) {
-  return (__umulhi(n, magic) + n) >> shift;
-}
-
-// Bytes of a word of scales that are kScaleNan, or more than any stored position's (253 and
-// 254 make infinities): bits 7, 15, 23 and 31.
-__device__ __forceinline__ uint32_t beyond_252(uint32_t x) { return ((x & 0x7F7F7F7Fu) + 0x03030303u) & x & 0x80808080u; }
-
-// The tiles of a run of rows at positions [first, last]: the sinks' [0, sinks),
-// then [begin, end).
-struct Tiles {
-  int sinks, begin, end;
-  __device__ __forceinline__ int count() const { return sinks + end - begin; }
-  __device__ __forceinline__ int at(int i) const { return i < sinks ? i : i - sinks + begin; }
-};
-__device__ __forceinline__ Tiles tiles_of(const WindowLaunch& p, int first, int last) {
-  const int low = max(0, first - p.window + 1);
-  Tiles t;
-  t.begin = low / kTileKeys;
-  t.end = last / kTileKeys + 1;
-  t.sinks = min((min(p.sinks, low) + kTileKeys - 1) / kTileKeys, t.begin);
-  return t;
-}
-
 template <int D>
 __global__ __launch_bounds__(kAttnThreads, 2) void kv4_chunk_kernel(const Kv4ChunkLaunch launch) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -115,11 +91,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void kv4_chunk_kernel(const Kv4Chu
   const Tiles tiles = tiles_of(p, wg_first, wg_last), own = tiles_of(p, first, last);
   const int i0 = (int)((int64_t)tiles.count() * range / p.n_ranges);
   const int i1 = (int)((int64_t)tiles.count() * (range + 1) / p.n_ranges);
-  // A tile that all rows of [a, b] see in full; one that some row of this wavefront sees.
-  auto full_for = [&](int t, int a, int b) __attribute__((always_inline)) -> bool {
-    const int k0 = t * kTileKeys, k1 = k0 + kTileKeys;
-    return k1 <= a + 1 && (k0 > b - p.window || k1 <= p.sinks);
-  };
+  // A tile that some row of this wavefront sees.
   auto seen = [&](int t) __attribute__((always_inline)) -> bool {
     return wave_on && (t < own.sinks || (t >= own.begin && t < own.end));
   };
@@ -175,14 +147,18 @@ __global__ __launch_bounds__(kAttnThreads, 2) void kv4_chunk_kernel(const Kv4Chu
   // Where all rows see a whole tile, a NaN value block reaches all of them as NaN; in other
   // tiles it is noted and its scale set next to 0, as are scales of unwritten positions.
   auto set_apart = [&](int i) __attribute__((always_inline)) {
-    if (!takes_v || full_for(tiles.at(i), wg_first, wg_last)) return;
+    if (!takes_v || seen_in_full(p, tiles.at(i), wg_first, wg_last)) return;
     uint32_t bad = 0;
 #pragma unroll
     for (int w = 0; w < WORDS; ++w) bad |= beyond_252(raw.scales[w]);
     if (bad == 0) return;
-    found[i % 4] = 1;
+    const int behind = wg_last + 1 - tiles.at(i) * kTileKeys - v_part * (D / 8);  // the first byte that no row sees
 #pragma unroll
-    for (int w = 0; w < WORDS; ++w) raw.scales[w] &= ~((beyond_252(raw.scales[w]) >> 7) * 0xFFu);
+    for (int w = 0; w < WORDS; ++w) {
+      const uint32_t b = beyond_252(raw.scales[w]);
+      if (b != 0 && w * 4 + __builtin_ctz(b) / 8 < behind) found[i % 4] = 1;
+      raw.scales[w] &= ~((b >> 7) * 0xFFu);
+    }
   };
   // Turns the fetched codes into bf16 in the stages of tile i, in STEPS steps.
   u32x4 out[2];
@@ -232,13 +208,11 @@ __global__ __launch_bounds__(kAttnThreads, 2) void kv4_chunk_kernel(const Kv4Chu
   // Tile i holds NaN value blocks: the 32-dim blocks in which this lane's row sees one, as bits.
   uint32_t nan_dims = 0;
   auto note_nan = [&](int i) __attribute__((always_inline)) {
-    const uint8_t* s = launch.v_scale + tile_number(i) * (MD * kTileKeys);
     const int k0 = tiles.at(i) * kTileKeys;
-#pragma unroll 1
-    for (int x = 0; x < MD * kTileKeys; ++x) {
-      const int at = k0 + x % kTileKeys;
-      if (s[x] == kScaleNan && at <= pos && (at > pos - p.window || at < p.sinks)) nan_dims |= 1u << x / kTileKeys;
-    }
+    each_nan<MD>(launch.v_scale + tile_number(i) * (MD * kTileKeys), [&](int b, int slot) {
+      const int at = k0 + slot;
+      if (at <= pos && (at > pos - p.window || at < p.sinks)) nan_dims |= 1u << b;
+    });
   };
 
   // Visible keys of this lane's 16 of a 32-key half: keys base + {0..7, 16..23}, as bits.
@@ -291,7 +265,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void kv4_chunk_kernel(const Kv4Chu
   };
   auto mask = [&](int i) __attribute__((always_inline)) {
     const int t = tiles.at(i);
-    if (!full_for(t, first, last)) {
+    if (!seen_in_full(p, t, first, last)) {
 #pragma unroll
       for (int sb = 0; sb < 2; ++sb) {
         const uint32_t vm = visible_bits(t * kTileKeys + sb * 32 + half * 8);

@@ -1,5 +1,6 @@
 // Decoding over the 4-bit store for gfx950 (CDNA4): the attention of one token per
-// sequence, decode_attn.hip's over keys and values of 4.25 bits.
+// sequence, decode_attn.hip's over keys and values of 4.25 bits; and of a chunk's few rows, which
+// are then as many heads of one token, each with its own last key.
 //
 // A key or value of d dims is d / 2 + d / 32 bytes and 4 d G FLOP for the G query
 // heads of a group: HBM bounds it still, at 3.8 times the keys a second.
@@ -25,17 +26,21 @@
 #include "kv4_device.h"
 #include "serve_device.h"
 
+#include <type_traits>
+
 namespace mocap {
 namespace {
 
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 
-// NT: 16-head blocks of the group that a workgroup takes.
-template <int D, int NT>
-__global__ __launch_bounds__(kThreads) void kv4_decode_kernel(const Kv4DecodeLaunch launch) {
+// NT: 16-row blocks that a workgroup takes.  Rows are the heads of a sequence's group, or
+// (CHUNK) those of all tokens of a chunk, row r token r / G.
+template <int D, int NT, bool CHUNK>
+__global__ __launch_bounds__(kThreads) void kv4_rows_kernel(
+    const typename std::conditional<CHUNK, Kv4ChunkLaunch, Kv4DecodeLaunch>::type launch) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  const DecodeAttnLaunch& p = launch.a;
+  const auto& p = launch.a;
   constexpr int KS = D / 32;   // k-steps of a score product
   constexpr int B = D / 32;    // blocks of 32 dims
   constexpr int MD = D / 16;   // 16-dim blocks of O
@@ -48,32 +53,82 @@ __global__ __launch_bounds__(kThreads) void kv4_decode_kernel(const Kv4DecodeLau
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g4 = lane >> 4;
 
-  // Logical order: item, KV head; the blocks of query heads that read the same
-  // keys are 8 workgroups apart, on one XCD.
-  const int stripe = blockIdx.x / (8 * p.row_blocks), in_stripe = blockIdx.x - stripe * 8 * p.row_blocks;
-  const int work = stripe * 8 + (in_stripe & 7);
+  // Logical order: item (a sequence's part, or a range of the chunk's tiles), KV head.  The blocks
+  // of rows that read the same keys are 8 workgroups apart, on one XCD, or (a chunk) as many as
+  // there are items and heads, the last rows first: on 8 / gcd(8, that) XCDs, each with late
+  // and early rows (a contiguous share of all for each XCD: 80 us for 2882 tokens of 12/4/128
+  // without a prefix).
+  int work, row0;  // (row0: of the KV head)
+  if constexpr (CHUNK) {
+    const int works = p.n_ranges * p.h_kv, block = blockIdx.x / works;
+    work = blockIdx.x - block * works;
+    row0 = (p.row_blocks - 1 - block) * (NT * 16);
+  } else {
+    const int stripe = blockIdx.x / (8 * p.row_blocks), in_stripe = blockIdx.x - stripe * 8 * p.row_blocks;
+    work = stripe * 8 + (in_stripe & 7);
+    row0 = (in_stripe >> 3) * (NT * 16);
+  }
   const int item = work / p.h_kv;
   const int kv_head = work - item * p.h_kv;
-  const int head0 = (in_stripe >> 3) * (NT * 16);  // of the group
-  if (item >= p.seqs.items) return;
-  const SeqPart w = locate_item(p.seqs, lane, item);
-  if (w.seq == p.seqs.batch) return;
-  int begin, end;
-  part_range_longer_first(w, &begin, &end);
+  SeqPart w;         // of a batch
+  Tiles chunk;       // of a chunk's rows, at positions first to last
+  int begin, end, rows, first = 0, last = 0;
+  const_i32_ptr table;
+  int bs, block_shift;
+  uint32_t block_magic;
+  // Row r's token of the chunk; its row of Q and O.
+  auto token_of = [&](int row) __attribute__((always_inline)) {
+    if constexpr (CHUNK) return (int)div_by((uint32_t)min(row, rows - 1), p.group_magic, p.group_shift);
+    return 0;
+  };
+  auto out_row = [&](int row) __attribute__((always_inline)) -> int64_t {
+    if constexpr (CHUNK) {
+      const int token = token_of(row);
+      return (int64_t)token * p.h_q + kv_head * p.group + row - token * p.group;
+    } else {
+      return (int64_t)w.seq * p.h_q + kv_head * p.group + row;
+    }
+  };
+  if constexpr (CHUNK) {
+    rows = p.chunk_len * p.group;
+    first = p.prefix_len + token_of(row0);
+    last = p.prefix_len + token_of(row0 + NT * 16 - 1);
+    chunk = tiles_of(p, first, last);
+    begin = (int)((int64_t)chunk.count() * item / p.n_ranges);
+    end = (int)((int64_t)chunk.count() * (item + 1) / p.n_ranges);
+    table = (const_i32_ptr)p.table;
+    bs = p.block_size, block_magic = p.block_magic, block_shift = p.block_shift;
+  } else {
+    if (item >= p.seqs.items) return;
+    w = locate_item(p.seqs, lane, item);
+    if (w.seq == p.seqs.batch) return;
+    part_range_longer_first(w, &begin, &end);
+    rows = p.group;
+    table = (const_i32_ptr)(p.seqs.tables + w.seq * p.seqs.table_stride);
+    bs = p.seqs.block_size, block_magic = p.seqs.block_magic, block_shift = p.seqs.block_shift;
+  }
+  // Tile i of the part or range.
+  auto tile_of = [&](int i) __attribute__((always_inline)) {
+    if constexpr (CHUNK) {
+      return chunk.at(begin + i);
+    } else {
+      return w.span.tile(begin + i);
+    }
+  };
 
-  // Q as the B operand: lane l holds head l % 16, dims D / 4 (l / 16) + 8 ks .. + 7.
-  // Lanes past the group's last head take that head; nothing of theirs is stored.
+  // Q as the B operand: lane l holds row l % 16, dims D / 4 (l / 16) + 8 ks .. + 7.
+  // Lanes past the last row take that row; nothing of theirs is stored.
   bf16x8 qf[NT][KS];
+  int pos[NT];  // the row's position (CHUNK)
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    const int g = min(head0 + t * 16 + l16, p.group - 1);
-    const uint16_t* row = p.q + ((int64_t)w.seq * p.h_q + kv_head * p.group + g) * D + g4 * (D / 4);
+    const int at = min(row0 + t * 16 + l16, rows - 1);
+    if constexpr (CHUNK) pos[t] = p.prefix_len + token_of(at);
+    const uint16_t* row = p.q + out_row(at) * D + g4 * (D / 4);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qf[t][ks] = *reinterpret_cast<const bf16x8*>(row + ks * 8);
   }
 
-  const const_i32_ptr table = (const_i32_ptr)(p.seqs.tables + w.seq * p.seqs.table_stride);
-  const int bs = p.seqs.block_size;
   const int block_tiles = bs / kTileKeys;
   const uint8_t* const k_pool = reinterpret_cast<const uint8_t*>(p.k_pool);
   const uint8_t* const v_pool = reinterpret_cast<const uint8_t*>(p.v_pool);
@@ -91,9 +146,9 @@ __global__ __launch_bounds__(kThreads) void kv4_decode_kernel(const Kv4DecodeLau
   } raw;
   // The number of tile i of the part in [blocks][Hkv][bs / 64].
   auto tile_at = [&](int i) __attribute__((always_inline)) {
-    const int pos = w.span.tile(begin + i) * kTileKeys;
-    const int lb = (int)((__umulhi((uint32_t)pos, p.seqs.block_magic) + (uint32_t)pos) >> p.seqs.block_shift);
-    return ((int64_t)table[lb] * p.h_kv + kv_head) * block_tiles + (pos - lb * bs) / kTileKeys;
+    const int key0 = tile_of(i) * kTileKeys;
+    const int lb = (int)div_by((uint32_t)key0, block_magic, block_shift);
+    return ((int64_t)table[lb] * p.h_kv + kv_head) * block_tiles + (key0 - lb * bs) / kTileKeys;
   };
   auto fetch_k = [&](int64_t tile) __attribute__((always_inline)) {
     const uint8_t* src = k_pool + tile * (kTileKeys * D / 2) + k_lane;
@@ -110,8 +165,6 @@ __global__ __launch_bounds__(kThreads) void kv4_decode_kernel(const Kv4DecodeLau
       raw.v_scale[b] = *reinterpret_cast<const u32x4*>(scales + b * kTileKeys);
     }
   };
-  auto visible = [&](int key) { return key < w.span.len && (key < w.span.sink_end || key >= w.span.low); };
-
   f32x4 oacc[NT][MD];
   float m_run[NT], l_run[NT];
 #pragma unroll
@@ -122,6 +175,48 @@ __global__ __launch_bounds__(kThreads) void kv4_decode_kernel(const Kv4DecodeLau
     for (int md = 0; md < MD; ++md) oacc[t][md] = f32x4{};
   }
   const float sl2 = p.scale_log2;
+
+  // CHUNK: hides keys that a row does not see.  A tile's NaN value blocks would reach all rows
+  // of the product: their scales are set next to 0, and rows that see one are noted.
+  uint32_t nan_dims[NT] = {};
+  auto mask_chunk = [&](int i, int key0, f32x4 (&s)[NT][4]) __attribute__((always_inline)) {
+    if constexpr (CHUNK) {
+      const int base = key0 + g4 * 16;
+      auto below = [&](int x) { return (1u << min(max(x - base, 0), 16)) - 1u; };  // keys below x, as bits
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const uint32_t seen = below(pos[t] + 1) & (~below(max(pos[t] - p.window + 1, 0)) | below(p.sinks));
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float x = s[t][e >> 2][e & 3];
+          if constexpr (NT == 1) {
+            const int keep = __builtin_amdgcn_sbfe((int)seen, e, 1);
+            s[t][e >> 2][e & 3] = __int_as_float((__float_as_int(x) & keep) | (~keep & (int)0xFF800000u));
+          } else {  // (fewer vector registers: two wavefronts a SIMD at head_dim 128, three at 64)
+            s[t][e >> 2][e & 3] = seen >> e & 1 ? x : -INFINITY;
+          }
+        }
+      }
+      uint32_t bad = 0;
+#pragma unroll
+      for (int b = 0; b < B; ++b)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const uint32_t y = beyond_252(raw.v_scale[b][x]);
+          if (y != 0 && base + x * 4 + __builtin_ctz(y) / 8 <= last) bad = 1;
+          raw.v_scale[b][x] &= ~((y >> 7) * 0xFFu);
+        }
+      if (__builtin_amdgcn_ballot_w64(bad != 0) != 0) {
+        const uint8_t* scales = launch.v_scale + tile_at(i) * (B * kTileKeys);
+        each_nan<B>(scales, [&](int b, int slot) {
+          const int at = key0 + slot;
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+            if (at <= pos[t] && (at > pos[t] - p.window || at < p.sinks)) nan_dims[t] |= 1u << b;
+        });
+      }
+    }
+  };
 
   // A wavefront's tiles: wave, wave + 4, ...  The next tile's K is requested as
   // soon as this one's is used up, its V likewise.
@@ -151,11 +246,14 @@ __global__ __launch_bounds__(kThreads) void kv4_decode_kernel(const Kv4DecodeLau
     }
     if (more) fetch_k(next);
     // Score e of a lane (product e / 4) belongs to key key0 + 16 g4 + e.
-    const int key0 = w.span.tile(begin + i) * kTileKeys;
-    if (key0 + kTileKeys > w.span.len || (key0 < w.span.low && key0 + kTileKeys > w.span.sink_end)) {
+    const int key0 = tile_of(i) * kTileKeys;
+    if constexpr (CHUNK) {
+      if (!seen_in_full(p, key0 / kTileKeys, first, last)) mask_chunk(i, key0, s);
+    } else if (key0 + kTileKeys > w.span.len || (key0 < w.span.low && key0 + kTileKeys > w.span.sink_end)) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const bool gone = !visible(key0 + g4 * 16 + e);
+        const int key = key0 + g4 * 16 + e;
+        const bool gone = key >= w.span.len || (key >= w.span.sink_end && key < w.span.low);
 #pragma unroll
         for (int t = 0; t < NT; ++t) s[t][e >> 2][e & 3] = gone ? -INFINITY : s[t][e >> 2][e & 3];
         // A hidden position's scale may be NaN; its probability is 0.
@@ -233,12 +331,14 @@ __global__ __launch_bounds__(kThreads) void kv4_decode_kernel(const Kv4DecodeLau
       part_l[wave][t * 16 + l16] = l;
     }
 #pragma unroll
-    for (int md = 0; md < MD; ++md)
+    for (int md = 0; md < MD; ++md) {
+      if (CHUNK && nan_dims[t] >> md / 2 & 1) oacc[t][md] = f32x4{NAN, NAN, NAN, NAN};
       *reinterpret_cast<f32x4*>(&part_o[wave][t * 16 + l16][md * 16 + g4 * 4]) = oacc[t][md];
+    }
   }
   __syncthreads();
   constexpr int QUADS = D / 4;
-  for (int i = tid; i < min(NT * 16, p.group - head0) * QUADS; i += kThreads) {
+  for (int i = tid; i < min(NT * 16, rows - row0) * QUADS; i += kThreads) {
     const int row = i / QUADS, quad = i % QUADS;
     float m = -INFINITY;
 #pragma unroll
@@ -257,19 +357,33 @@ __global__ __launch_bounds__(kThreads) void kv4_decode_kernel(const Kv4DecodeLau
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const float row_lse = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
-    const int head = kv_head * p.group + head0 + row;
     acc *= inv;
-    if (w.parts == 1) {
-      const int64_t at = (int64_t)w.seq * p.h_q + head;
+    const int64_t at = out_row(row0 + row);
+    bool alone;
+    int64_t part_at;
+    if constexpr (CHUNK) {
+      alone = p.n_ranges == 1;
+      part_at = (int64_t)item * p.chunk_len * p.h_q + at;
+    } else {
+      alone = w.parts == 1;
+      part_at = (int64_t)(item - w.seq) * p.h_q + at;
+    }
+    if (alone) {
       bf16x4 v;
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] = (__bf16)acc[e];
       *reinterpret_cast<bf16x4*>(p.o + at * D + quad * 4) = v;
-      if (quad == 0) p.lse[at] = row_lse;
+      if (quad == 0) {
+        if constexpr (CHUNK) {
+          const int token = token_of(row0 + row);
+          p.lse[(at - (int64_t)token * p.h_q) * p.chunk_len + token] = row_lse;
+        } else {
+          p.lse[at] = row_lse;
+        }
+      }
     } else {
-      const int64_t at = (int64_t)item * p.h_q + head;
-      *reinterpret_cast<f32x4*>(p.ws_o + at * D + quad * 4) = acc;
-      if (quad == 0) p.ws_lse[at] = row_lse;
+      *reinterpret_cast<f32x4*>(p.ws_o + part_at * D + quad * 4) = acc;
+      if (quad == 0) p.ws_lse[part_at] = row_lse;
     }
   }
 #endif  // __HIP_DEVICE_COMPILE__
@@ -280,9 +394,19 @@ void launch(const Kv4DecodeLaunch& p, hipStream_t stream) {
   const int64_t work = ((int64_t)p.a.seqs.items * p.a.h_kv + 7) / 8 * 8;
   const dim3 grid((unsigned)(work * p.a.row_blocks)), block(kThreads);
   if (p.a.group <= 16 * p.a.row_blocks) {
-    hipLaunchKernelGGL((kv4_decode_kernel<D, 1>), grid, block, 0, stream, p);
+    hipLaunchKernelGGL((kv4_rows_kernel<D, 1, false>), grid, block, 0, stream, p);
   } else {
-    hipLaunchKernelGGL((kv4_decode_kernel<D, 2>), grid, block, 0, stream, p);
+    hipLaunchKernelGGL((kv4_rows_kernel<D, 2, false>), grid, block, 0, stream, p);
+  }
+}
+
+template <int D>
+void launch(const Kv4ChunkLaunch& p, hipStream_t stream) {
+  const dim3 grid(p.a.total_wgs), block(kThreads);
+  if (p.a.chunk_len * p.a.group <= 16) {
+    hipLaunchKernelGGL((kv4_rows_kernel<D, 1, true>), grid, block, 0, stream, p);
+  } else {
+    hipLaunchKernelGGL((kv4_rows_kernel<D, 2, true>), grid, block, 0, stream, p);
   }
 }
 
@@ -296,6 +420,15 @@ hipError_t launch_kv4_decode(const Kv4DecodeLaunch& p, int head_dim, hipStream_t
   }
   const hipError_t e = hipGetLastError();
   return e != hipSuccess || !p.a.may_split ? e : launch_decode_join(p.a, head_dim, true, stream);
+}
+
+hipError_t launch_kv4_few_rows(const Kv4ChunkLaunch& p, int head_dim, hipStream_t stream) {
+  if (head_dim == 128) {
+    launch<128>(p, stream);
+  } else {
+    launch<64>(p, stream);
+  }
+  return hipGetLastError();
 }
 
 }  // namespace mocap

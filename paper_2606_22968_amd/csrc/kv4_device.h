@@ -62,5 +62,42 @@ __device__ __forceinline__ uint32_t largest_bits(const float* x) {
   return m;
 }
 
+// Bytes of a word of scales that are kScaleNan, or more than any stored position's (253 and
+// 254 make infinities): bits 7, 15, 23 and 31.
+__device__ __forceinline__ uint32_t beyond_252(uint32_t x) { return ((x & 0x7F7F7F7Fu) + 0x03030303u) & x & 0x80808080u; }
+
+// Calls found(block, slot) for the NaN blocks among a tile's value scales [B][64].
+template <int B, typename Found>
+__device__ __forceinline__ void each_nan(const uint8_t* scales, Found found) {
+#pragma unroll 1
+  for (int i = 0; i < B * 64; ++i)
+    if (scales[i] == kScaleNan) found(i / 64, i % 64);
+}
+
+__device__ __forceinline__ uint32_t div_by(uint32_t n, uint32_t magic, int shift) {
+  return (__umulhi(n, magic) + n) >> shift;
+}
+
+// The tiles of a run of a chunk's rows at positions [first, last]: the sinks' [0, sinks),
+// then [begin, end).
+struct Tiles {
+  int sinks, begin, end;
+  __device__ __forceinline__ int count() const { return sinks + end - begin; }
+  __device__ __forceinline__ int at(int i) const { return i < sinks ? i : i - sinks + begin; }
+};
+__device__ __forceinline__ Tiles tiles_of(const WindowLaunch& p, int first, int last) {
+  const int low = max(0, first - p.window + 1);
+  Tiles t;
+  t.begin = low / kTileKeys;
+  t.end = last / kTileKeys + 1;
+  t.sinks = min((min(p.sinks, low) + kTileKeys - 1) / kTileKeys, t.begin);
+  return t;
+}
+// Whether all of these rows see a whole tile.
+__device__ __forceinline__ bool seen_in_full(const WindowLaunch& p, int tile, int first, int last) {
+  const int k0 = tile * kTileKeys, k1 = k0 + kTileKeys;
+  return k1 <= first + 1 && (k0 > last - p.window || k1 <= p.sinks);
+}
+
 }  // namespace
 }  // namespace mocap

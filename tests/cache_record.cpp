@@ -9,6 +9,7 @@
 namespace {
 mocap::RopeAppendLaunch append;
 mocap::Kv4ChunkLaunch chunk;
+bool few = false;
 mocap::SeqBatch seqs;
 int launches = 0;
 }  // namespace
@@ -29,6 +30,12 @@ hipError_t launch_kv4_decode(const Kv4DecodeLaunch& p, int, hipStream_t) {
 }
 hipError_t launch_kv4_chunk(const Kv4ChunkLaunch& p, int, hipStream_t) {
   chunk = p;
+  few = false;
+  return ++launches, hipSuccess;
+}
+hipError_t launch_kv4_few_rows(const Kv4ChunkLaunch& p, int, hipStream_t) {
+  chunk = p;
+  few = true;
   return ++launches, hipSuccess;
 }
 hipError_t launch_lse_merge(const MergeLaunch&, int, hipStream_t) { return ++launches, hipSuccess; }
@@ -57,8 +64,9 @@ void record_append(long long* out) {
   for (int i = 0; i < 11; ++i) out[i] = v[i];
 }
 void record_chunk(int* out) {
-  const int v[] = {chunk.a.row_blocks, chunk.a.n_ranges, chunk.a.total_wgs, chunk.a.window, chunk.a.sinks, chunk.mirrored};
-  for (int i = 0; i < 6; ++i) out[i] = v[i];
+  const int v[] = {chunk.a.row_blocks, chunk.a.n_ranges, chunk.a.total_wgs, chunk.a.window, chunk.a.sinks, chunk.mirrored,
+                   few};
+  for (int i = 0; i < 7; ++i) out[i] = v[i];
 }
 void record_batch(int* out) {
   const int v[] = {seqs.target, seqs.fill,  seqs.min_tiles, seqs.least_tiles,

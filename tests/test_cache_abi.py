@@ -239,21 +239,67 @@ def test_empty_calls_launch_nothing(host):
     assert host.record_launches() == before
 
 
+def plan_of(host, **kwargs):
+    out = (ctypes.c_int * 7)()
+    assert chunk(host, **kwargs) == 0
+    host.record_chunk(out)
+    return dict(zip(("row_blocks", "n_ranges", "total_wgs", "window", "sinks", "mirrored", "few"), out))
+
+
 def test_chunk_plans(host):
-    """Windows that hide nothing are none; rows are mirrored where one workgroup per compute unit holds them."""
-    out = (ctypes.c_int * 6)()
+    """Windows that hide nothing are none; rows are mirrored where one workgroup per compute unit holds them; few rows,
+    or many with few keys, go in blocks of 16 or 32."""
     kv = store4(block_size=1024)
-    for P, L, window, splits, mirrored in ((0, 2048, 0, 1, True), (30720, 2048, 0, 1, True), (0, 2049, 0, 1, False),
-                                           (0, 8192, 0, 1, False), (0, 2048, 2047, 1, False), (0, 2048, 2048, 1, True),
-                                           (100, 10, 0, 1, True), (20000, 100, 0, 16, True), (20000, 100, 0, 17, False),
-                                           (20000, 100, 5000, 3, False)):
-        assert chunk(host, kv=kv, n_table=64, P=P, L=L, window=window, sinks=4, splits=splits) == 0
-        host.record_chunk(out)
-        assert out[0] == -(-L * 4 // 256) and out[2] == out[0] * 8 * out[1] and bool(out[5]) == mirrored
+    for P, L, window, splits, mirrored, few in (
+            (0, 2048, 0, 1, True, False), (30720, 2048, 0, 1, True, False), (0, 2049, 0, 1, False, False),
+            (0, 8192, 0, 1, False, False), (0, 2048, 2047, 1, False, False), (0, 2048, 2048, 1, True, False),
+            (20000, 500, 0, 4, True, False), (20000, 500, 0, 5, False, False), (20000, 500, 5000, 3, False, False),
+            (100, 10, 0, 1, None, True), (20000, 1, 0, 0, None, True), (20000, 4, 0, 0, None, True),
+            (20000, 5, 5000, 0, None, True), (20000, 16, 0, 9, None, True), (0, 300, 0, 0, None, True)):
+        p = plan_of(host, kv=kv, n_table=64, P=P, L=L, window=window, sinks=4, splits=splits)
+        rows = 256 if not few else 16 if L <= 4 else 32
+        assert bool(p["few"]) == few and p["row_blocks"] == -(-L * 4 // rows)
+        assert p["total_wgs"] == p["row_blocks"] * 8 * p["n_ranges"]
+        assert splits == 0 or p["n_ranges"] == splits
+        assert few or bool(p["mirrored"]) == mirrored
         if window == 0:
-            assert out[3] >= P + L and out[4] == 0
+            assert p["window"] >= P + L and p["sinks"] == 0
         else:
-            assert (out[3], out[4]) == (window, 4)
+            assert (p["window"], p["sinks"]) == (window, 4)
+
+
+def test_chunk_workspaces_hold_what_is_planned(host):
+    """A call takes the workspace that the size function names, and no less, for either way and any count of ranges."""
+    size, n = ctypes.c_size_t(), ctypes.c_int32()
+    for h_q, h_kv, d in ((32, 8, 128), (16, 2, 64), (64, 1, 64), (128, 16, 128)):
+        kv = store4(block_size=1024, h_kv=h_kv, head_dim=d)
+        for P in (0, 700, 5000, 40000):
+            for L in (1, 3, 17, 130, 700):
+                for window, splits in ((0, 0), (300, 0), (0, 2), (0, 7), (1000, 100)):
+                    assert host.mocap_kv4_chunk_attn_workspace_size(P, L, h_q, h_kv, d, window, 1, splits, ctypes.byref(n),
+                                                                    ctypes.byref(size)) == 0
+                    args = dict(kv=kv, n_table=64, P=P, L=L, h_q=h_q, h_kv=h_kv, d=d, window=window, sinks=1, splits=splits)
+                    p = plan_of(host, ws_bytes=size.value, **args)
+                    assert p["n_ranges"] == n.value <= max(1, -(-(P + L) // 64))
+                    assert (size.value == 0) == (n.value == 1)
+                    assert size.value >= (0 if n.value == 1 else n.value * L * h_q * (d + 1) * 4)
+                    if size.value:
+                        assert chunk(host, ws_bytes=size.value - 1, **args) == WORKSPACE
+
+
+def test_the_gpu_tests_run_both_ways(host):
+    from test_kv4_attn_gpu import MANY
+    for d in (64, 128):
+        kv = store4(block_size=192, h_kv=16, head_dim=d)
+        edges = [(200, 250, w, s, 0) for w in (1, 2, 33, 64, 65, 129, 192) for s in (0, 1, 64, 65)]
+        nan = [(100, 300, w, 3 if w else 0, s) for w in (0, 100) for s in (1, 3)] + [(0, 300, 0, 0, 1), (0, 300, 0, 0, 2)]
+        for P, L, window, sinks, splits in MANY + (edges if d == 64 else []) + nan:
+            p = plan_of(host, kv=kv, n_table=64, P=P, L=L, h_q=128, h_kv=16, d=d, window=window, sinks=sinks, splits=splits)
+            assert not p["few"], (d, P, L, window, sinks, splits)
+        for P, L, window, sinks in ((500, 1, 0, 0), (511, 2, 65, 64), (700, 137, 100, 4), (0, 300, 0, 0), (250, 150, 100, 3)):
+            kv2 = store4(block_size=64, num_blocks=4096, h_kv=2, head_dim=d)
+            p = plan_of(host, kv=kv2, n_table=64, P=P, L=L, h_q=8, h_kv=2, d=d, window=window, sinks=sinks)
+            assert p["few"], (d, P, L, window, sinks)
 
 
 def test_debug_build_checks_tables(mocap_lib, tmp_path):

@@ -154,6 +154,27 @@ def test_chunks(gpu, h_q, h_kv, d, prefix, rows, window, sinks):
     run_chunk(100, h_q, h_kv, d, 64, prefix, rows, window, sinks)
 
 
+# Chunks of so many rows that a workgroup takes 256 of them (test_cache_abi.py holds that they do; the others here are
+# in blocks of up to 32 rows): prefix, rows, window, sinks, splits of 128/16 heads.
+MANY = [(0, 300, 0, 0, 0), (0, 300, 1, 1, 0), (0, 300, 1 << 40, 7, 0), (250, 300, 0, 0, 1), (250, 300, 100, 3, 0),
+        (250, 299, 65, 64, 2), (511, 131, 63, 65, 3), (700, 137, 0, 0, 3), (963, 290, 1000, 1 << 40, 5), (64, 257, 64, 0, 0),
+        (1500, 301, 700, 70, 4)]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("prefix,rows,window,sinks,splits", MANY)
+def test_many_rows(gpu, d, prefix, rows, window, sinks, splits):
+    say(f"[case] kv4 chunk of many rows d={d} P={prefix} L={rows} W={window} sinks={sinks} splits={splits}")
+    run_chunk(104, 128, 16, d, 192, prefix, rows, window, sinks, splits)
+
+
+@pytest.mark.parametrize("window", [1, 2, 33, 64, 65, 129, 192])
+@pytest.mark.parametrize("sinks", [0, 1, 64, 65])
+def test_window_and_sink_edges_of_many_rows(gpu, window, sinks):
+    say(f"[case] kv4 chunk edges of many rows W={window} sinks={sinks}")
+    run_chunk(105, 128, 16, 64, 192, 200, 250, window, sinks)
+
+
 @pytest.mark.parametrize("window", [1, 2, 31, 32, 33, 63, 64, 65, 127, 128, 129, 191, 192, 193])
 @pytest.mark.parametrize("sinks", [0, 1, 63, 64, 65])
 def test_window_and_sink_edges(gpu, window, sinks):
@@ -242,6 +263,36 @@ def test_nan_blocks(gpu, d, window, sinks):
             assert ((got.double() - ref.o[0, g]).abs() <= bound[0, g])[~want].all()
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (100, 3)])
+def test_nan_blocks_of_many_rows(gpu, d, window, sinks):
+    """As test_nan_blocks, where a workgroup takes 256 rows."""
+    n, prefix, rows, h_q, h_kv = 400, 100, 300, 128, 16
+    group = h_q // h_kv
+    _, store, tables, ks, vs = make_store4(122, [n], 64, h_kv, d)
+    pos = prefix + torch.arange(rows)
+    want, whole = torch.zeros((rows, h_q, d), dtype=torch.bool), torch.zeros((rows, h_q), dtype=torch.bool)
+
+    def sees(t):
+        return (t <= pos) & ((t > pos - window) if window else True) | (t <= pos) & (t < sinks)
+
+    for h, t, b in [(0, 0, 1), (0, 2, 0), (3, 99, 1), (15, 100, d // 32 - 1), (7, 170, 0), (1, 383, 1), (15, 399, 0), (1, 320, 1)]:
+        store.v_scale[tables[0, t // 64].long(), h, 0, b, t % 64] = 255
+        want[sees(t), group * h:group * (h + 1), 32 * b:32 * b + 32] = True
+    for h, t in [(1, 340), (9, 63)]:
+        store.k_scale[tables[0, t // 64].long(), h, 0, 1, t % 64] = 255
+        whole[sees(t), group * h:group * (h + 1)] = True
+    want |= whole[..., None]
+    q = randn(123, rows, h_q, d)
+    ref = Attention(q, ks[0], vs[0], prefix, 0.1, window, sinks)
+    for splits in (1, 3):
+        o, lse, _ = chunk(store, tables[0], q.cuda(), prefix, 0.1, window, sinks, splits)
+        got = o.cpu()
+        assert torch.equal(torch.isnan(got), want)
+        assert torch.equal(torch.isnan(lse.cpu()), whole.T)
+        assert ((got.double() - ref.o).abs() <= ref.o_bound(CHUNK_ERROR))[~want].all()
+
+
 @pytest.mark.parametrize("fill", [0x00, 0x7F, 0xFC, 0xFD, 0xFE, 0xFF])
 @pytest.mark.parametrize("d", [64, 128])
 def test_whatever_unwritten_memory_holds(gpu, fill, d):
@@ -259,6 +310,13 @@ def test_whatever_unwritten_memory_holds(gpu, fill, d):
             ref = Attention(rows, ks[b], vs[b], 0, d ** -0.5)
             check_close(o, ref.o, ref.o_bound(CHUNK_ERROR), f"o n={n}")
             check_close(lse, ref.lse, ref.lse_bound(), f"lse n={n}")
+    _, store, tables, ks, vs = make_store4(198, [300], 192, 16, d, fill=fill)
+    rows = randn(199, 300, 128, d)
+    ref = Attention(rows, ks[0], vs[0], 0, d ** -0.5)
+    for splits in (1, 2):
+        o, lse, _ = chunk(store, tables[0], rows.cuda(), 0, d ** -0.5, splits=splits)
+        check_close(o, ref.o, ref.o_bound(CHUNK_ERROR), "o of many rows")
+        check_close(lse, ref.lse, ref.lse_bound(), "lse of many rows")
 
 
 def test_rows_of_larger_arrays(gpu):
@@ -352,19 +410,19 @@ def test_captured_step(gpu):
 def test_chunk_on_another_stream_and_in_a_graph(gpu):
     _, store, tables, ks, vs = make_store4(160, [700], 64, 2, 128)
     q = randn(161, 60, 8, 128).cuda()
-    o, lse, n_ranges = chunk(store, tables[0], q, 640, 0.1)
+    o, lse, n_ranges = chunk(store, tables[0], q, 640, 0.1, splits=3)
     assert n_ranges > 1
-    size = binding.mocap_kv4_chunk_attn_workspace_size(640, 60, 8, 2, 128)[1]
+    size = binding.mocap_kv4_chunk_attn_workspace_size(640, 60, 8, 2, 128, num_splits=3)[1]
     ws = torch.empty(size, dtype=torch.uint8, device="cuda")
     o2, lse2 = torch.zeros_like(o), torch.zeros_like(lse)
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
-    binding.mocap_kv4_chunk_attn(store, tables[0], q, 640, 0.1, o2, lse2, ws, stream=side)
+    binding.mocap_kv4_chunk_attn(store, tables[0], q, 640, 0.1, o2, lse2, ws, num_splits=3, stream=side)
     side.synchronize()
     assert torch.equal(o, o2) and torch.equal(lse, lse2)
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
-        binding.mocap_kv4_chunk_attn(store, tables[0], q, 640, 0.1, o2, lse2, ws)
+        binding.mocap_kv4_chunk_attn(store, tables[0], q, 640, 0.1, o2, lse2, ws, num_splits=3)
     for _ in range(3):
         o2.zero_()
         lse2.zero_()
@@ -379,7 +437,7 @@ def test_two_calls_at_once(gpu):
     _, store, tables, ks, vs = make_store4(165, [n, n - 100], 64, 2, d)
     lens = torch.tensor([n, n - 100], dtype=torch.int32, device="cuda")
     q, q1 = randn(166, 2, rows, 8, d).cuda(), randn(167, 2, 2, 8, d).cuda()
-    chunk_size = binding.mocap_kv4_chunk_attn_workspace_size(n - 100 - rows, rows, 8, 2, d)[1]
+    chunk_size = binding.mocap_kv4_chunk_attn_workspace_size(n - 100 - rows, rows, 8, 2, d, num_splits=4)[1]
     batch_size = binding.mocap_kv4_decode_attn_workspace_size(2, 8, 2, d, n)
     assert chunk_size > 0 and batch_size > 0
     streams, outs = [torch.cuda.Stream() for _ in range(2)], []
@@ -391,11 +449,12 @@ def test_two_calls_at_once(gpu):
     torch.cuda.synchronize()
     for _ in range(20):
         for i, (ws, o, lse, o1, lse1) in enumerate(outs):
-            binding.mocap_kv4_chunk_attn(store, tables[i], q[i], n - 100 - rows, 0.125, o, lse, ws[0], stream=streams[i])
+            binding.mocap_kv4_chunk_attn(store, tables[i], q[i], n - 100 - rows, 0.125, o, lse, ws[0], num_splits=4,
+                                         stream=streams[i])
             binding.mocap_kv4_decode_attn(store, tables, lens, q1[i], n, 0.125, o1, lse1, ws[1], stream=streams[i])
     torch.cuda.synchronize()
     for i, (_, o, lse, o1, lse1) in enumerate(outs):
-        alone = chunk(store, tables[i], q[i], n - 100 - rows, 0.125)
+        alone = chunk(store, tables[i], q[i], n - 100 - rows, 0.125, splits=4)
         assert torch.equal(o, alone[0]) and torch.equal(lse, alone[1])
         alone = decode(store, tables, lens.tolist(), q1[i], n, 0.125)
         assert torch.equal(o1, alone[0]) and torch.equal(lse1, alone[1])
