@@ -35,15 +35,15 @@ mocap_status done(hipError_t e) { return e == hipSuccess ? MOCAP_OK : MOCAP_ERR_
 // ---- A chunk's attention ----
 
 // A chunk of few rows, or with few keys, takes decoding's way (kv4_decode.hip): tiles from the
-// store to registers, a wavefront each, without barriers, in blocks of up to 32 rows that each
-// read them.  Its 32 rows of a tile cost 0.44 us of a compute unit where 256 rows cost 1.9 in
-// kv4_chunk.hip, but a few rows there cost 1.5 as well, and a workgroup takes 2 us less to
-// start.  Measured, blocks of 32 against workgroups of 256, in us (d 128 with 8 KV heads, groups
-// of 4): 16 rows a KV head behind 30000 15 and 29, behind 120000 34 and 95; 64 rows 25 and 31;
-// 128 rows 38 and 34; chunks without a prefix of 300 tokens 11 and 16, of 1000 29 and 31, of 2000
-// 73 and 52; 137 tokens of 16/2/64 in a window of 1000 11.4 and 15.5.  The rule is a time of either
-// way in us: turns of the fullest compute unit, a fixed part, the merge's traffic.  Of 142 shapes
-// the way it chose took at most 1.19 of the better one's time, 1.00 on average.
+// store to registers, a wavefront each, without barriers, in blocks of 16 or 32 rows that each
+// read them.  A block's four wavefronts take 1.4 or 1.75 us for a tile each, where 256 rows take
+// 1.9 us a tile in kv4_chunk.hip, but few rows 1.5 there as well; and their fixed part is shorter.
+// Measured in us, blocks of 16, of 32, workgroups of 256, d 128, 8 KV heads with groups of 4: 300
+// tokens without a prefix 9.4, 10.9, 15.7; 1000 29.5, 29.3, 30.8; 2000 80, 73, 52; 100 in a window of
+// 1000 11.8, 17.0, 20.7.  One of 32 and of 256: 16 rows a KV head behind 120000 positions 34 and
+// 95; 64 rows behind 30000 25 and 31, 128 rows 38 and 34.  The rule is a time of each way: turns of
+// the fullest compute unit, a fixed part, the merge's traffic.  Of 142 shapes the way it
+// chose took at most 1.14 of the best one's time, 1.007 on average, and 0.68 of that of 256.
 constexpr double kMergeUs = 3.5, kBigUs = 6.0, kSmallUs16 = 4.0, kSmallUs32 = 6.0;
 // Rows that see all keys before them: long and short row groups together where every
 // workgroup starts at once (32/8/128 heads, 2048 tokens without a prefix 74 -> 60 us,
@@ -77,33 +77,36 @@ mocap_status plan_chunk(int64_t prefix_len, int32_t chunk_len, int32_t h_q, int3
   int cus = 0;
   st = device_cu_count(&cus);
   if (st != MOCAP_OK) return st;
-  const int64_t rows = (int64_t)chunk_len * p->group, block = rows <= 16 ? 16 : 32, blocks = ceil_div(rows, block);
-  const ChunkWork big = work_of(*p, kWindowRows), small = work_of(*p, block);
+  const int64_t rows = (int64_t)chunk_len * p->group;
+  const ChunkWork big = work_of(*p, kWindowRows);
   const bool d64 = head_dim == 64;
   const double big_tile = rows <= kWindowRows / 2 ? (d64 ? 1.1 : 1.5) : (d64 ? 1.4 : 1.9);
   // (A workgroup with mirrored row groups walks the later one's tiles, half of them for both.)
   const double big_tiles = mirrored_rows(*p, cus)
                                ? 0.5 * (big.tiles + big.mean)
                                : std::max((double)big.tiles, ceil_div(p->total_wgs, cus) * big.mean);
-  const double big_us = big_tiles / p->n_ranges * big_tile + kBigUs + merge_us(*p, head_dim, p->n_ranges);
-  const double turn = block == 16 ? (d64 ? 1.1 : 1.4) : (d64 ? 1.25 : 1.75);  // of a workgroup's four wavefronts
-  const double fixed = block == 16 ? kSmallUs16 : kSmallUs32;
-  int64_t best = 0;
-  double best_us = big_us;
-  const int64_t most = std::min<int64_t>(128, small.tiles);
-  for (int64_t n = num_splits > 0 ? std::min<int64_t>(num_splits, small.tiles) : 1; n <= std::max<int64_t>(most, num_splits);
-       n += n < 32 ? 1 : 8) {
-    const double turns = std::max((double)ceil_div(small.tiles, 4 * n),
-                                  ceil_div(blocks * h_kv * n, cus) * (small.mean / (4 * n) + 0.5));
-    const double us = turns * turn + fixed + merge_us(*p, head_dim, n);
-    if (us < best_us) best_us = us, best = n;
-    if (num_splits > 0) break;
+  double best_us = big_tiles / p->n_ranges * big_tile + kBigUs + merge_us(*p, head_dim, p->n_ranges);
+  int64_t best = 0, best_blocks = 0;
+  for (const int64_t block : {16, 32}) {
+    const int64_t blocks = ceil_div(rows, block);
+    if (block == 32 && rows <= 16) break;
+    const ChunkWork small = work_of(*p, block);
+    const double turn = block == 16 ? (d64 ? 1.1 : 1.4) : (d64 ? 1.25 : 1.75);  // of a workgroup's four wavefronts
+    const double fixed = block == 16 ? kSmallUs16 : kSmallUs32;
+    const int64_t most = std::min<int64_t>(num_splits > 0 ? num_splits : 128, small.tiles);
+    for (int64_t n = num_splits > 0 ? most : 1; n <= most; n += n < 32 ? 1 : 8) {
+      if (blocks * h_kv * n > kMaxGroups) break;
+      const double turns = std::max((double)ceil_div(small.tiles, 4 * n),
+                                    ceil_div(blocks * h_kv * n, cus) * (small.mean / (4 * n) + 0.5));
+      const double us = turns * turn + fixed + merge_us(*p, head_dim, n);
+      if (us < best_us) best_us = us, best = n, best_blocks = blocks;
+    }
   }
-  if (best == 0 || best * h_kv * blocks > kMaxGroups) return MOCAP_OK;
+  if (best == 0) return MOCAP_OK;
   *few = true;
-  p->row_blocks = (int32_t)blocks;
+  p->row_blocks = (int32_t)best_blocks;
   p->n_ranges = (int32_t)best;
-  p->total_wgs = (int32_t)(blocks * h_kv * best);
+  p->total_wgs = (int32_t)(best_blocks * h_kv * best);
   return MOCAP_OK;
 }
 

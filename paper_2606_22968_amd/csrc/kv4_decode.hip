@@ -403,7 +403,7 @@ void launch(const Kv4DecodeLaunch& p, hipStream_t stream) {
 template <int D>
 void launch(const Kv4ChunkLaunch& p, hipStream_t stream) {
   const dim3 grid(p.a.total_wgs), block(kThreads);
-  if (p.a.chunk_len * p.a.group <= 16) {
+  if ((int64_t)p.a.chunk_len * p.a.group <= (int64_t)16 * p.a.row_blocks) {
     hipLaunchKernelGGL((kv4_rows_kernel<D, 1, true>), grid, block, 0, stream, p);
   } else {
     hipLaunchKernelGGL((kv4_rows_kernel<D, 2, true>), grid, block, 0, stream, p);

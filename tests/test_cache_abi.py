@@ -248,17 +248,16 @@ def plan_of(host, **kwargs):
 
 def test_chunk_plans(host):
     """Windows that hide nothing are none; rows are mirrored where one workgroup per compute unit holds them; few rows,
-    or many with few keys, go in blocks of 16 or 32."""
+    or many with few keys, go in blocks of 16, or 32 where those would take turns."""
     kv = store4(block_size=1024)
     for P, L, window, splits, mirrored, few in (
             (0, 2048, 0, 1, True, False), (30720, 2048, 0, 1, True, False), (0, 2049, 0, 1, False, False),
             (0, 8192, 0, 1, False, False), (0, 2048, 2047, 1, False, False), (0, 2048, 2048, 1, True, False),
             (20000, 500, 0, 4, True, False), (20000, 500, 0, 5, False, False), (20000, 500, 5000, 3, False, False),
-            (100, 10, 0, 1, None, True), (20000, 1, 0, 0, None, True), (20000, 4, 0, 0, None, True),
-            (20000, 5, 5000, 0, None, True), (20000, 16, 0, 9, None, True), (0, 300, 0, 0, None, True)):
+            (100, 10, 0, 1, None, 16), (20000, 1, 0, 0, None, 16), (20000, 4, 0, 0, None, 16), (20000, 5, 5000, 0, None, 16),
+            (20000, 16, 0, 40, None, 32), (0, 300, 0, 0, None, 16), (0, 600, 0, 0, None, 32)):
         p = plan_of(host, kv=kv, n_table=64, P=P, L=L, window=window, sinks=4, splits=splits)
-        rows = 256 if not few else 16 if L <= 4 else 32
-        assert bool(p["few"]) == few and p["row_blocks"] == -(-L * 4 // rows)
+        assert bool(p["few"]) == bool(few) and p["row_blocks"] == -(-L * 4 // (few or 256)), p
         assert p["total_wgs"] == p["row_blocks"] * 8 * p["n_ranges"]
         assert splits == 0 or p["n_ranges"] == splits
         assert few or bool(p["mirrored"]) == mirrored
@@ -287,19 +286,25 @@ def test_chunk_workspaces_hold_what_is_planned(host):
                         assert chunk(host, ws_bytes=size.value - 1, **args) == WORKSPACE
 
 
-def test_the_gpu_tests_run_both_ways(host):
-    from test_kv4_attn_gpu import MANY
+def test_the_gpu_tests_run_every_way(host):
+    from test_kv4_attn_gpu import IN_32, MANY
+
+    def block(h_q, h_kv, d, P, L, window, sinks, splits=0):
+        kv = store4(block_size=64, num_blocks=4096, h_kv=h_kv, head_dim=d)
+        p = plan_of(host, kv=kv, n_table=4096, P=P, L=L, h_q=h_q, h_kv=h_kv, d=d, window=window, sinks=sinks, splits=splits)
+        return 256 if not p["few"] else 16 if L * h_q // h_kv <= 16 * p["row_blocks"] else 32
+
     for d in (64, 128):
-        kv = store4(block_size=192, h_kv=16, head_dim=d)
         edges = [(200, 250, w, s, 0) for w in (1, 2, 33, 64, 65, 129, 192) for s in (0, 1, 64, 65)]
         nan = [(100, 300, w, 3 if w else 0, s) for w in (0, 100) for s in (1, 3)] + [(0, 300, 0, 0, 1), (0, 300, 0, 0, 2)]
-        for P, L, window, sinks, splits in MANY + (edges if d == 64 else []) + nan:
-            p = plan_of(host, kv=kv, n_table=64, P=P, L=L, h_q=128, h_kv=16, d=d, window=window, sinks=sinks, splits=splits)
-            assert not p["few"], (d, P, L, window, sinks, splits)
-        for P, L, window, sinks in ((500, 1, 0, 0), (511, 2, 65, 64), (700, 137, 100, 4), (0, 300, 0, 0), (250, 150, 100, 3)):
-            kv2 = store4(block_size=64, num_blocks=4096, h_kv=2, head_dim=d)
-            p = plan_of(host, kv=kv2, n_table=64, P=P, L=L, h_q=8, h_kv=2, d=d, window=window, sinks=sinks)
-            assert p["few"], (d, P, L, window, sinks)
+        for case in MANY + (edges if d == 64 else []) + nan:
+            assert block(128, 16, d, *case) == 256, (d, case)
+        for window, sinks in ((0, 0), (100, 3)):
+            assert block(128, 16, d, 250, 150, window, sinks) == 32
+        for case in ((500, 1, 0, 0), (511, 2, 65, 64), (700, 137, 100, 4), (0, 300, 0, 0), (250, 150, 100, 3)):
+            assert block(8, 2, d, *case) == 16, (d, case)
+    for case in IN_32:
+        assert block(*case) == 32, case
 
 
 def test_debug_build_checks_tables(mocap_lib, tmp_path):

@@ -155,10 +155,22 @@ def test_chunks(gpu, h_q, h_kv, d, prefix, rows, window, sinks):
 
 
 # Chunks of so many rows that a workgroup takes 256 of them (test_cache_abi.py holds that they do; the others here are
-# in blocks of up to 32 rows): prefix, rows, window, sinks, splits of 128/16 heads.
+# in blocks of 16 or 32 rows): prefix, rows, window, sinks, splits of 128/16 heads.
 MANY = [(0, 300, 0, 0, 0), (0, 300, 1, 1, 0), (0, 300, 1 << 40, 7, 0), (250, 300, 0, 0, 1), (250, 300, 100, 3, 0),
         (250, 299, 65, 64, 2), (511, 131, 63, 65, 3), (700, 137, 0, 0, 3), (963, 290, 1000, 1 << 40, 5), (64, 257, 64, 0, 0),
         (1500, 301, 700, 70, 4)]
+
+
+# In blocks of 32 rows: heads, head_dim, prefix, rows, window, sinks.
+IN_32 = [(32, 1, 128, 700, 137, 0, 0), (64, 1, 64, 700, 137, 0, 0), (64, 1, 64, 963, 200, 7, 63), (64, 1, 64, 0, 300, 0, 0),
+         (64, 1, 64, 700, 65, 1 << 40, 7), (64, 1, 64, 2001, 100, 1100, 70), (128, 16, 128, 700, 137, 0, 0),
+         (128, 16, 128, 700, 137, 100, 4), (128, 16, 64, 700, 137, 100, 4), (128, 16, 128, 250, 150, 100, 3)]
+
+
+@pytest.mark.parametrize("h_q,h_kv,d,prefix,rows,window,sinks", IN_32)
+def test_blocks_of_32_rows(gpu, h_q, h_kv, d, prefix, rows, window, sinks):
+    say(f"[case] kv4 chunk in blocks of 32 {h_q}/{h_kv}/{d} P={prefix} L={rows} W={window} sinks={sinks}")
+    run_chunk(106, h_q, h_kv, d, 192, prefix, rows, window, sinks)
 
 
 @pytest.mark.parametrize("d", [64, 128])
@@ -265,10 +277,11 @@ def test_nan_blocks(gpu, d, window, sinks):
 
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("window,sinks", [(0, 0), (100, 3)])
-def test_nan_blocks_of_many_rows(gpu, d, window, sinks):
-    """As test_nan_blocks, where a workgroup takes 256 rows."""
-    n, prefix, rows, h_q, h_kv = 400, 100, 300, 128, 16
-    group = h_q // h_kv
+@pytest.mark.parametrize("rows,splits", [(300, (1, 3)), (150, (0, 2))])
+def test_nan_blocks_of_more_rows(gpu, d, window, sinks, rows, splits):
+    """As test_nan_blocks, where a workgroup takes 256 rows, and blocks of 32."""
+    n, h_q, h_kv = 400, 128, 16
+    prefix, group = n - rows, h_q // h_kv
     _, store, tables, ks, vs = make_store4(122, [n], 64, h_kv, d)
     pos = prefix + torch.arange(rows)
     want, whole = torch.zeros((rows, h_q, d), dtype=torch.bool), torch.zeros((rows, h_q), dtype=torch.bool)
@@ -285,8 +298,8 @@ def test_nan_blocks_of_many_rows(gpu, d, window, sinks):
     want |= whole[..., None]
     q = randn(123, rows, h_q, d)
     ref = Attention(q, ks[0], vs[0], prefix, 0.1, window, sinks)
-    for splits in (1, 3):
-        o, lse, _ = chunk(store, tables[0], q.cuda(), prefix, 0.1, window, sinks, splits)
+    for num in splits:
+        o, lse, _ = chunk(store, tables[0], q.cuda(), prefix, 0.1, window, sinks, num)
         got = o.cpu()
         assert torch.equal(torch.isnan(got), want)
         assert torch.equal(torch.isnan(lse.cpu()), whole.T)
