@@ -110,6 +110,31 @@ mocap_status plan_chunk(int64_t prefix_len, int32_t chunk_len, int32_t h_q, int3
   return MOCAP_OK;
 }
 
+// ---- A batch's attention ----
+
+// Groups of more than 16 heads: blocks of 16, which start sooner (NT 1: less to join in LDS), or of
+// 32, which read and convert keys and values once, where a compute unit has more than kBlockTurns
+// turns of four tiles at the most.  Measured in us, blocks of 16 and of 32: one sequence of 2048,
+// 32/1/128 10.6 and 12.7; 8 of 1024, 64/2/128 10.3 and 14.3; at 8 turns 64/2/128 22.5 and 23.1,
+// 128/2/64 21.9 and 22.4, 40/2/128 21.9 and 21.2; at 24 64/1/64 29.4 and 27.7; at 64 128/2/64 61.1
+// and 52.3.
+constexpr int64_t kBlockTurns = 8;
+mocap_status plan_batch_rows(int32_t batch, int64_t max_len, int32_t h_q, int32_t h_kv, int64_t window, int64_t sinks,
+                             DecodeAttnLaunch* p) {
+  mocap_status st = plan_decode(batch, max_len, h_q, h_kv, window, sinks, p);
+  if (st != MOCAP_OK || p->group <= 16) return st;
+  int cus = 0;
+  st = device_cu_count(&cus);
+  if (st != MOCAP_OK) return st;
+  int64_t tiles = ceil_div(max_len, kTileKeys);
+  if (p->seqs.window > 0)
+    tiles = std::min(tiles, ceil_div(p->seqs.window, kTileKeys) + 1 + ceil_div(p->seqs.sinks, kTileKeys));
+  const int64_t blocks = ceil_div(p->group, 16);
+  if (batch * tiles * h_kv * blocks > kBlockTurns * 4 * cus) return MOCAP_OK;
+  p->row_blocks = (int32_t)blocks;
+  return plan_batch(batch, max_len, window, sinks, h_kv * blocks, kDecodeWideGroupsPerCu, true, &p->seqs, &p->may_split);
+}
+
 // ---- Rows ----
 
 // 2-byte values of `tokens` rows of `heads` heads.
@@ -280,7 +305,7 @@ mocap_status mocap_kv4_decode_attn_workspace_size(int32_t batch, int64_t max_len
   *bytes_out = 0;
   if (batch == 0) return MOCAP_OK;
   DecodeAttnLaunch p;
-  st = plan_decode(batch, max_len, h_q, h_kv, window, sinks, &p);
+  st = plan_batch_rows(batch, max_len, h_q, h_kv, window, sinks, &p);
   if (st == MOCAP_OK) *bytes_out = decode_workspace(p, head_dim);
   return st;
 }
@@ -300,7 +325,7 @@ mocap_status mocap_kv4_decode_attn(const mocap_kv4_store* kv, const int32_t* blo
   if (scales_missing(kv) || !q || !o || !lse || !aligned16(q) || !aligned16(o) || !aligned4(lse))
     return MOCAP_ERR_INVALID_ARG;
   Kv4DecodeLaunch p;
-  st = plan_decode(batch, max_len, h_q, h_kv, window, sinks, &p.a);
+  st = plan_batch_rows(batch, max_len, h_q, h_kv, window, sinks, &p.a);
   if (st != MOCAP_OK) return st;
   if (p.a.may_split && (!workspace || !aligned16(workspace) || workspace_bytes < decode_workspace(p.a, head_dim)))
     return MOCAP_ERR_WORKSPACE;

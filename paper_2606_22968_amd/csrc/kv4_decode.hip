@@ -34,7 +34,7 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 
-// NT: 16-row blocks that a workgroup takes.  Rows are the heads of a sequence's group, or
+// NT: 16-row blocks that a workgroup takes (1 or 2: see cache_api.cpp).  Rows are the heads of a sequence's group, or
 // (CHUNK) those of all tokens of a chunk, row r token r / G.
 template <int D, int NT, bool CHUNK>
 __global__ __launch_bounds__(kThreads) void kv4_rows_kernel(

@@ -11,6 +11,7 @@ mocap::RopeAppendLaunch append;
 mocap::Kv4ChunkLaunch chunk;
 bool few = false;
 mocap::SeqBatch seqs;
+int row_blocks = 0;
 int launches = 0;
 }  // namespace
 
@@ -26,6 +27,7 @@ hipError_t launch_decode_rope_append(const RopeAppendLaunch& p, int, hipStream_t
 hipError_t launch_kv4_load(const Kv4LoadLaunch&, int, hipStream_t) { return ++launches, hipSuccess; }
 hipError_t launch_kv4_decode(const Kv4DecodeLaunch& p, int, hipStream_t) {
   seqs = p.a.seqs;
+  row_blocks = p.a.row_blocks;
   return ++launches, hipSuccess;
 }
 hipError_t launch_kv4_chunk(const Kv4ChunkLaunch& p, int, hipStream_t) {
@@ -57,6 +59,7 @@ hipError_t hipMemcpy(void* dst, const void* src, size_t bytes, hipMemcpyKind) {
 }
 
 int record_launches() { return launches; }
+int record_row_blocks() { return row_blocks; }
 void record_append(long long* out) {
   const long long v[] = {append.rot, append.interleaved, append.h_q, append.h_kv, append.q_stride, append.k_stride,
                          append.v_stride, append.start_pos, append.first_pos, append.chunk_len,

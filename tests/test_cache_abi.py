@@ -307,6 +307,22 @@ def test_the_gpu_tests_run_every_way(host):
         assert block(*case) == 32, case
 
 
+def test_blocks_of_heads(host):
+    """Groups of more than 16 heads: blocks of 16, of 32 in batches that may be large; workspaces are as planned."""
+    size = ctypes.c_size_t()
+    for h_q, h_kv, batch, max_len, window, blocks in (
+            (16, 1, 1, 100, 0, 1), (17, 1, 1, 100, 0, 2), (64, 1, 18, 700, 0, 4), (20, 1, 18, 700, 0, 2),
+            (32, 8, 64, 1 << 20, 0, 1), (32, 1, 32, 8192, 0, 2), (32, 1, 33, 8192, 0, 1), (64, 1, 33, 8192, 0, 2),
+            (64, 1, 33, 8192, 1000, 4), (40, 1, 4000, 700, 1, 2), (20, 1, 3012, 700, 1, 1), (40, 2, 3012, 700, 700, 1)):
+        kv = store4(h_kv=h_kv)
+        args = dict(kv=kv, stride=-(-max_len // 256), batch=batch, max_len=max_len, h_q=h_q, h_kv=h_kv, window=window, sinks=1)
+        assert host.mocap_kv4_decode_attn_workspace_size(batch, max_len, h_q, h_kv, 128, window, 1, ctypes.byref(size)) == 0
+        assert decode(host, ws_bytes=size.value, **args) == 0
+        assert host.record_row_blocks() == blocks, (h_q, h_kv, batch, max_len, window)
+        if size.value:
+            assert decode(host, ws_bytes=size.value - 1, **args) == WORKSPACE
+
+
 def test_debug_build_checks_tables(mocap_lib, tmp_path):
     """The checking build refuses what a call's tables may not name, and looks at no other entry."""
     lib = recording_build(mocap_lib, tmp_path, "-DMOCAP_DEBUG_TABLES")

@@ -98,6 +98,27 @@ def test_decode_windows(gpu, h_q, h_kv, d, window, sinks):
     check_decode(o, lse, q, ks, vs, lens, d ** -0.5, window, sinks)
 
 
+@pytest.mark.parametrize("h_q,h_kv,d", [(20, 1, 64), (32, 1, 128), (40, 2, 128)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 1), (100, 65), (700, 4), (701, 4)])
+def test_large_batches(gpu, h_q, h_kv, d, window, sinks):
+    """So many sequences that groups of more than 16 heads go 32 at a time; most are empty."""
+    lens = [1, 0, 5, 64, 65, 100, 129, 333, 448, 700]
+    say(f"[case] kv4 decode large batch window={window} sinks={sinks} {h_q}/{h_kv}/{d}")
+    _, store, tables, ks, vs = make_store4(8, lens, 64, h_kv, d)
+    for b, n in enumerate(lens):
+        for t in range(n):
+            if window and not (t < sinks or t > n - 1 - window):
+                block, slot = tables[b, t // 64].long(), t % 64
+                store.k_scale[block, :, 0, :, slot] = 255
+                store.v_scale[block, :, 0, :, slot] = 255
+    more = lens + [0] * 3002
+    tables = torch.cat((tables, torch.zeros((3002, tables.shape[1]), dtype=torch.int32, device="cuda")))
+    q = randn(9, len(more), h_q, d).cuda()
+    o, lse = decode(store, tables, more, q, 700, d ** -0.5, window, sinks)
+    check_decode(o[:len(lens)], lse[:len(lens)], q[:len(lens)], ks, vs, lens, d ** -0.5, window, sinks)
+    assert (o[len(lens):] == 0).all() and (lse[len(lens):] == -math.inf).all()
+
+
 @pytest.mark.parametrize("lens", [[20000], [9001, 1, 64], [5000, 0, 30000, 257, 12345], [2049] * 70, [1] * 200 + [4000]])
 @pytest.mark.parametrize("h_q,h_kv,d,bs", [(4, 1, 128, 256), (8, 2, 64, 1600)])
 def test_cut_sequences(gpu, lens, h_q, h_kv, d, bs):
