@@ -159,8 +159,8 @@ mocap_status mocap_kv4_decode_attn(const mocap_kv4_store* kv, const int32_t* blo
  * mocap_kv4_chunk_attn_workspace_size, mocap_kv4_chunk_attn -- a chunk's causal
  * attention over a 4-bit store: mocap_chunk_attn with window = 0,
  * mocap_window_attn with window >= 1 (sinks then count), with their arguments,
- * results and precision (probabilities in bf16).  The chunk's own keys and
- * values are read from the store as well.  num_splits as in
+ * results and precision (probabilities in bf16, or nearer).  The chunk's own keys
+ * and values are read from the store as well.  num_splits as in
  * mocap_window_attn_workspace_size.  NaN blocks reach exactly the rows that see
  * them, as in mocap_kv4_decode_attn.
  * Errors: as mocap_window_attn, but window = 0 and blocks of any size are taken.

@@ -15,7 +15,7 @@
 //     g holds the scores of keys 16 g .. + 15, in order over the four products.  That
 //     is what a 16-byte load of a V row gives it: 16 keys of dims 32 b + i and
 //     32 b + 16 + i, one byte a key, which with that key's scale become a pair.
-// Measured: four sequences of 65537 to 131072 positions, 64/8/128 heads, 452 MB in 85 us,
+// Measured: four sequences of 65537 to 131072 positions, 64/8/128 heads, 452 MB in 85 to 89 us,
 // 5.3 TB/s, 5.9 without the 6 us that a launch of one tile a wavefront takes; 32 of up to
 // 8192, 32/8/128, 23 us for 83 MB; one of 2048, 6 us.  HBM and that latency bound it:
 // without V's conversion it takes 3% less, without the low halves of the probabilities 2%.
