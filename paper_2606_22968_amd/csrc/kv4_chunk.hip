@@ -13,7 +13,7 @@
 //   * A value block that reads as NaN is left to the product where all rows of the
 //     workgroup see its tile.  In other tiles its scale is set next to 0, and the rows
 //     that see it get NaN in its dims at the end.
-// Measured: 2048 tokens of 32/8/128 heads behind 30720, 960 to 1010 us by the card, 1.05 to
+// Measured: 2048 tokens of 32/8/128 heads behind 30720, 960 to 1030 us by the card, 1.03 to
 // 1.11 PFLOP/s.  Issue bounds it: MFMAs hold 45% of the SIMDs' cycles, a third of those beside
 // vector instructions (2.3 GHz).  The conversion is 5.5% of it, half of that the stores to LDS.
 // Tried: a table entry looked up a tile ahead (no difference); pieces dealt to the lanes so
