@@ -117,3 +117,46 @@ def test_run(gpu, four, h_q, h_kv, d, interleaved):
                 assert torch.equal(k_held[-1:].double(), values(*quantise(want_k[b:b + 1])))
             check_rows(o[b:b + 1], lse[b][:, None], q_out[b:b + 1], k_held, v_held, n - 1, scale, 2.0 ** -16,
                        f"step {step} sequence {b}")
+
+
+def test_table_checks(gpu):
+    """With table checks every call looks at the entries that its positions use, before anything is enqueued, and does the
+    same as without."""
+    rope = binding.Rope(inv_freq(64).cuda())
+    store4, store = binding.Kv4Store(4, 64, 2, 64, fill=0), binding.KvStore(4, 64, 2, 64, fill=0.0)
+    good, bad = (torch.tensor([3, 1, x], dtype=torch.int32, device="cuda") for x in (0, 9))   # bad: from position 128
+    k, v, q = (randn(120 + i, 20, h, 64).cuda() for i, h in enumerate((2, 2, 4)))
+    q_out, o = torch.empty_like(q), torch.empty_like(q)
+    lse, lse1 = torch.empty((4, 20), device="cuda"), torch.empty((1, 4), device="cuda")
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+
+    def at(n):
+        return torch.tensor([n], dtype=torch.int32, device="cuda")
+
+    def calls(table, end):
+        yield lambda: binding.mocap_kv4_append(store4, table, end - 20, k, v, rope, None, q, q_out)
+        yield lambda: binding.mocap_rope_append(store, table, end - 20, k, v, rope, None, q, q_out)
+        yield lambda: binding.mocap_kv4_decode_append(store4, table[None], at(end), k[:1], v[:1], rope, None, q[:1], q_out[:1])
+        yield lambda: binding.mocap_decode_rope_append(store, table[None], at(end), k[:1], v[:1], rope, None, q[:1], q_out[:1])
+        yield lambda: binding.mocap_kv4_load(store4, table[None], at(end), torch.empty_like(k)[None], torch.empty_like(v)[None])
+        yield lambda: binding.mocap_kv4_decode_attn(store4, table[None], at(end), q[:1], 192, 0.1, o[:1], lse1, ws)
+        yield lambda: binding.mocap_kv4_chunk_attn(store4, table, q, end - 20, 0.1, o, lse, ws)
+
+    binding.set_table_checks(True)
+    try:
+        for call in (*calls(good, 150), *calls(bad, 128)):
+            call()
+        for call in calls(bad, 130):
+            with pytest.raises(binding.MocapError):
+                call()
+    finally:
+        binding.set_table_checks(False)
+    for call in calls(good, 150):
+        call()
+    again = torch.empty_like(o)
+    binding.set_table_checks(True)
+    try:
+        binding.mocap_kv4_chunk_attn(store4, good, q, 130, 0.1, again, lse, ws)
+    finally:
+        binding.set_table_checks(False)
+    assert torch.equal(again, o)
