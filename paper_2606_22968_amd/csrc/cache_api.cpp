@@ -43,7 +43,7 @@ mocap_status done(hipError_t e) { return e == hipSuccess ? MOCAP_OK : MOCAP_ERR_
 // 1000 11.8, 17.0, 20.7.  One of 32 and of 256: 16 rows a KV head behind 120000 positions 34 and
 // 95; 64 rows behind 30000 25 and 31, 128 rows 38 and 34.  The rule is a time of each way: turns of
 // the fullest compute unit, a fixed part, the merge's traffic.  Of 142 shapes the way it
-// chose took at most 1.14 of the best one's time, 1.007 on average, and 0.68 of that of 256.
+// chose took at most 1.15 of the best one's time, 1.002 on average, and 0.68 of that of 256.
 constexpr double kMergeUs = 3.5, kBigUs = 6.0, kSmallUs16 = 4.0, kSmallUs32 = 6.0;
 // Rows that see all keys before them: long and short row groups together where every
 // workgroup starts at once (32/8/128 heads, 2048 tokens without a prefix 74 -> 60 us,
@@ -96,8 +96,10 @@ mocap_status plan_chunk(int64_t prefix_len, int32_t chunk_len, int32_t h_q, int3
     const int64_t most = std::min<int64_t>(num_splits > 0 ? num_splits : 128, small.tiles);
     for (int64_t n = num_splits > 0 ? most : 1; n <= most; n += n < 32 ? 1 : 8) {
       if (blocks * h_kv * n > kMaxGroups) break;
-      const double turns = std::max((double)ceil_div(small.tiles, 4 * n),
-                                    ceil_div(blocks * h_kv * n, cus) * (small.mean / (4 * n) + 0.5));
+      // (Two workgroups of 16 rows share a compute unit's time; of 32, one after the other.)
+      const int64_t wgs = blocks * h_kv * n;
+      const double per_cu = wgs <= cus ? 1.0 : block == 16 ? 0.5 * ceil_div(2 * wgs, cus) : (double)ceil_div(wgs, cus);
+      const double turns = std::max((double)ceil_div(small.tiles, 4 * n), per_cu * (small.mean / (4 * n) + 0.5));
       const double us = turns * turn + fixed + merge_us(*p, head_dim, n);
       if (us < best_us) best_us = us, best = n, best_blocks = blocks;
     }

@@ -183,9 +183,10 @@ MANY = [(0, 300, 0, 0, 0), (0, 300, 1, 1, 0), (0, 300, 1 << 40, 7, 0), (250, 300
 
 
 # In blocks of 32 rows: heads, head_dim, prefix, rows, window, sinks.
-IN_32 = [(32, 1, 128, 700, 137, 0, 0), (64, 1, 64, 700, 137, 0, 0), (64, 1, 64, 963, 200, 7, 63), (64, 1, 64, 0, 300, 0, 0),
-         (64, 1, 64, 700, 65, 1 << 40, 7), (64, 1, 64, 2001, 100, 1100, 70), (128, 16, 128, 700, 137, 0, 0),
-         (128, 16, 128, 700, 137, 100, 4), (128, 16, 64, 700, 137, 100, 4), (128, 16, 128, 250, 150, 100, 3)]
+IN_32 = [(32, 1, 128, 200, 500, 64, 64), (32, 1, 128, 1000, 200, 900, 65), (64, 1, 64, 0, 300, 0, 0),
+         (64, 1, 64, 2001, 100, 1100, 70), (32, 8, 128, 0, 600, 0, 0), (32, 8, 128, 200, 500, 64, 64),
+         (128, 16, 128, 700, 137, 0, 0), (128, 16, 64, 700, 160, 100, 4), (128, 16, 64, 512, 150, 64, 65),
+         (128, 16, 128, 250, 150, 100, 3)]
 
 
 @pytest.mark.parametrize("h_q,h_kv,d,prefix,rows,window,sinks", IN_32)
