@@ -6,6 +6,10 @@
 // Nothing is refused here.  Where an argument is not what a call takes, or only unusual,
 // the answer is None, and binding.py's own path checks it, says what is wrong or makes the
 // call.
+//
+// The library's call itself runs without the interpreter's lock, as with ctypes: a launch may wait
+// for a full queue, or for a stream behind a host function that needs the lock.  The caller
+// holds the arguments meanwhile; the tensors that a store or a rotation names are held here.
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -65,13 +69,18 @@ bool integer32(PyObject* o, int32_t* out) {
   return true;
 }
 
-// An attribute, released at the end of its scope (its owner keeps what it names).
+// An attribute, released at the end of its scope.
 struct Attr {
-  PyObject* o;
-  Attr(PyObject* from, PyObject* name) : o(PyObject_GetAttr(from, name)) {
+  PyObject* o = nullptr;
+  Attr() = default;
+  Attr(PyObject* from, PyObject* name) { get(from, name); }
+  Attr(const Attr&) = delete;
+  Attr& operator=(const Attr&) = delete;
+  ~Attr() { Py_XDECREF(o); }
+  void get(PyObject* from, PyObject* name) {
+    Py_XSETREF(o, PyObject_GetAttr(from, name));
     if (o == nullptr) PyErr_Clear();
   }
-  ~Attr() { Py_XDECREF(o); }
 };
 PyObject *n_k_pool, *n_v_pool, *n_k_scale, *n_v_scale, *n_num_blocks, *n_block_size, *n_h_kv, *n_head_dim, *n_inv_freq,
     *n_interleaved;
@@ -80,9 +89,9 @@ bool number(PyObject* from, PyObject* name, int32_t* out) {
   const Attr a(from, name);
   return a.o != nullptr && integer32(a.o, out);
 }
-bool pool(PyObject* from, PyObject* name, at::ScalarType type, long ndim, long device, void** out) {
-  const Attr a(from, name);
-  const at::Tensor* t = a.o != nullptr ? dense(a.o, type, ndim, device) : nullptr;
+bool pool(PyObject* from, PyObject* name, at::ScalarType type, long ndim, long device, Attr* held, void** out) {
+  held->get(from, name);
+  const at::Tensor* t = held->o != nullptr ? dense(held->o, type, ndim, device) : nullptr;
   if (t == nullptr) return false;
   *out = t->data_ptr();
   return true;
@@ -93,6 +102,7 @@ struct Store {
   mocap_kv_store b;
   mocap_kv4_store q;
   int32_t h_kv, head_dim;
+  Attr held[4];
 };
 bool store_of(PyObject* o, bool four, long device, Store* s) {
   int32_t blocks, size;
@@ -101,21 +111,24 @@ bool store_of(PyObject* o, bool four, long device, Store* s) {
     return false;
   if (!four) {
     s->b = mocap_kv_store{nullptr, nullptr, blocks, size, s->h_kv, s->head_dim};
-    return pool(o, n_k_pool, at::kBFloat16, 4, device, &s->b.k_pool) &&
-           pool(o, n_v_pool, at::kBFloat16, 4, device, &s->b.v_pool);
+    return pool(o, n_k_pool, at::kBFloat16, 4, device, &s->held[0], &s->b.k_pool) &&
+           pool(o, n_v_pool, at::kBFloat16, 4, device, &s->held[1], &s->b.v_pool);
   }
   s->q = mocap_kv4_store{nullptr, nullptr, nullptr, nullptr, blocks, size, s->h_kv, s->head_dim};
-  return pool(o, n_k_pool, at::kByte, 4, device, &s->q.k_pool) && pool(o, n_v_pool, at::kByte, 5, device, &s->q.v_pool) &&
-         pool(o, n_k_scale, at::kByte, 5, device, &s->q.k_scale) && pool(o, n_v_scale, at::kByte, 5, device, &s->q.v_scale);
+  return pool(o, n_k_pool, at::kByte, 4, device, &s->held[0], &s->q.k_pool) &&
+         pool(o, n_v_pool, at::kByte, 5, device, &s->held[1], &s->q.v_pool) &&
+         pool(o, n_k_scale, at::kByte, 5, device, &s->held[2], &s->q.k_scale) &&
+         pool(o, n_v_scale, at::kByte, 5, device, &s->held[3], &s->q.v_scale);
 }
 
 // A Rope or None.
-bool rope_of(PyObject* o, long device, mocap_rope* r, const mocap_rope** out) {
+bool rope_of(PyObject* o, long device, Attr* held, mocap_rope* r, const mocap_rope** out) {
   *out = nullptr;
   if (o == Py_None) return true;
-  const Attr f(o, n_inv_freq), i(o, n_interleaved);
-  if (f.o == nullptr || i.o == nullptr || !PyBool_Check(i.o)) return false;
-  const at::Tensor* t = dense(f.o, at::kFloat, 1, device);
+  held->get(o, n_inv_freq);
+  const Attr i(o, n_interleaved);
+  if (held->o == nullptr || i.o == nullptr || !PyBool_Check(i.o)) return false;
+  const at::Tensor* t = dense(held->o, at::kFloat, 1, device);
   if (t == nullptr || t->size(0) > (1 << 20)) return false;
   *r = mocap_rope{static_cast<const float*>(t->data_ptr()), (int32_t)(2 * t->size(0)), i.o == Py_True};
   *out = r;
@@ -126,6 +139,7 @@ bool rope_of(PyObject* o, long device, mocap_rope* r, const mocap_rope** out) {
 struct Append {
   Store store;
   Rows k, v, q;
+  Attr inv_freq;
   mocap_rope rope_value;
   const mocap_rope* rope;
   void* q_out = nullptr;
@@ -145,7 +159,7 @@ bool append_of(PyObject* store, bool four, PyObject* k, PyObject* v, PyObject* r
   } else if (q_out != Py_None) {
     return false;
   }
-  return rope_of(rope, device, &a->rope_value, &a->rope);
+  return rope_of(rope, device, &a->inv_freq, &a->rope_value, &a->rope);
 }
 
 // Block tables [batch][stride] and lengths [batch].
@@ -236,7 +250,20 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return nullptr;
 }
 
-PyObject* status(mocap_status st) { return PyLong_FromLong(st); }
+// Makes a call without the interpreter's lock.
+struct Unlocked {
+  PyThreadState* state = PyEval_SaveThread();
+  ~Unlocked() { PyEval_RestoreThread(state); }
+};
+template <typename... P, typename... A>
+PyObject* made(mocap_status (*call)(P...), A... args) {
+  mocap_status st;
+  {
+    const Unlocked u;
+    st = call(args...);
+  }
+  return PyLong_FromLong(st);
+}
 
 // append_chunk(store, table, start_pos, k, v, rope, position, q, q_out, stream, device)
 template <bool FOUR>
@@ -254,10 +281,10 @@ PyObject* append_chunk(PyObject* const* a) {
   const int32_t* t = static_cast<const int32_t*>(table->data_ptr());
   const int32_t n = (int32_t)table->size(0), tokens = (int32_t)p.k.tokens, h_q = (int32_t)p.q.heads;
   if (FOUR)
-    return status(lib.kv4_append(&p.store.q, t, n, start, tokens, p.rope, position, p.q.at, p.q.stride, h_q, p.k.at,
-                                 p.k.stride, p.v.at, p.v.stride, p.q_out, stream));
-  return status(lib.rope_append(&p.store.b, t, n, start, tokens, p.rope, position, p.q.at, p.q.stride, h_q, p.k.at,
-                                p.k.stride, p.v.at, p.v.stride, p.q_out, stream));
+    return made(lib.kv4_append, &p.store.q, t, n, start, tokens, p.rope, position, p.q.at, p.q.stride, h_q, p.k.at,
+                p.k.stride, p.v.at, p.v.stride, p.q_out, stream);
+  return made(lib.rope_append, &p.store.b, t, n, start, tokens, p.rope, position, p.q.at, p.q.stride, h_q, p.k.at,
+              p.k.stride, p.v.at, p.v.stride, p.q_out, stream);
 }
 
 // append_batch(store, tables, lens, k, v, rope, positions, q, q_out, stream, device)
@@ -278,10 +305,10 @@ PyObject* append_batch(PyObject* const* a) {
   }
   const int32_t h_q = (int32_t)p.q.heads;
   if (FOUR)
-    return status(lib.kv4_decode_append(&p.store.q, b.tables, b.stride, b.lens, b.batch, p.rope, positions, p.q.at,
-                                        p.q.stride, h_q, p.k.at, p.k.stride, p.v.at, p.v.stride, p.q_out, stream));
-  return status(lib.decode_rope_append(&p.store.b, b.tables, b.stride, b.lens, b.batch, p.rope, positions, p.q.at,
-                                       p.q.stride, h_q, p.k.at, p.k.stride, p.v.at, p.v.stride, p.q_out, stream));
+    return made(lib.kv4_decode_append, &p.store.q, b.tables, b.stride, b.lens, b.batch, p.rope, positions, p.q.at,
+                p.q.stride, h_q, p.k.at, p.k.stride, p.v.at, p.v.stride, p.q_out, stream);
+  return made(lib.decode_rope_append, &p.store.b, b.tables, b.stride, b.lens, b.batch, p.rope, positions, p.q.at,
+              p.q.stride, h_q, p.k.at, p.k.stride, p.v.at, p.v.stride, p.q_out, stream);
 }
 
 // load(store, tables, ends, k, v, stream, device)
@@ -296,8 +323,8 @@ PyObject* load(PyObject* const* a) {
   if (k == nullptr || v == nullptr || k->sizes() != v->sizes() || k->size(0) != b.batch || !fits(k->size(1)) ||
       k->size(2) != s.h_kv || k->size(3) != s.head_dim)
     return nullptr;
-  return status(lib.kv4_load(&s.q, b.tables, b.stride, b.lens, b.batch, (int32_t)k->size(1), k->data_ptr(), v->data_ptr(),
-                             stream));
+  return made(lib.kv4_load, &s.q, b.tables, b.stride, b.lens, b.batch, (int32_t)k->size(1), k->data_ptr(), v->data_ptr(),
+              stream);
 }
 
 // decode_attn(store, tables, lens, q, max_len, scale, o, lse, workspace, window, sinks, stream, device)
@@ -312,8 +339,8 @@ PyObject* decode_attn(PyObject* const* a) {
       !store_of(a[0], true, device, &s) || !batch_of(a[1], a[2], device, &b) ||
       !attn_of(a[3], a[5], a[6], a[7], a[8], true, device, &t) || t.rows != b.batch)
     return nullptr;
-  return status(lib.kv4_decode_attn(&s.q, b.tables, b.stride, b.lens, b.batch, max_len, t.q, t.h_q, s.h_kv, t.dim, t.scale,
-                                    window, sinks, t.o, t.lse, t.workspace, t.bytes, stream));
+  return made(lib.kv4_decode_attn, &s.q, b.tables, b.stride, b.lens, b.batch, max_len, t.q, t.h_q, s.h_kv, t.dim, t.scale,
+              window, sinks, t.o, t.lse, t.workspace, t.bytes, stream);
 }
 
 // chunk_attn(store, table, q, prefix_len, scale, o, lse, workspace, window, sinks, num_splits, stream, device)
@@ -330,9 +357,9 @@ PyObject* chunk_attn(PyObject* const* a) {
     return nullptr;
   const at::Tensor* table = dense(a[1], at::kInt, 1, device);
   if (table == nullptr || !fits(table->size(0))) return nullptr;
-  return status(lib.kv4_chunk_attn(&s.q, static_cast<const int32_t*>(table->data_ptr()), (int32_t)table->size(0), t.q, prefix,
-                                   t.rows, t.h_q, s.h_kv, t.dim, t.scale, window, sinks, t.o, t.lse, t.workspace, t.bytes,
-                                   splits, stream));
+  return made(lib.kv4_chunk_attn, &s.q, static_cast<const int32_t*>(table->data_ptr()), (int32_t)table->size(0), t.q, prefix,
+              t.rows, t.h_q, s.h_kv, t.dim, t.scale, window, sinks, t.o, t.lse, t.workspace, t.bytes,
+              splits, stream);
 }
 
 // A call with N arguments: its status, or None.  (Calls whose library is not loaded too.)
