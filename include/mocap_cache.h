@@ -25,9 +25,10 @@ extern "C" {
  * the pair (x, y) becomes
  *   (x cos a - y sin a, x sin a + y cos a),   a = p * inv_freq[i],
  * where x, y are dims i and i + rot_dim / 2, or 2 i and 2 i + 1 if interleaved.
- * Other dims stay as they are.  Angles are taken in 64 bits, so far positions
- * lose nothing.
- *   inv_freq      device fp32 [rot_dim / 2], any values
+ * Other dims stay as they are.  Angles are taken exactly, so far positions lose
+ * nothing; a pair whose angle is 2^48 radians or more, or no number, becomes NaN.
+ *   inv_freq      device fp32 [rot_dim / 2]; below 2^17 (a layer's are at most 1) no
+ *                 position reaches that
  *   rot_dim       16 .. head_dim, a multiple of 16
  */
 typedef struct mocap_rope {

@@ -10,7 +10,7 @@
 //     16-byte pieces that hold eight whole pairs (dims 8 c .. and rot / 2 + 8 c ..,
 //     or 16 c .. with neighbours paired), so pairs never leave a thread, and its
 //     eight angles serve all its heads.
-//   * p inv_freq is exact in fp64 (31 + 24 bits) but for positions beyond 2^29, and is
+//   * p inv_freq has 31 + 24 bits and is taken as the sum of two fp64 values, exact, and
 //     reduced to a quarter turn with pi/2 in two parts; sine and cosine of the rest
 //     are Taylor polynomials.  gfx950 runs fp64 at the fp32 rate.
 //   * For 4 bits the products stay in fp64, and the result goes to fp32 rounded to odd
@@ -31,14 +31,22 @@
 namespace mocap {
 namespace {
 
-// cos and sin of x.  T: what the polynomials are evaluated in.
+// cos and sin of p f.  T: what the polynomials are evaluated in.  fp64 results are within 2^-52;
+// without the product's low part they would lose 2^-54 of the angle where p f has more than
+// 53 bits (1e-7 at positions near 2^31).  From kMaxAngle on, where the number of turns would lose
+// its fraction, they are NaN.
+constexpr double kMaxAngle = 281474976710656.;  // 2^48
 template <typename T>
-__device__ __forceinline__ void turn(double x, T* c, T* s) {
-  const double n = rint(x * 0.63661977236758134);  // 2 / pi
-  // pi / 2 = 1.5707963267948966 + 6.123233995736766e-17 (to 2^-107)
-  const T r = (T)fma(-n, 6.123233995736766e-17, fma(-n, 1.5707963267948966, x));
+__device__ __forceinline__ void turn(double p, double f, T* c, T* s) {
+  const double x = p * f, x_low = fma(p, f, -x);
+  // Quarter turns, x 2 / pi, rounded by a sum of which the last bits hold whole numbers.
+  constexpr double kWhole = 6755399441055744.;  // 1.5 * 2^52
+  const double shifted = fma(x, 0.63661977236758134, kWhole), n = shifted - kWhole;
+  // pi / 2 = 1.5707963267948966 + 6.123233995736766e-17 (to 2^-107); the first sum is exact.
+  const double rest = fma(-n, 1.5707963267948966, x) + fma(-n, 6.123233995736766e-17, x_low);
+  const T r = fabs(x) < kMaxAngle ? (T)rest : (T)NAN;
   const T r2 = r * r;
-  T sine, cosine;  // |r| <= pi / 4: the terms left out are below 5e-17 (fp32: 4e-9)
+  T sine, cosine;  // |r| < 0.81: the terms left out are below 1e-16 (fp32: 4e-9)
   if (sizeof(T) == 8) {
     sine = T(-1. / 1307674368000);
     sine = sine * r2 + T(1. / 6227020800);
@@ -61,7 +69,7 @@ __device__ __forceinline__ void turn(double x, T* c, T* s) {
   cosine = cosine * r2 + T(1. / 24);
   cosine = cosine * r2 + T(-0.5);
   cosine = cosine * r2 + T(1);
-  const int quarter = (int)(n - 4. * floor(0.25 * n));
+  const uint32_t quarter = (uint32_t)__double2loint(shifted);
   const T a = quarter & 1 ? sine : cosine, b = quarter & 1 ? cosine : sine;
   *c = (quarter + 1) & 2 ? -a : a;
   *s = quarter & 2 ? -b : b;
@@ -97,7 +105,7 @@ __device__ __forceinline__ void make_turns(const RopeAppendLaunch& p, int c, int
 #pragma unroll
   for (int j = 0; j < 8; ++j) f[j] = p.inv_freq[c * 8 + j];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) turn((double)pos * (double)f[j], &t->c[j], &t->s[j]);
+  for (int j = 0; j < 8; ++j) turn((double)pos, (double)f[j], &t->c[j], &t->s[j]);
 }
 
 __device__ __forceinline__ void widen(const u32x4& x, float* y) {
@@ -351,7 +359,7 @@ __global__ __launch_bounds__(64) void decode_rope_append_kernel(const RopeAppend
   }
   if ((int)threadIdx.x < p.rot / 2) {
     double cosine, sine;
-    turn((double)pos * (double)p.inv_freq[threadIdx.x], &cosine, &sine);
+    turn((double)pos, (double)p.inv_freq[threadIdx.x], &cosine, &sine);
     cosines[threadIdx.x] = cosine;
     sines[threadIdx.x] = sine;
   }

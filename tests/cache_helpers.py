@@ -1,5 +1,7 @@
 """Plain 64-bit forms of the rotation and of the 4-bit store's format, on the CPU,
 and builders of 4-bit stores."""
+import math
+
 import torch
 
 from paper_2606_22968_amd import binding
@@ -109,3 +111,51 @@ def make_store4(seed, lens, bs, h_kv, d, spare=1, fill=0xFF):
         ks.append(k.to(torch.bfloat16))
         vs.append(v.to(torch.bfloat16))
     return pools, pools.to_gpu(), tables.cuda(), ks, vs
+
+
+# Angles from whole numbers: pi by Machin's formula, to 2^-400.
+_BITS = 400
+
+
+def _arctan_of_inverse(x):
+    term = (1 << _BITS + 20) // x
+    total, n, sign = term, 3, -1
+    while term:
+        term //= x * x
+        total += sign * (term // n)
+        n, sign = n + 2, -sign
+    return total
+
+
+_PI = (16 * _arctan_of_inverse(5) - 4 * _arctan_of_inverse(239)) >> 20
+
+
+def exact_turn(position, freq):
+    """cos and sin of position * freq (an fp32 value, finite), each within 2^-52 of it at any size."""
+    if position < 0:
+        c, s = exact_turn(-position, freq)
+        return c, -s
+    m, e = math.frexp(freq)
+    angle, shift = position * int(m * (1 << 24)), _BITS + e - 24
+    angle = angle << shift if shift >= 0 else angle >> -shift
+    n = (2 * angle + _PI // 2) // _PI                     # quarter turns, rounded
+    rest = (2 * angle - n * _PI) / (1 << _BITS + 1)       # within pi / 4
+    c, s = math.cos(rest), math.sin(rest)
+    return ((c, s), (-s, c), (-c, -s), (s, -c))[n % 4]
+
+
+def rotate_exact(x, positions, freq, interleaved, limit=2.0 ** 48):
+    """As rotate, with exact_turn; angles of `limit` or more, and those that are no number, make NaN pairs."""
+    x = x.double()
+    half = freq.numel()
+    out, size = x.clone(), x.abs()
+    for i in range(half):
+        a, b = (2 * i, 2 * i + 1) if interleaved else (i, i + half)
+        f, turns = float(freq[i]), []
+        for p in positions.tolist():
+            near = math.isfinite(f) and abs(p * f) < limit
+            turns.append(exact_turn(p, f) if near else (math.nan, math.nan))
+        c, s = torch.tensor(turns, dtype=torch.float64).T[:, :, None]
+        out[..., a], out[..., b] = x[..., a] * c - x[..., b] * s, x[..., a] * s + x[..., b] * c
+        size[..., a] = size[..., b] = x[..., a].abs() + x[..., b].abs()
+    return out, size
