@@ -95,8 +95,8 @@ mocap_status mocap_rope_append(const mocap_kv_store* kv, const int32_t* block_ta
                                const void* v, int64_t v_stride, void* q_out, void* stream);
 
 /*
- * mocap_decode_rope_append -- the same for the new token of every sequence of a
- * batch: its key and value are stored at position n_b - 1 (see
+ * mocap_decode_rope_append -- the same, to the bit, for the new token of every
+ * sequence of a batch: its key and value are stored at position n_b - 1 (see
  * mocap_decode_append).
  *
  *   positions     device int32 [batch]: the rotation's positions, or NULL: n_b - 1

@@ -34,7 +34,8 @@ namespace {
 // cos and sin of p f.  T: what the polynomials are evaluated in.  fp64 results are within 2^-52;
 // without the product's low part they would lose 2^-54 of the angle where p f has more than
 // 53 bits (1e-7 at positions near 2^31).  From kMaxAngle on, where the number of turns would lose
-// its fraction, they are NaN.
+// its fraction, they are NaN.  (Here and in rotate(), sums of products are written as they are
+// rounded: a token gets the same bits in a chunk and in a batch.)
 constexpr double kMaxAngle = 281474976710656.;  // 2^48
 template <typename T>
 __device__ __forceinline__ void turn(double p, double f, T* c, T* s) {
@@ -49,26 +50,26 @@ __device__ __forceinline__ void turn(double p, double f, T* c, T* s) {
   T sine, cosine;  // |r| < 0.81: the terms left out are below 1e-16 (fp32: 4e-9)
   if (sizeof(T) == 8) {
     sine = T(-1. / 1307674368000);
-    sine = sine * r2 + T(1. / 6227020800);
-    sine = sine * r2 + T(-1. / 39916800);
+    sine = fma(sine, r2, T(1. / 6227020800));
+    sine = fma(sine, r2, T(-1. / 39916800));
     cosine = T(1. / 20922789888000);
-    cosine = cosine * r2 + T(-1. / 87178291200);
-    cosine = cosine * r2 + T(1. / 479001600);
-    cosine = cosine * r2 + T(-1. / 3628800);
+    cosine = fma(cosine, r2, T(-1. / 87178291200));
+    cosine = fma(cosine, r2, T(1. / 479001600));
+    cosine = fma(cosine, r2, T(-1. / 3628800));
   } else {
     sine = T(0);
     cosine = T(-1. / 3628800);
   }
-  sine = sine * r2 + T(1. / 362880);
-  sine = sine * r2 + T(-1. / 5040);
-  sine = sine * r2 + T(1. / 120);
-  sine = sine * r2 + T(-1. / 6);
-  sine = sine * (r2 * r) + r;
-  cosine = cosine * r2 + T(1. / 40320);
-  cosine = cosine * r2 + T(-1. / 720);
-  cosine = cosine * r2 + T(1. / 24);
-  cosine = cosine * r2 + T(-0.5);
-  cosine = cosine * r2 + T(1);
+  sine = fma(sine, r2, T(1. / 362880));
+  sine = fma(sine, r2, T(-1. / 5040));
+  sine = fma(sine, r2, T(1. / 120));
+  sine = fma(sine, r2, T(-1. / 6));
+  sine = fma(sine, r2 * r, r);
+  cosine = fma(cosine, r2, T(1. / 40320));
+  cosine = fma(cosine, r2, T(-1. / 720));
+  cosine = fma(cosine, r2, T(1. / 24));
+  cosine = fma(cosine, r2, T(-0.5));
+  cosine = fma(cosine, r2, T(1));
   const uint32_t quarter = (uint32_t)__double2loint(shifted);
   const T a = quarter & 1 ? sine : cosine, b = quarter & 1 ? cosine : sine;
   *c = (quarter + 1) & 2 ? -a : a;
@@ -141,7 +142,7 @@ __device__ __forceinline__ void rotate(float* x, const Turns<T>& t, bool interle
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     const T a = (T)(interleaved ? x[2 * j] : x[j]), b = (T)(interleaved ? x[2 * j + 1] : x[8 + j]);
-    const float u = finish(a * t.c[j] - b * t.s[j]), v = finish(a * t.s[j] + b * t.c[j]);
+    const float u = finish(fma(a, t.c[j], -(b * t.s[j]))), v = finish(fma(a, t.s[j], b * t.c[j]));
     x[interleaved ? 2 * j : j] = u;
     x[interleaved ? 2 * j + 1 : 8 + j] = v;
   }
@@ -332,12 +333,14 @@ __global__ __launch_bounds__(4 * D) void rope_append_kernel(const RopeAppendLaun
 
 // ---- One token of every sequence of a batch ----
 // One wavefront: 64 / (D / 16) heads of one token, the KV heads before the query heads.
-// The heads share their angles, one a lane, through LDS (each thread its eight: 1 us more).
+// The heads share their angles, one a lane, through LDS (each thread its eight: 1 us more), in
+// fp32 for bf16 results and in fp64 for 4 bits, as in a chunk.
 template <int D, bool FOUR>
 __global__ __launch_bounds__(64) void decode_rope_append_kernel(const RopeAppendLaunch p) {
   constexpr int C = D / 16;
   __shared__ __attribute__((aligned(4))) uint8_t k_max[FOUR ? 64 / C * (D / 8) : 4];
-  __shared__ double cosines[D / 2], sines[D / 2];
+  __shared__ float cosines[D / 2], sines[D / 2];
+  __shared__ double key_cosines[FOUR ? D / 2 : 1], key_sines[FOUR ? D / 2 : 1];  // for 4 bits
   const int b = blockIdx.x;
   const int local = threadIdx.x / C, c = threadIdx.x % C;
   const int h = blockIdx.y * (64 / C) + local;
@@ -358,22 +361,21 @@ __global__ __launch_bounds__(64) void decode_rope_append_kernel(const RopeAppend
     load_pieces(p.v + b * p.v_stride + (int64_t)h * D, Piece{c * 16, c * 16 + 8, false}, v);
   }
   if ((int)threadIdx.x < p.rot / 2) {
-    double cosine, sine;
-    turn((double)pos, (double)p.inv_freq[threadIdx.x], &cosine, &sine);
-    cosines[threadIdx.x] = cosine;
-    sines[threadIdx.x] = sine;
+    const double f = p.inv_freq[threadIdx.x];
+    turn((double)pos, f, &cosines[threadIdx.x], &sines[threadIdx.x]);
+    if (FOUR) turn((double)pos, f, &key_cosines[threadIdx.x], &key_sines[threadIdx.x]);
   }
   __syncthreads();
-  auto shared_turns = [&](auto* t) __attribute__((always_inline)) {
+  auto shared_turns = [&](auto* t, const auto* cos, const auto* sin) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      t->c[j] = cosines[c * 8 + j];
-      t->s[j] = sines[c * 8 + j];
+      t->c[j] = cos[c * 8 + j];
+      t->s[j] = sin[c * 8 + j];
     }
   };
   if (is_q || (is_kv && !FOUR)) {
     Turns<float> t;
-    if (at.turned) shared_turns(&t);
+    if (at.turned) shared_turns(&t, cosines, sines);
     uint16_t* dst;
     if (is_q) {
       dst = p.q_out + ((int64_t)b * p.h_q + h - p.h_kv) * D;
@@ -413,7 +415,7 @@ __global__ __launch_bounds__(64) void decode_rope_append_kernel(const RopeAppend
       widen(x[1], y + 8);
       if (at.turned) {
         Turns<double> t;
-        shared_turns(&t);
+        shared_turns(&t, key_cosines, key_sines);
         rotate_any(p, y, t);
       }
       k_max[local * (D / 8) + at.first / 8] = (uint8_t)scale_byte(largest_bits(y));

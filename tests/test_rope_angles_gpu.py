@@ -107,3 +107,28 @@ def test_angles_beyond_their_limit(gpu, four, way):
         got = keys_of(store, tables, way, len(at))
         assert torch.equal(torch.isnan(got), gone_k)
         check_close(got[~gone_k], want_k[~gone_k], rotated_bound(want_k, k_size)[~gone_k], "k")
+
+
+@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("d,rot", [(64, 64), (128, 128), (128, 48)])
+@pytest.mark.parametrize("first", [0, 30000, (1 << 31) - 1000])
+def test_a_token_is_the_same_both_ways(gpu, four, interleaved, d, rot, first):
+    """A prompt's chunk and a batch's tokens at the same positions: the same bits of queries, keys and values."""
+    say(f"[case] rope both ways four={four} interleaved={interleaved} {rot} of {d} from {first}")
+    n, bs = 640, 64
+    rows = randn(320, n, H_Q + 2 * H_KV, d).cuda()
+    q, k, v = rows[:, :H_Q], rows[:, H_Q:H_Q + H_KV], rows[:, H_Q + H_KV:]
+    rope = binding.Rope((10000.0 ** (-torch.arange(0, rot, 2, dtype=torch.float64) / rot)).float().cuda(), interleaved)
+    kind = binding.Kv4Store if four else binding.KvStore
+    stores = [kind(n // bs, bs, H_KV, d, fill=0) for _ in range(2)]
+    outs = [torch.zeros((n, H_Q, d), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    table = torch.arange(n // bs, dtype=torch.int32, device="cuda")
+    (binding.mocap_kv4_append if four else binding.mocap_rope_append)(stores[0], table, 0, k, v, rope, first, q, outs[0])
+    lens = torch.arange(1, n + 1, dtype=torch.int32, device="cuda")
+    (binding.mocap_kv4_decode_append if four else binding.mocap_decode_rope_append)(
+        stores[1], table.repeat(n, 1), lens, k, v, rope, lens + (first - 1), q, outs[1])
+    pools = ("k_pool", "v_pool", "k_scale", "v_scale") if four else ("k_pool", "v_pool")
+    for name, (a, b) in dict(q=outs, **{x: [getattr(s, x) for s in stores] for x in pools}).items():
+        a, b = (x.view(torch.int16) if x.dtype is torch.bfloat16 else x for x in (a, b))
+        assert torch.equal(a, b), f"{name}: {int((a != b).sum())} of {a.numel()} differ"
