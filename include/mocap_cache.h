@@ -147,7 +147,9 @@ mocap_status mocap_kv4_load(const mocap_kv4_store* kv, const int32_t* block_tabl
  * mocap_decode_attn over a 4-bit store: the same arguments, results, precision
  * and errors (but blocks of any size are taken), with the values that the store
  * stands for.  A key block that reads as NaN makes the rows that see it NaN, a
- * value block its 32 dims of them.
+ * value block its 32 dims of them.  Weighted values are summed in fp32 before they
+ * are divided by the weights' sum: values up to 2^96 in magnitude never leave it, at
+ * any length; larger ones may make O infinite or NaN where it should be finite.
  */
 mocap_status mocap_kv4_decode_attn_workspace_size(int32_t batch, int64_t max_len, int32_t h_q, int32_t h_kv,
                                                   int32_t head_dim, int64_t window, int64_t sinks, size_t* bytes_out);
@@ -163,7 +165,8 @@ mocap_status mocap_kv4_decode_attn(const mocap_kv4_store* kv, const int32_t* blo
  * results and precision (probabilities in bf16, or nearer).  The chunk's own keys
  * and values are read from the store as well.  num_splits as in
  * mocap_window_attn_workspace_size.  NaN blocks reach exactly the rows that see
- * them, as in mocap_kv4_decode_attn.
+ * them, as in mocap_kv4_decode_attn.  Weights may exceed 1 here, by 2^62 a tile, so
+ * the values that never leave fp32 are those up to 2^40.
  * Errors: as mocap_window_attn, but window = 0 and blocks of any size are taken.
  */
 mocap_status mocap_kv4_chunk_attn_workspace_size(int64_t prefix_len, int32_t chunk_len, int32_t h_q, int32_t h_kv,

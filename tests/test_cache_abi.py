@@ -366,3 +366,15 @@ def test_rope_and_store_objects():
     s = binding.Kv4Store(3, 192, 2, 128, device="cpu", fill=7)
     assert s.k_pool.shape == (3, 2, 192, 64) and s.v_pool.shape == (3, 2, 3, 64, 64)
     assert s.k_scale.shape == s.v_scale.shape == (3, 2, 3, 4, 64) and int(s.v_scale.min()) == 7
+
+
+def test_the_extreme_values_run_every_way(host):
+    from test_kv4_extremes_gpu import WAYS
+
+    for way, (h_q, h_kv, P, L, splits, windows) in WAYS.items():
+        for d in (64, 128):
+            for window in windows:
+                kv = store4(block_size=64, num_blocks=4096, h_kv=h_kv, head_dim=d)
+                p = plan_of(host, kv=kv, n_table=4096, P=P, L=L, h_q=h_q, h_kv=h_kv, d=d, window=window, splits=splits)
+                rows = 256 if not p["few"] else 16 if L * h_q // h_kv <= 16 * p["row_blocks"] else 32
+                assert rows == way, (way, d, window, p)
