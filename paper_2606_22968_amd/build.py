@@ -6,6 +6,7 @@ instructions disabled in device code, then linked into one shared library.
 import os
 import subprocess
 import sys
+import warnings
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -57,7 +58,12 @@ def build(verbose: bool = False, extra_flags=(), lib_path: str = LIB, build_dir:
     _check_stubs(tmp)
     os.replace(tmp, lib_path)
     if lib_path == LIB:
-        build_marshal(verbose)
+        try:
+            build_marshal(verbose)
+        except Exception as e:  # no g++, or without the headers of Python or torch
+            if os.path.exists(MARSHAL):
+                os.remove(MARSHAL)
+            warnings.warn(f"the binding's shortcuts were not built, its calls take some us longer without them: {e}")
     return lib_path
 
 
@@ -82,7 +88,7 @@ def build_marshal(verbose: bool = False) -> str:
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         sys.stderr.write(res.stdout + res.stderr)
-        raise RuntimeError("g++ failed on marshal.cpp")
+        raise RuntimeError(f"{cmd[0]} failed on marshal.cpp")
     os.replace(tmp, MARSHAL)
     return MARSHAL
 
