@@ -8,16 +8,22 @@ missing this module raises instead of falling back to anything else.
 """
 import ctypes
 import os
+import warnings
 from typing import List, Optional, Sequence, Tuple
 
 import torch
 
 try:  # shortcuts in C++ (csrc/marshal.cpp): checks of a tensor in 0.1 us, and whole calls
     from . import _marshal
-    _address, _row_address = _marshal.address, _marshal.rows
 except ImportError:
     _marshal = None
-
+if _marshal is not None and getattr(_marshal, "torch_version", None) != torch.__version__:
+    # It reads torch's C++ objects, whose layout is that of the torch that it was built for.
+    warnings.warn(f"{_marshal.__file__} was built for another torch and is not used: build it again")
+    _marshal = None
+if _marshal is not None:
+    _address, _row_address = _marshal.address, _marshal.rows
+else:
     def _address(t, dtype, ndim: int, device: int) -> Optional[int]:
         if type(t) is torch.Tensor and t.dtype is dtype and t.get_device() == device and t.is_contiguous() and \
                 (ndim < 0 or t.dim() == ndim):

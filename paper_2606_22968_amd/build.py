@@ -6,6 +6,7 @@ instructions disabled in device code, then linked into one shared library.
 import os
 import subprocess
 import sys
+import sysconfig
 import warnings
 from concurrent.futures import ThreadPoolExecutor
 
@@ -67,20 +68,19 @@ def build(verbose: bool = False, extra_flags=(), lib_path: str = LIB, build_dir:
     return lib_path
 
 
-MARSHAL = os.path.join(PKG, "_marshal.so")
+# Named for the Python that it is built for; it holds the torch that it is built for.
+MARSHAL = os.path.join(PKG, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
 
 
 def build_marshal(verbose: bool = False) -> str:
     """The binding's shortcuts (csrc/marshal.cpp): a Python extension over torch's headers, host code only."""
-    import sysconfig
-
     import torch
     from torch.utils import cpp_extension
     includes = [*cpp_extension.include_paths(), sysconfig.get_path("include")]
     lib_dir = os.path.join(os.path.dirname(torch.__file__), "lib")
     tmp = MARSHAL + ".tmp"
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-w",
-           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DMOCAP_TORCH="{torch.__version__}"',
            *(f"-isystem{i}" for i in includes), f"-I{INCLUDE}", os.path.join(CSRC, "marshal.cpp"), "-o", tmp,
            f"-L{lib_dir}", "-lc10", "-ltorch_cpu", "-ltorch_python"]
     if verbose:
@@ -91,6 +91,16 @@ def build_marshal(verbose: bool = False) -> str:
         raise RuntimeError(f"{cmd[0]} failed on marshal.cpp")
     os.replace(tmp, MARSHAL)
     return MARSHAL
+
+
+def stale() -> list:
+    """Which of the library and the shortcuts are missing or older than what they are built from."""
+    headers = [os.path.join(INCLUDE, f) for f in os.listdir(INCLUDE)]
+    marshal = os.path.join(CSRC, "marshal.cpp")
+    sources = [os.path.join(CSRC, f) for f in os.listdir(CSRC)]
+    made_from = {LIB: headers + [s for s in sources if s != marshal], MARSHAL: headers + [marshal]}
+    return [made for made, parts in made_from.items()
+            if not os.path.exists(made) or any(os.path.getmtime(s) > os.path.getmtime(made) for s in parts)]
 
 
 def _check_stubs(lib: str) -> None:

@@ -448,5 +448,7 @@ PyMODINIT_FUNC PyInit__marshal() {
                {&n_interleaved, "interleaved"}};
   for (const auto& x : names)
     if ((*x.at = PyUnicode_InternFromString(x.name)) == nullptr) return nullptr;
-  return PyModule_Create(&module);
+  PyObject* m = PyModule_Create(&module);
+  if (m != nullptr && PyModule_AddStringConstant(m, "torch_version", MOCAP_TORCH) < 0) Py_CLEAR(m);
+  return m;
 }

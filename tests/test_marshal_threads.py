@@ -28,8 +28,8 @@ def host(tmp_path_factory):
     path = str(tmp_path_factory.mktemp("marshal") / "_marshal.so")
     includes = [*cpp_extension.include_paths(), sysconfig.get_path("include")]
     cmd = ["g++", "-O1", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-w",
-           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *(f"-isystem{i}" for i in includes),
-           f"-I{build.INCLUDE}", os.path.join(ROOT, "tests", "marshal_host.cpp"), "-o", path,
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", '-DMOCAP_TORCH="host"',
+           *(f"-isystem{i}" for i in includes), f"-I{build.INCLUDE}", os.path.join(ROOT, "tests", "marshal_host.cpp"), "-o", path,
            f"-L{os.path.join(os.path.dirname(torch.__file__), 'lib')}", "-lc10", "-ltorch_cpu", "-ltorch_python"]
     res = subprocess.run(cmd, capture_output=True, text=True)
     assert res.returncode == 0, res.stderr[-2000:]
