@@ -121,6 +121,10 @@ mocap_status plan_chunk(int64_t prefix_len, int32_t chunk_len, int32_t h_q, int3
 // 128/2/64 21.9 and 22.4, 40/2/128 21.9 and 21.2; at 24 64/1/64 29.4 and 27.7; at 64 128/2/64 61.1
 // and 52.3.
 constexpr int64_t kBlockTurns = 8;
+// Workgroups a compute unit, at most, of blocks of 16 heads of such groups: as for wide groups over the
+// bf16 store.  With so few turns it hardly matters: 2, 3, 4, 5 and 8 were within 2% of one another
+// for 40 batches (1 of 572 to 32 of 1024; 32/1/128, 64/1/64, 64/2/128, 40/2/128, 128/2/64).
+constexpr int kBlockGroupsPerCu = 3;
 mocap_status plan_batch_rows(int32_t batch, int64_t max_len, int32_t h_q, int32_t h_kv, int64_t window, int64_t sinks,
                              DecodeAttnLaunch* p) {
   mocap_status st = plan_decode(batch, max_len, h_q, h_kv, window, sinks, p);
@@ -134,7 +138,7 @@ mocap_status plan_batch_rows(int32_t batch, int64_t max_len, int32_t h_q, int32_
   const int64_t blocks = ceil_div(p->group, 16);
   if (batch * tiles * h_kv * blocks > kBlockTurns * 4 * cus) return MOCAP_OK;
   p->row_blocks = (int32_t)blocks;
-  return plan_batch(batch, max_len, window, sinks, h_kv * blocks, kDecodeWideGroupsPerCu, true, &p->seqs, &p->may_split);
+  return plan_batch(batch, max_len, window, sinks, h_kv * blocks, kBlockGroupsPerCu, true, &p->seqs, &p->may_split);
 }
 
 // ---- Rows ----

@@ -16,6 +16,9 @@
 // Measured: 2048 tokens of 32/8/128 heads behind 30720, 960 to 1030 us by the card, 1.03 to
 // 1.11 PFLOP/s.  Issue bounds it: MFMAs hold 45% of the SIMDs' cycles, a third of those beside
 // vector instructions (2.3 GHz).  The conversion is 5.5% of it, half of that the stores to LDS.
+// At head_dim 64 a tile has half the MFMAs beside the same exponentials, packing and sums (12 vector
+// instructions an MFMA for 6.6, 2 of them exponentials for 1): 2048 tokens of 16/2/64 behind 16384
+// 217 to 230 us, 0.64 to 0.67 PFLOP/s, MFMAs busy 26% of the cycles, vector instructions 49%.
 // Tried: a table entry looked up a tile ahead (no difference); pieces dealt to the lanes so
 // that those stores, 16 lanes over 32 banks, meet no bank twice, with loads 64 bytes apart
 // (1% more); the conversion of wavefronts 0-3 or 4-7 between the scores and the products or

@@ -3,7 +3,9 @@
 // are then as many heads of one token, each with its own last key.
 //
 // A key or value of d dims is d / 2 + d / 32 bytes and 4 d G FLOP for the G query
-// heads of a group: HBM bounds it still, at 3.8 times the keys a second.
+// heads of a group: HBM bounds groups of up to 16 heads still, at 3.8 times the keys a second.
+// Larger groups are bound by issue: each 16 or 32 of their heads load and convert a tile again,
+// and one wavefront carries that, the exponentials and the doubled P V product of its tile.
 //
 //   * How work is cut, the products, the softmax and the join are decode_attn.hip's:
 //     the fp4 values become bf16 in registers (exact), and enter the same bf16 MFMAs.
@@ -19,6 +21,8 @@
 // 5.3 TB/s, 5.9 without the 6 us that a launch of one tile a wavefront takes; 32 of up to
 // 8192, 32/8/128, 23 us for 83 MB; one of 2048, 6 us.  HBM and that latency bound it:
 // without V's conversion it takes 3% less, without the low halves of the probabilities 2%.
+// 32 of 32768 in larger groups, us and what their bytes take: 32/1/128 50 and 28, 64/1/128 75 and 28, 64/1/64
+// 51 and 14, 128/2/64 88 and 28, 64/2/128 83 and 56.
 // Tried: the next tile's codes in a second set of registers (two wavefronts a SIMD, 89
 // us), 1 to 9 workgroups per compute unit, parts of whole turns of the four wavefronts, 128
 // registers and four wavefronts a SIMD (6 to 37 of them spilled: 117 to 158 us), Q in LDS,
@@ -35,7 +39,8 @@ constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 
 // NT: 16-row blocks that a workgroup takes (1 or 2: see cache_api.cpp).  Rows are the heads of a sequence's group, or
-// (CHUNK) those of all tokens of a chunk, row r token r / G.
+// (CHUNK) those of all tokens of a chunk, row r token r / G.  (CHUNK with NT 2 keeps 39 scalar values, at head_dim 64
+// 45, in lanes of vector registers.)
 template <int D, int NT, bool CHUNK>
 __global__ __launch_bounds__(kThreads) void kv4_rows_kernel(
     const typename std::conditional<CHUNK, Kv4ChunkLaunch, Kv4DecodeLaunch>::type launch) {

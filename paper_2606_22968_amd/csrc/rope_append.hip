@@ -18,8 +18,10 @@
 //     every border between codes, so the one rounding that counts is exact.
 //   * V is stored with the positions contiguous, through LDS (see kv_append.hip).
 // Measured (kernel time, inputs out of cache): 2048 tokens of 32/8/128 heads 10.8 us into the
-// bf16 store (50 MB, 4.7 TB/s) and 12.4 into the 4-bit one (44 MB; all workgroups start at
-// once, so loads, angles and stores overlap little); 20011 tokens of 8 KV heads of 128,
+// bf16 store (50 MB, 4.7 TB/s) and 12.4 into the 4-bit one (44 MB).  All workgroups start at
+// once, and for 4 bits those of K and V take longer than those of Q: a chain of V's conversion
+// and turn, 8 fp64 angles, 16 fp64 products and K's conversion (passes with the rotation 9.8 us into
+// bf16 and 11.6 into 4 bits, without 9.4 and 8.9).  20011 tokens of 8 KV heads of 128,
 // without a rotation, into 4 bits 29 us (104 MB), of which 25 are its reads; without the
 // conversion and the turn in LDS 29.  One token 3.1 us, 32 of 32/8/128 4.2.  Tried, none
 // faster than +-2%: 2 or 8 query heads a workgroup, half the registers and a third more
